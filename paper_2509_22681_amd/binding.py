@@ -142,6 +142,44 @@ _lib.flame_climber_block_range.restype = C.c_int
 _lib.flame_climber_last_error.argtypes = []
 _lib.flame_climber_last_error.restype = C.c_char_p
 
+
+class flame_kv_config(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("scale", C.c_float)]
+
+
+class flame_kv_rows(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class flame_kv_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("slot_stride", C.c_int64), ("head_stride", C.c_int64),
+                ("n_pages", C.c_int32), ("page_size", C.c_int32), ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("pages_per_seq", C.c_int32)]
+
+
+class flame_kv_rotation(C.Structure):
+    _fields_ = [("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("frequencies", C.POINTER(C.c_double))]
+
+
+_kv_cfg, _kv_rows_p, _kv_cache_p = C.POINTER(flame_kv_config), C.POINTER(flame_kv_rows), C.POINTER(flame_kv_cache)
+_lib.flame_kv_append.argtypes = [_kv_cfg, _kv_cache_p, _kv_rows_p, _kv_rows_p, _kv_rows_p, _kv_rows_p, C.POINTER(flame_kv_rotation), C.c_void_p, C.c_void_p,
+                                 C.c_int32, C.c_int64, C.c_void_p, C.c_void_p]
+_lib.flame_kv_append.restype = C.c_int
+_lib.flame_kv_prompt.argtypes = [_kv_cfg, _kv_rows_p, _kv_rows_p, _kv_rows_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, _kv_rows_p, C.c_void_p, C.c_void_p]
+_lib.flame_kv_prompt.restype = C.c_int
+_lib.flame_kv_extend.argtypes = [_kv_cfg, _kv_cache_p, _kv_rows_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, _kv_rows_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+_lib.flame_kv_extend.restype = C.c_int
+_lib.flame_kv_decode.argtypes = [_kv_cfg, _kv_cache_p, _kv_rows_p, C.c_void_p, C.c_int32, _kv_rows_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+_lib.flame_kv_decode.restype = C.c_int
+_lib.flame_kv_workspace_bytes.argtypes = [_kv_cfg, C.c_int32, C.c_int64, C.POINTER(C.c_int64)]
+_lib.flame_kv_workspace_bytes.restype = C.c_int
+_lib.flame_kv_rotation_frequencies.argtypes = [C.c_int32, C.c_double, C.POINTER(C.c_double)]
+_lib.flame_kv_rotation_frequencies.restype = C.c_int
+_lib.flame_kv_last_error.argtypes = []
+_lib.flame_kv_last_error.restype = C.c_char_p
+
+KV_EXPORTS = ("flame_kv_append", "flame_kv_prompt", "flame_kv_extend", "flame_kv_decode", "flame_kv_workspace_bytes", "flame_kv_rotation_frequencies",
+              "flame_kv_last_error")
+
 CLIMBER_EXPORTS = ("flame_climber_head", "flame_climber_block_range", "flame_climber_last_error")
 
 DSO_EXPORTS = ("flame_dso_create", "flame_dso_submit", "flame_dso_submit_jagged", "flame_dso_wait", "flame_dso_drain", "flame_dso_flush", "flame_dso_destroy",
@@ -506,6 +544,175 @@ def flame_climber_head(head: Dict[str, object], hidden, fused, probs, stream=Non
     rc = _lib.flame_climber_head(C.byref(cfg), C.byref(ws), ptrs, rows, _ptr(fused), _ptr(probs), C.c_void_p(_stream_ptr(stream)))
     if rc != 0:
         raise FlameGRError(rc, _lib.flame_climber_last_error().decode())
+
+
+# ---------------------------------------------------------------------------------------------
+# softmax attention on a paged key/value cache (include/flame_kv.h).  Tensors are checked here for what the C side cannot see: shapes,
+# element types, and that they lie on the current device.
+# ---------------------------------------------------------------------------------------------
+FLAME_KV_F32, FLAME_KV_BF16, FLAME_KV_F16 = 0, 1, 2
+FLAME_KV_FAULT_PAGE, FLAME_KV_FAULT_LENGTH, FLAME_KV_FAULT_OFFSET = 1, 2, 4
+_KV_DTYPES = {"f32": FLAME_KV_F32, "bf16": FLAME_KV_BF16, "f16": FLAME_KV_F16}
+_KV_TORCH = (torch.float32, torch.bfloat16, torch.float16)
+
+
+def _kv_check(rc: int):
+    if rc != 0:
+        raise FlameGRError(rc, _lib.flame_kv_last_error().decode())
+
+
+def make_kv_config(dtype, n_q_heads, n_kv_heads, head_dim, scale=0.0) -> flame_kv_config:
+    """dtype: "f32", "bf16" or "f16"; scale of the logits, 0 for 1 / sqrt(head_dim)."""
+    return flame_kv_config(_KV_DTYPES.get(dtype, dtype), n_q_heads, n_kv_heads, head_dim, scale)
+
+
+def _kv_torch_dtype(cfg):
+    if not 0 <= cfg.dtype < 3:
+        raise ValueError("dtype must be f32, bf16 or f16")
+    return _KV_TORCH[cfg.dtype]
+
+
+def _kv_rows(cfg, t, heads: int, what: str, written: bool = False) -> flame_kv_rows:
+    rows, h, dim = t.shape
+    sr, sh, sd = t.stride()
+    if h != heads or dim != cfg.head_dim or t.dtype is not _kv_torch_dtype(cfg):
+        raise ValueError(f"{what} must be [rows, {heads}, {cfg.head_dim}] of {_kv_torch_dtype(cfg)}")
+    if rows and t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what} is not on the current device")
+    if sd != 1:
+        raise ValueError(f"{what}: the features of a head must lie side by side")
+    if written and ((sr == 0 and rows > 1) or (sh == 0 and h > 1)):
+        raise ValueError(f"{what} is written and must not be an expanded tensor")
+    # a stride of a dimension of one is never used, whatever torch says it is
+    return flame_kv_rows(t.data_ptr(), sr if rows > 1 else 0, sh if h > 1 else 0)
+
+
+def _kv_ints(t, n: int, what: str) -> int:
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] < n or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous int32 tensor of {n} entries")
+    if t.get_device() != torch.cuda.current_device():
+        raise ValueError(f"{what} is not on the current device")
+    return t.data_ptr()
+
+
+def _kv_workspace(workspace):
+    if workspace is None:
+        return None, 0
+    if not workspace.is_contiguous() or workspace.get_device() != torch.cuda.current_device():
+        raise ValueError("the workspace must be contiguous and on the current device")
+    return _ptr(workspace), workspace.numel() * workspace.element_size()
+
+
+def pack_kv_cache(cfg: flame_kv_config, k_pool, v_pool, page_table) -> flame_kv_cache:
+    """k_pool, v_pool: device tensors [n_pages, page_size, n_kv_heads, head_dim] (any strides, the same for both, features side by side: a pool
+    laid out [n_pages, n_kv_heads, page_size, head_dim] comes transposed); page_table: device int32 [n_seqs, pages_per_seq].  The struct keeps
+    the tensors alive; their contents may change."""
+    n_pages, page_size, heads, dim = k_pool.shape
+    if heads != cfg.n_kv_heads or dim != cfg.head_dim or k_pool.dtype is not _kv_torch_dtype(cfg):
+        raise ValueError(f"k_pool must be [n_pages, page_size, {cfg.n_kv_heads}, {cfg.head_dim}] of {_kv_torch_dtype(cfg)}")
+    if v_pool.shape != k_pool.shape or v_pool.dtype is not k_pool.dtype or v_pool.device != k_pool.device:
+        raise ValueError("v_pool must be like k_pool")
+    if page_table.dtype is not torch.int32 or page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table must be int32 [n_seqs, pages_per_seq], the entries of a row side by side")
+    if not k_pool.is_cuda or page_table.device != k_pool.device:
+        raise ValueError("the pools and the page table must be on one device")
+    used = [i for i in range(4) if k_pool.shape[i] > 1]
+    if [k_pool.stride(i) for i in used] != [v_pool.stride(i) for i in used] or k_pool.stride(3) != 1:
+        raise ValueError("k_pool and v_pool must have the same strides, and the features of a head side by side")
+    if any(k_pool.stride(i) == 0 for i in used):
+        raise ValueError("the pools must not be expanded tensors")
+    stride = [k_pool.stride(i) if k_pool.shape[i] > 1 else 0 for i in range(3)]
+    c = flame_kv_cache(k_pool.data_ptr(), v_pool.data_ptr(), *stride, n_pages, page_size, page_table.data_ptr(),
+                       page_table.stride(0) if page_table.shape[0] > 1 else 0, page_table.shape[1])
+    c.tensors = (k_pool, v_pool, page_table)
+    c.n_seqs, c.device, c.shape = page_table.shape[0], k_pool.get_device(), (cfg.dtype, heads, dim)
+    return c
+
+
+def _kv_cache_for(cfg, cache, n_seqs: int):
+    if cache.shape != (cfg.dtype, cfg.n_kv_heads, cfg.head_dim):
+        raise ValueError("the cache was packed for another configuration")
+    if cache.n_seqs < n_seqs:
+        raise ValueError("the page table has fewer rows than there are sequences")
+    if cache.device != torch.cuda.current_device():
+        raise ValueError("the cache is not on the current device")
+    return C.byref(cache)
+
+
+def make_kv_rotation(frequencies, interleaved: bool = False) -> flame_kv_rotation:
+    """frequencies: host float64 [rot_dim / 2], radians per position (flame_kv_rotation_frequencies, or those of any other scheme)."""
+    f = np.ascontiguousarray(frequencies, dtype=np.float64)
+    r = flame_kv_rotation(2 * f.size, int(bool(interleaved)), f.ctypes.data_as(C.POINTER(C.c_double)))
+    r.array = f
+    return r
+
+
+def flame_kv_rotation_frequencies(rot_dim: int, base: float = 10000.0) -> np.ndarray:
+    out = np.empty(max(rot_dim // 2, 0), np.float64)
+    _kv_check(_lib.flame_kv_rotation_frequencies(rot_dim, base, out.ctypes.data_as(C.POINTER(C.c_double))))
+    return out
+
+
+def flame_kv_workspace_bytes(cfg: flame_kv_config, n_seqs: int, n_tokens: Optional[int] = None) -> int:
+    """Bytes that flame_kv_extend needs for this many sequences and query rows; n_tokens None: flame_kv_decode."""
+    out = C.c_int64(0)
+    _kv_check(_lib.flame_kv_workspace_bytes(C.byref(cfg), n_seqs, n_seqs if n_tokens is None else n_tokens, C.byref(out)))
+    return out.value
+
+
+def flame_kv_append(cfg, cache, k, v, offsets, kv_lens, q=None, q_out=None, rotation=None, faults=None, stream=None) -> None:
+    """k, v: device rows [n_tokens, n_kv_heads, head_dim]; offsets [n_seqs + 1] and kv_lens [n_seqs] (with the new tokens): device int32;
+    q, q_out: rows [n_tokens, n_q_heads, head_dim]; rotation: make_kv_rotation or None; faults: device int32 [1] or None."""
+    n_seqs, n = kv_lens.shape[0], k.shape[0]
+    if v.shape[0] != n or (q is not None and (q.shape[0] != n or q_out is None or q_out.shape[0] != n)) or (q is None and q_out is not None):
+        raise ValueError("k, v, q and q_out must have the same rows, and q comes with q_out")
+    qr = qo = None
+    if q is not None:
+        qr, qo = C.byref(_kv_rows(cfg, q, cfg.n_q_heads, "q")), C.byref(_kv_rows(cfg, q_out, cfg.n_q_heads, "q_out", True))
+    rc = _lib.flame_kv_append(C.byref(cfg), _kv_cache_for(cfg, cache, n_seqs), C.byref(_kv_rows(cfg, k, cfg.n_kv_heads, "k")), C.byref(_kv_rows(cfg, v, cfg.n_kv_heads, "v")),
+                              qr, qo, C.byref(rotation) if rotation is not None else None, _kv_ints(offsets, n_seqs + 1, "offsets"), _kv_ints(kv_lens, n_seqs, "kv_lens"),
+                              n_seqs, n, None if faults is None else _kv_ints(faults, 1, "faults"), _stream_ptr(stream))
+    if rc:
+        _kv_check(rc)
+
+
+def flame_kv_prompt(cfg, q, k, v, q_offsets, out, k_offsets=None, faults=None, stream=None) -> None:
+    """q, out: device rows [n_tokens, n_q_heads, head_dim]; k, v: [n_keys, n_kv_heads, head_dim]; offsets: device int32 [n_seqs + 1]."""
+    n_seqs, n, n_keys = q_offsets.shape[0] - 1, q.shape[0], k.shape[0]
+    if out.shape[0] != n or v.shape[0] != n_keys:
+        raise ValueError("out must have the rows of q, and v those of k")
+    rc = _lib.flame_kv_prompt(C.byref(cfg), C.byref(_kv_rows(cfg, q, cfg.n_q_heads, "q")), C.byref(_kv_rows(cfg, k, cfg.n_kv_heads, "k")), C.byref(_kv_rows(cfg, v, cfg.n_kv_heads, "v")),
+                              _kv_ints(q_offsets, n_seqs + 1, "q_offsets"), None if k_offsets is None else _kv_ints(k_offsets, n_seqs + 1, "k_offsets"), n_seqs, n, n_keys,
+                              C.byref(_kv_rows(cfg, out, cfg.n_q_heads, "out", True)), None if faults is None else _kv_ints(faults, 1, "faults"), _stream_ptr(stream))
+    if rc:
+        _kv_check(rc)
+
+
+def flame_kv_extend(cfg, cache, q, q_offsets, kv_lens, out, workspace=None, faults=None, stream=None) -> None:
+    """q, out: device rows [n_tokens, n_q_heads, head_dim], the newest tokens of every sequence; q_offsets [n_seqs + 1], kv_lens [n_seqs]: device int32;
+    workspace: device tensor of at least flame_kv_workspace_bytes(cfg, n_seqs, n_tokens) bytes."""
+    n_seqs, n = kv_lens.shape[0], q.shape[0]
+    if out.shape[0] != n:
+        raise ValueError("out must have the rows of q")
+    wp, wb = _kv_workspace(workspace)
+    rc = _lib.flame_kv_extend(C.byref(cfg), _kv_cache_for(cfg, cache, n_seqs), C.byref(_kv_rows(cfg, q, cfg.n_q_heads, "q")), _kv_ints(q_offsets, n_seqs + 1, "q_offsets"),
+                              _kv_ints(kv_lens, n_seqs, "kv_lens"), n_seqs, n, C.byref(_kv_rows(cfg, out, cfg.n_q_heads, "out", True)), wp, wb,
+                              None if faults is None else _kv_ints(faults, 1, "faults"), _stream_ptr(stream))
+    if rc:
+        _kv_check(rc)
+
+
+def flame_kv_decode(cfg, cache, q, kv_lens, out, workspace=None, faults=None, stream=None) -> None:
+    """q, out: device rows [n_seqs, n_q_heads, head_dim], one new token of every sequence; kv_lens: device int32 [n_seqs];
+    workspace: device tensor of at least flame_kv_workspace_bytes(cfg, n_seqs) bytes."""
+    n_seqs = kv_lens.shape[0]
+    if q.shape[0] != n_seqs or out.shape[0] != n_seqs:
+        raise ValueError("q and out must have one row per sequence")
+    wp, wb = _kv_workspace(workspace)
+    rc = _lib.flame_kv_decode(C.byref(cfg), _kv_cache_for(cfg, cache, n_seqs), C.byref(_kv_rows(cfg, q, cfg.n_q_heads, "q")), _kv_ints(kv_lens, n_seqs, "kv_lens"), n_seqs,
+                              C.byref(_kv_rows(cfg, out, cfg.n_q_heads, "out", True)), wp, wb, None if faults is None else _kv_ints(faults, 1, "faults"), _stream_ptr(stream))
+    if rc:
+        _kv_check(rc)
 
 
 # ---------------------------------------------------------------------------------------------

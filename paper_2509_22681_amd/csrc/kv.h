@@ -1,0 +1,47 @@
+// The operators on a paged key/value cache (include/flame_kv.h): what the C entries hand to the kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/flame_kv.h"
+#include "kv_index.h"
+
+namespace flame {
+
+// rows of heads, strides in bytes
+struct KvRows {
+  char *p;
+  int64_t row, head;
+};
+
+constexpr int kMaxRotationPairs = 64;
+struct KvRotation {
+  int32_t pairs, interleaved;
+  uint64_t turns[kMaxRotationPairs];  // revolutions per position, modulo 1, times 2^64
+};
+
+// sequences of a batch: rows at offsets[b]..offsets[b+1] (NULL: row b), n_rows of them in the arrays
+struct KvBatch {
+  const int32_t *offsets, *kv_lens;
+  int32_t n_seqs;
+  int64_t n_rows;
+  int32_t *faults;
+};
+
+struct KvAttention {
+  KvBatch batch;
+  KvRows q, out;
+  KvRows k, v;                // packed keys (paged: unused)
+  const int32_t *k_offsets;
+  int64_t n_keys;
+  KvPages pages;              // paged keys: table != NULL
+  int32_t n_q_heads, n_kv_heads, head_dim, dtype;
+  float scale;
+};
+
+hipError_t launch_kv_append(const KvBatch &batch, const KvPages &pages, const KvRows &k, const KvRows &v, const KvRows *q, const KvRows *q_out,
+                            const KvRotation &rotation, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, hipStream_t stream);
+hipError_t launch_kv_attention(const KvAttention &a, void *workspace, hipStream_t stream);
+int64_t kv_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t n_seqs, int64_t n_tokens);
+
+}  // namespace flame

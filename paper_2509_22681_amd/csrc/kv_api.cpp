@@ -1,0 +1,194 @@
+// C entries of the operators on a paged key/value cache (include/flame_kv.h): checks of arguments, byte strides, launches.
+#include <cmath>
+
+#include "kv.h"
+
+using namespace flame;
+
+namespace {
+
+thread_local const char *g_kv_error = "";
+
+int bad(const char *message, int code = FLAME_GR_INVALID_ARGUMENT) {
+  g_kv_error = message;
+  return code;
+}
+
+int done(hipError_t e) {
+  if (e == hipSuccess) return FLAME_GR_OK;
+  return bad(hipGetErrorString(e), FLAME_GR_HIP_ERROR);
+}
+
+// A grid dimension may have 2^32 - 1 threads in all, and offsets are 32 bits: this many rows times heads is far beyond both a call's use and its memory.
+constexpr int64_t kMaxRowHeads = (int64_t)1 << 25;
+constexpr int32_t kMaxSequences = 1 << 22;
+
+int64_t element(int32_t dtype) { return dtype == FLAME_KV_F32 ? 4 : 2; }
+bool aligned(const void *p) { return ((uintptr_t)p & 15) == 0; }
+
+int check_config(const flame_kv_config *c) {
+  if (!c) return bad("the configuration is NULL");
+  if (c->dtype < FLAME_KV_F32 || c->dtype > FLAME_KV_F16) return bad("dtype must be a flame_kv_dtype");
+  if (c->n_kv_heads < 1 || c->n_q_heads < 1 || c->n_q_heads % c->n_kv_heads) return bad("n_q_heads must be a positive multiple of n_kv_heads");
+  if (c->n_q_heads > 4096) return bad("more than 4096 heads", FLAME_GR_UNSUPPORTED);
+  if (c->head_dim != 32 && c->head_dim != 64 && c->head_dim != 128) return bad("head_dim must be 32, 64 or 128", FLAME_GR_UNSUPPORTED);
+  if (!(c->scale >= 0.f) || !std::isfinite(c->scale)) return bad("scale must be finite and not negative");
+  return FLAME_GR_OK;
+}
+
+int check_batch(const flame_kv_config *c, int32_t n_seqs, int64_t n_rows) {
+  if (n_seqs < 0 || n_seqs > kMaxSequences) return bad("n_seqs out of range");
+  if (n_rows < 0 || n_rows * c->n_q_heads > kMaxRowHeads) return bad("rows times heads must be in [0, 2^25]");
+  return FLAME_GR_OK;
+}
+
+int take_rows(const flame_kv_config *c, const flame_kv_rows *r, KvRows *out) {
+  if (!r || !r->data) return bad("rows are NULL");
+  const int64_t size = element(c->dtype);
+  if (!aligned(r->data) || (r->row_stride * size) % 16 || (r->head_stride * size) % 16) return bad("rows must be 16-byte aligned, with strides of multiples of 16 bytes");
+  *out = KvRows{(char *)r->data, r->row_stride * size, r->head_stride * size};
+  return FLAME_GR_OK;
+}
+
+int take_pages(const flame_kv_config *c, const flame_kv_cache *cache, KvPages *out) {
+  if (!cache) return bad("the cache is NULL");
+  if (!cache->k || !cache->v || !cache->page_table) return bad("a pointer of the cache is NULL");
+  if (cache->n_pages < 1 || cache->page_size < 1 || cache->page_size > 65536) return bad("n_pages must be positive and page_size in [1, 65536]");
+  if (cache->pages_per_seq < 1 || (int64_t)cache->pages_per_seq * cache->page_size > INT32_MAX) return bad("pages_per_seq must be positive, and a sequence within 2^31 - 1 tokens");
+  const int64_t size = element(c->dtype);
+  if (!aligned(cache->k) || !aligned(cache->v) || (cache->page_stride * size) % 16 || (cache->slot_stride * size) % 16 || (cache->head_stride * size) % 16)
+    return bad("the cache must be 16-byte aligned, with strides of multiples of 16 bytes");
+  *out = KvPages{(char *)cache->k, (char *)cache->v, cache->page_stride * size, cache->slot_stride * size, cache->head_stride * size, cache->n_pages, 0, 0, 0,
+                 cache->page_table, cache->table_stride, cache->pages_per_seq * cache->page_size};
+  kv_set_page_size(out, cache->page_size);
+  return FLAME_GR_OK;
+}
+
+int take_rotation(const flame_kv_config *c, const flame_kv_rotation *r, KvRotation *out) {
+  *out = KvRotation{};
+  if (!r) return FLAME_GR_OK;
+  if (r->rot_dim < 16 || r->rot_dim % 16 || r->rot_dim > c->head_dim) return bad("rot_dim must be a multiple of 16 up to head_dim");
+  if (!r->frequencies) return bad("the frequencies are NULL");
+  out->pairs = r->rot_dim / 2;
+  out->interleaved = r->interleaved != 0;
+  for (int j = 0; j < out->pairs; ++j) {
+    if (!std::isfinite(r->frequencies[j])) return bad("a frequency is not finite");
+    // revolutions per position, of which only the fraction turns anything
+    const long double turns = (long double)r->frequencies[j] / 6.283185307179586476925286766559005768L;
+    const long double fraction = turns - floorl(turns);
+    out->turns[j] = fraction < 1.0L ? (uint64_t)ldexpl(fraction, 64) : 0;
+  }
+  return FLAME_GR_OK;
+}
+
+void take_heads(const flame_kv_config *c, KvAttention *a) {
+  a->n_q_heads = c->n_q_heads;
+  a->n_kv_heads = c->n_kv_heads;
+  a->head_dim = c->head_dim;
+  a->dtype = c->dtype;
+  a->scale = c->scale == 0.f ? 1.f / std::sqrt((float)c->head_dim) : c->scale;
+}
+
+int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_rows,
+                 const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream) {
+  KvAttention a{};
+  if (int rc = take_rows(cfg, q, &a.q)) return rc;
+  if (int rc = take_rows(cfg, out, &a.out)) return rc;
+  if (int rc = take_pages(cfg, cache, &a.pages)) return rc;
+  if (!kv_lens) return bad("kv_lens is NULL");
+  const int64_t need = kv_workspace_bytes(cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim, cfg->dtype, n_seqs, n_rows);
+  if (need > 0 && (!workspace || !aligned(workspace))) return bad("the workspace is NULL or not 16-byte aligned");
+  if (workspace_bytes < need) return bad("the workspace is smaller than flame_kv_workspace_bytes", FLAME_GR_CAPACITY_EXCEEDED);
+  a.batch = KvBatch{offsets, kv_lens, n_seqs, n_rows, faults};
+  take_heads(cfg, &a);
+  return done(launch_kv_attention(a, workspace, (hipStream_t)stream));
+}
+
+}  // namespace
+
+extern "C" {
+
+const char *flame_kv_last_error(void) { return g_kv_error; }
+
+int flame_kv_rotation_frequencies(int32_t rot_dim, double base, double *out) {
+  g_kv_error = "";
+  if (rot_dim < 2 || rot_dim % 2 || !out) return bad("rot_dim must be positive and even, out not NULL");
+  if (!(base > 0.0) || !std::isfinite(base)) return bad("base must be positive and finite");
+  for (int32_t j = 0; j < rot_dim / 2; ++j) out[j] = std::pow(base, -2.0 * j / rot_dim);
+  return FLAME_GR_OK;
+}
+
+int flame_kv_workspace_bytes(const flame_kv_config *cfg, int32_t n_seqs, int64_t n_tokens, int64_t *bytes) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
+  if (!bytes) return bad("bytes is NULL");
+  *bytes = kv_workspace_bytes(cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim, cfg->dtype, n_seqs, n_tokens);
+  return FLAME_GR_OK;
+}
+
+int flame_kv_append(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *k, const flame_kv_rows *v, const flame_kv_rows *q, const flame_kv_rows *q_out,
+                    const flame_kv_rotation *rotation, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_tokens, int32_t *faults, void *stream) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
+  if (!q != !q_out) return bad("q and q_out go together");
+  KvRotation rot;
+  if (int rc = take_rotation(cfg, rotation, &rot)) return rc;
+  if (n_seqs == 0 || n_tokens == 0) return FLAME_GR_OK;
+  KvRows kr, vr, qr, qo;
+  if (int rc = take_rows(cfg, k, &kr)) return rc;
+  if (int rc = take_rows(cfg, v, &vr)) return rc;
+  if (q) {
+    if (int rc = take_rows(cfg, q, &qr)) return rc;
+    if (int rc = take_rows(cfg, q_out, &qo)) return rc;
+  }
+  KvPages pages;
+  if (int rc = take_pages(cfg, cache, &pages)) return rc;
+  if (!offsets || !kv_lens) return bad("offsets or kv_lens is NULL");
+  return done(launch_kv_append(KvBatch{offsets, kv_lens, n_seqs, n_tokens, faults}, pages, kr, vr, q ? &qr : nullptr, &qo, rot, cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim, cfg->dtype,
+                               (hipStream_t)stream));
+}
+
+int flame_kv_prompt(const flame_kv_config *cfg, const flame_kv_rows *q, const flame_kv_rows *k, const flame_kv_rows *v, const int32_t *q_offsets, const int32_t *k_offsets,
+                    int32_t n_seqs, int64_t n_tokens, int64_t n_keys, const flame_kv_rows *out, int32_t *faults, void *stream) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
+  if (n_keys < 0 || n_keys > INT32_MAX) return bad("n_keys out of range");
+  if (n_seqs == 0 || n_tokens == 0) return FLAME_GR_OK;
+  KvAttention a{};
+  if (int rc = take_rows(cfg, q, &a.q)) return rc;
+  if (int rc = take_rows(cfg, out, &a.out)) return rc;
+  if (n_keys > 0) {
+    if (int rc = take_rows(cfg, k, &a.k)) return rc;
+    if (int rc = take_rows(cfg, v, &a.v)) return rc;
+  }
+  if (!q_offsets) return bad("q_offsets is NULL");
+  a.batch = KvBatch{q_offsets, nullptr, n_seqs, n_tokens, faults};
+  a.k_offsets = k_offsets;
+  a.n_keys = n_keys;
+  take_heads(cfg, &a);
+  return done(launch_kv_attention(a, nullptr, (hipStream_t)stream));
+}
+
+int flame_kv_extend(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *q_offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_tokens,
+                    const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
+  if (n_seqs == 0 || n_tokens == 0) return FLAME_GR_OK;
+  if (!q_offsets) return bad("q_offsets is NULL");
+  return attend_cache(cfg, cache, q, q_offsets, kv_lens, n_seqs, n_tokens, out, workspace, workspace_bytes, faults, stream);
+}
+
+int flame_kv_decode(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *kv_lens, int32_t n_seqs, const flame_kv_rows *out, void *workspace,
+                    int64_t workspace_bytes, int32_t *faults, void *stream) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (int rc = check_batch(cfg, n_seqs, n_seqs)) return rc;
+  if (n_seqs == 0) return FLAME_GR_OK;
+  return attend_cache(cfg, cache, q, nullptr, kv_lens, n_seqs, n_seqs, out, workspace, workspace_bytes, faults, stream);
+}
+
+}  // extern "C"

@@ -1,0 +1,46 @@
+// Device helpers of the operators on a paged key/value cache: whose row is this, how long is its sequence, where does a token lie.
+#pragma once
+#include "device_common.h"
+#include "kv.h"
+
+namespace flame {
+
+__device__ __forceinline__ void kv_fault(int32_t *faults, int32_t bits) {
+  if (faults) atomicOr(faults, bits);
+}
+
+// The sequence whose rows hold row t, for the wavefront: the number of b with offsets[b + 1] <= t.  64 probes at a time, so one
+// load's latency for up to 64 sequences and two up to 4096.  n_seqs where the row is behind the last sequence.  Whatever the
+// offsets hold, the probes stay within offsets[1..n_seqs].
+__device__ __forceinline__ int kv_find_sequence(const int32_t *offsets, int n_seqs, int64_t t, int lane) {
+  int lo = 0, n = n_seqs;
+  while (n > 64) {
+    const int step = (n + 63) / 64;
+    const int at = lo + min((lane + 1) * step, n);
+    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(offsets[at] <= t));
+    if (c * step >= n) return lo + n;
+    lo += c * step;
+    n = min(step, n - c * step);
+  }
+  const bool below = lane < n && offsets[lo + lane + 1] <= t;
+  return lo + __builtin_popcountll(__builtin_amdgcn_ballot_w64(below));
+}
+
+// Tokens of a sequence, within what its row of the table has room for.
+__device__ __forceinline__ int kv_clip_length(int len, int capacity, int32_t *faults, bool report) {
+  const int n = kv_clip(len, capacity);
+  if (report && n != len) kv_fault(faults, FLAME_KV_FAULT_LENGTH);
+  return n;
+}
+
+// Element type as a template argument of the launches.
+template <typename F> inline void kv_with_type(int32_t dtype, F f) {
+  if (dtype == FLAME_KV_F32) f(0.f);
+  else if (dtype == FLAME_KV_BF16) f((bf16_t)0.f);
+  else f((half_t)0.f);
+}
+
+// One rounding of an fp32 result, to nearest; an fp16 one past the largest finite value becomes infinite, as in IEEE arithmetic.
+template <typename T> __device__ __forceinline__ T kv_round(float v) { return (T)v; }
+
+}  // namespace flame

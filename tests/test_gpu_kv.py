@@ -1,0 +1,559 @@
+"""The operators on a paged key/value cache (include/flame_kv.h) against the oracle in 64 bits, on the same rounded inputs.
+
+Tolerances, per value, are derived from the roundings that the header allows.  Attention, with u the half step of the element type (2^-8 bf16, 2^-11 f16, 2^-24 f32),
+W = sum w |v| of the row and Z its largest scale * sum |q||k|:
+  a logit is off by (dim + 3) 2^-24 Z at most (fp32 accumulation, scale, product with log2 e) and its difference to the maximum by 4 * 2^-24 Z more; the exponential by 2^-22:
+  d = (dim + 7) 2^-24 Z + 2^-22 relative per weight, in numerator and denominator;
+  n fp32 additions in both: n 2^-24 each, and as much again for the factors of new maxima;
+  the weights' rounding u_w (16-bit types: u) in the numerator, and an absolute 2^-25 for f16 weights below its normal range (their sum is at least 1);
+  the output's rounding u |o|, and f16's smallest step.
+Rotation: three fp32 roundings of (|a| + |b|) and cosines off by 2^-21, then u of the value."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import kv_oracle
+
+pytestmark = pytest.mark.gpu
+
+HALF_STEP = {"bf16": 2.0 ** -8, "f16": 2.0 ** -11, "f32": 2.0 ** -24}
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def B():
+    import torch
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_2509_22681_amd import binding
+    return binding
+
+
+def torch_type(dtype):
+    import torch
+    return {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[dtype]
+
+
+def rand(gen, dtype, *shape):
+    import torch
+    return torch.randn(*shape, generator=gen, device=DEV).to(torch_type(dtype))
+
+
+def generator(seed):
+    import torch
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return g
+
+
+def ints(a):
+    import torch
+    return torch.tensor(np.asarray(a), dtype=torch.int32, device=DEV)
+
+
+def host(t):
+    return t.detach().double().cpu().numpy()
+
+
+def offsets(lengths):
+    return np.concatenate([[0], np.cumsum(lengths)]).astype(np.int32)
+
+
+def attention_bound(dtype, dim, n, want, spread, size):
+    u = HALF_STEP[dtype]
+    uw = 0.0 if dtype == "f32" else u
+    d = (dim + 7) * 2.0 ** -24 * size[..., None] + 2.0 ** -22
+    b = u * np.abs(want) + spread * (uw + 2 * d + 4 * n * 2.0 ** -24)
+    if dtype == "f16":
+        b = b + 2.0 ** -24 + n * 2.0 ** -25 * 6         # (the largest |v| here is below 6)
+    return b + 1e-30
+
+
+def check_attention(got, q, k, v, dtype, scale=None, seen=None, what=""):
+    """got [m, Hq, dim] of one sequence against the oracle on q, k, v (host arrays)."""
+    dim = q.shape[2]
+    want, spread, size = kv_oracle.attend(q, k, v, dim ** -0.5 if scale is None else scale, seen)
+    bound = attention_bound(dtype, dim, k.shape[0], want, spread, size)
+    off = np.abs(got - want)
+    assert np.isfinite(got).all(), what
+    assert (off <= bound).all(), (what, float((off / bound).max()), float(off.max()))
+
+
+class Cache:
+    """Sequences of n tokens in scattered pages of a pool of random values, with a few pages that nobody has."""
+
+    def __init__(self, B, gen, dtype, hq, hkv, dim, lens, page, head_major=False, seed=0, room=0, extra_rows=0):
+        self.cfg, self.page, self.lens = B.make_kv_config(dtype, hq, hkv, dim), page, list(lens)
+        used = [-(-(n + room) // page) for n in lens]
+        self.n_pages = sum(used) + 3
+        shape = (self.n_pages, hkv, page, dim) if head_major else (self.n_pages, page, hkv, dim)
+        self.k, self.v = rand(gen, dtype, *shape), rand(gen, dtype, *shape)
+        if head_major:
+            self.k, self.v = self.k.transpose(1, 2), self.v.transpose(1, 2)
+        order = np.random.default_rng(seed).permutation(self.n_pages)
+        self.table_host = np.full((len(lens) + extra_rows, max(used + [1]) + 1), -7, np.int32)       # entries that nobody reads name no page
+        for b, first in enumerate(np.cumsum([0] + used[:-1])):
+            self.table_host[b, :used[b]] = order[first:first + used[b]]
+        self.table = ints(self.table_host)
+        self.packed = B.pack_kv_cache(self.cfg, self.k, self.v, self.table)
+
+    def rows(self, b, n):
+        page, slot, ok = kv_oracle.page_rows(self.table_host[b], self.page, self.n_pages, n)
+        k, v = host(self.k), host(self.v)
+        return k[page, slot], v[page, slot]
+
+
+# ---------------------------------------------------------------------------------------------- append
+@pytest.mark.parametrize("dtype,hq,hkv,dim,rot,inter,page,head_major", [
+    ("bf16", 8, 2, 64, 64, False, 16, False), ("bf16", 32, 8, 128, 128, True, 24, True), ("f16", 4, 4, 32, 32, False, 1, False), ("f16", 6, 1, 128, 64, False, 7, False),
+    ("f32", 8, 8, 64, 32, True, 100, True), ("f32", 3, 3, 128, 128, False, 16, False), ("bf16", 5, 5, 32, 16, True, 64, False), ("f32", 2, 1, 32, 0, False, 5, False)])
+def test_append(B, dtype, hq, hkv, dim, rot, inter, page, head_major):
+    import torch
+    gen = generator(dim + page)
+    new, before = [1, 0, 5, 70, 1, 33], [0, 9, 100, 3, 47, 64]
+    lens = [a + b for a, b in zip(new, before)]
+    c = Cache(B, gen, dtype, hq, hkv, dim, lens, page, head_major)
+    n = sum(new)
+    rows = rand(gen, dtype, n + 3, hq + 2 * hkv, dim)                   # slices of wider rows, three rows behind the last sequence
+    q, k, v = rows[:, :hq], rows[:, hq:hq + hkv], rows[:, hq + hkv:]
+    q_out = torch.full((n + 3, hq, dim), 7.0, device=DEV, dtype=torch_type(dtype))
+    f = B.flame_kv_rotation_frequencies(rot) if rot else np.zeros(0)
+    want_k, want_v = host(c.k), host(c.v)
+    keep_k, keep_v = c.k.clone(), c.v.clone()
+    faults = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kv_append(c.cfg, c.packed, k, v, ints(offsets(new)), ints(lens), q=q, q_out=q_out, rotation=B.make_kv_rotation(f, inter) if rot else None, faults=faults)
+    torch.cuda.synchronize()
+    assert int(faults[0]) == 0
+    position = np.concatenate([np.arange(a, a + m) for a, m in zip(before, new)])
+    seq = np.repeat(np.arange(len(new)), new)
+    page_of, slot = c.table_host[seq, position // page], position % page
+
+    def near(got, x, what):
+        turned = kv_oracle.rotate(x, position, f, inter)
+        pair = np.abs(x).max(-1, keepdims=True) * 2
+        bound = HALF_STEP[dtype] * np.abs(turned) + (pair * 2.0 ** -21 if rot else 0) + (2.0 ** -25 if dtype == "f16" else 0)
+        assert (np.abs(got - turned) <= bound).all(), (what, np.abs(got - turned).max())
+
+    near(host(c.k)[page_of, slot], host(k[:n]), "k")
+    near(host(q_out)[:n], host(q[:n]), "q")
+    assert np.array_equal(host(c.v)[page_of, slot], host(v[:n]))
+    assert bool((q_out[n:] == 7.0).all())                               # rows behind the last sequence
+    untouched = np.ones(want_k.shape[:2], bool)
+    untouched[page_of, slot] = False
+    assert np.array_equal(host(c.k)[untouched], host(keep_k)[untouched]) and np.array_equal(host(c.v)[untouched], host(keep_v)[untouched])
+    # in place, and without queries: the same bits
+    first, again = c.k.clone(), q.clone()
+    B.flame_kv_append(c.cfg, c.packed, k, v, ints(offsets(new)), ints(lens), q=again, q_out=again, rotation=B.make_kv_rotation(f, inter) if rot else None)
+    assert torch.equal(again[:n], q_out[:n]) and torch.equal(again[n:], q[n:]) and torch.equal(c.k, first)
+    c.k.copy_(keep_k)
+    B.flame_kv_append(c.cfg, c.packed, k, v, ints(offsets(new)), ints(lens), rotation=B.make_kv_rotation(f, inter) if rot else None)
+    assert torch.equal(c.k, first)
+
+
+@pytest.mark.parametrize("inter", [False, True])
+def test_append_far_positions(B, inter):
+    """Angles of positions up to 2^31 - 2^16: the table names the same few pages again and again."""
+    import torch
+    gen, page, width = generator(1), 65536, 32767
+    cfg = B.make_kv_config("f32", 2, 1, 64)
+    k_pool, v_pool = torch.zeros(2, page, 1, 64, device=DEV), torch.zeros(2, page, 1, 64, device=DEV)
+    cache = B.pack_kv_cache(cfg, k_pool, v_pool, torch.ones(3, width, dtype=torch.int32, device=DEV))
+    lens = np.array([page * width, (1 << 30) + 12345, 100003], np.int64)
+    q, k = rand(gen, "f32", 6, 2, 64), rand(gen, "f32", 6, 1, 64)
+    f = B.flame_kv_rotation_frequencies(64, 10000.0)
+    f[1] *= -1
+    f[2] = 5.0                                                          # more than a revolution in eight positions, and a turn to the other side
+    out = torch.empty_like(q)
+    B.flame_kv_append(cfg, cache, k, k, ints([0, 2, 4, 6]), ints(lens), q=q, q_out=out, rotation=B.make_kv_rotation(f, inter))
+    position = np.concatenate([[n - 2, n - 1] for n in lens])
+    want = kv_oracle.rotate(host(q), position, f, inter)
+    # the frequency's own rounding to 64 bits: 2^31 * 2^-64 revolutions, far below the bound
+    assert np.abs(host(out) - want).max() <= 2.0 ** -24 * np.abs(want).max() + 2 * np.abs(host(q)).max() * 2.0 ** -21
+    turned = kv_oracle.rotate(host(k), position, f, inter)
+    assert np.abs(host(k_pool)[1, position % page] - turned).max() <= 2.0 ** -24 * np.abs(turned).max() + 2 * np.abs(host(k)).max() * 2.0 ** -21
+
+
+def test_append_reports_what_it_cannot_place(B):
+    """Bad pages, lengths beyond the table's row and below the new tokens, offsets that decrease: nothing out of range is written, and the rest is."""
+    import torch
+    gen = generator(2)
+    cfg = B.make_kv_config("bf16", 2, 1, 32)
+    pool_k, pool_v = torch.zeros(6, 4, 1, 32, device=DEV, dtype=torch.bfloat16), torch.zeros(6, 4, 1, 32, device=DEV, dtype=torch.bfloat16)
+    guard_k, guard_v = pool_k[1:5], pool_v[1:5]                         # pages on both sides that no entry may reach
+    k = rand(gen, "bf16", 12, 1, 32)
+
+    def append(table, off, lens):
+        pool_k.zero_(), pool_v.zero_()
+        faults = torch.zeros(1, dtype=torch.int32, device=DEV)
+        B.flame_kv_append(cfg, B.pack_kv_cache(cfg, guard_k, guard_v, ints(table)), k, k, ints(off), ints(lens), faults=faults)
+        torch.cuda.synchronize()
+        assert not pool_k[0].any() and not pool_k[5].any() and not pool_v[0].any() and not pool_v[5].any()
+        assert torch.equal(pool_k, pool_v)
+        return int(faults[0]), [tuple(x) for x in (pool_k[1:5].abs().sum((2, 3)) > 0).nonzero().tolist()]
+
+    assert append([[0, 1], [2, 3]], [0, 2, 4], [2, 8]) == (0, [(0, 0), (0, 1), (3, 2), (3, 3)])
+    assert append([[0, 4], [-1, 3]], [0, 2, 6], [6, 6]) == (1, [(3, 0), (3, 1)])
+    assert append([[0, 1], [2, 3]], [0, 3, 5], [2, 9]) == (2, [(0, 0), (0, 1), (3, 3)])
+    append([[0, 1], [2, 3]], [0, 4, 2], [4, 2])                         # offsets that decrease
+    append([[0, 1], [2, 3]], [-3, 4, 5], [4, 2])
+    fault, there = append([[0, 1], [2, 3]], [0, 8, 20], [8, 8])         # twelve rows are there, and eight of the second sequence are not
+    assert fault & 4 and all(p in (0, 1, 2, 3) for p, _ in there)
+
+
+# ---------------------------------------------------------------------------------------------- prompt
+HEADS = [("bf16", 8, 2, 64), ("bf16", 4, 4, 128), ("f16", 6, 2, 128), ("f16", 3, 3, 32), ("bf16", 8, 1, 32), ("f16", 4, 4, 64), ("f32", 4, 2, 64), ("f32", 2, 2, 128), ("f32", 3, 1, 32)]
+LENGTHS = [[1], [0, 1, 2, 0, 31, 32, 33], [63, 64, 65, 1], [127, 128, 129], [300, 5, 257], [700]]
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim", HEADS)
+@pytest.mark.parametrize("lengths", LENGTHS, ids=str)
+def test_prompt(B, dtype, hq, hkv, dim, lengths):
+    import torch
+    gen, n = generator(len(lengths) + dim), sum(lengths)
+    rows = rand(gen, dtype, n + 5, hq + 2 * hkv, dim)
+    q, k, v = rows[:, :hq], rows[:, hq:hq + hkv], rows[:, hq + hkv:]
+    out = torch.full((n + 5, hq, dim), 7.0, device=DEV, dtype=torch_type(dtype))
+    off, faults = offsets(lengths), torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kv_prompt(B.make_kv_config(dtype, hq, hkv, dim), q, k, v, ints(off), out, faults=faults)
+    torch.cuda.synchronize()
+    assert int(faults[0]) == 0 and bool((out[n:] == 7.0).all())
+    for b, m in enumerate(lengths):
+        s = slice(off[b], off[b + 1])
+        check_attention(host(out[s]), host(q[s]), host(k[s]), host(v[s]), dtype, what=(lengths, b))
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 8, 2, 64), ("f16", 4, 4, 128), ("f32", 2, 1, 64), ("bf16", 4, 2, 32)])
+def test_prompt_with_other_key_lengths(B, dtype, hq, hkv, dim):
+    """More keys than queries, fewer (rows that see nothing are zeros), none; a scale; head-major queries and outputs; one fault bit for offsets behind the rows."""
+    import torch
+    gen, nq, nk = generator(dim), [5, 40, 3, 0, 130, 7], [70, 10, 0, 20, 131, 7]
+    q = rand(gen, dtype, hq, sum(nq), dim).transpose(0, 1)
+    k, v = rand(gen, dtype, hkv, sum(nk), dim).transpose(0, 1), rand(gen, dtype, sum(nk), hkv, dim)
+    out = torch.full((hq, sum(nq), dim), 7.0, device=DEV, dtype=torch_type(dtype)).transpose(0, 1)
+    cfg, qo, ko = B.make_kv_config(dtype, hq, hkv, dim, scale=0.3), offsets(nq), offsets(nk)
+    B.flame_kv_prompt(cfg, q, k, v, ints(qo), out, k_offsets=ints(ko))
+    for b in range(len(nq)):
+        sq, sk = slice(qo[b], qo[b + 1]), slice(ko[b], ko[b + 1])
+        check_attention(host(out[sq]), host(q[sq]), host(k[sk]), host(v[sk]), dtype, scale=float(np.float32(0.3)), what=b)
+        hidden = max(0, nq[b] - nk[b])
+        assert not out[sq][:hidden].any()
+    faults = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kv_prompt(cfg, q, k, v, ints(qo), out, k_offsets=ints(ko + 1), faults=faults)
+    assert int(faults[0]) == 4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+def test_prompt_rows_do_not_feel_what_they_do_not_see(B, dtype, dim):
+    """Later tokens of the same sequence and other sequences hold infinities and NaN: earlier rows keep their bits, rows that see a NaN value have it, and one that sees an infinite value is infinite there."""
+    import torch
+    gen, lengths = generator(3), [200, 90]
+    cfg, off = B.make_kv_config(dtype, 4, 2, dim), offsets([200, 90])
+    q, k, v = rand(gen, dtype, 290, 4, dim), rand(gen, dtype, 290, 2, dim), rand(gen, dtype, 290, 2, dim)
+    clean, dirty = torch.empty_like(q), torch.empty_like(q)
+    B.flame_kv_prompt(cfg, q, k, v, ints(off), clean)
+    for at in (0, 77, 130, 199):
+        for value, where in ((math.nan, "v"), (math.inf, "v"), (-math.inf, "v"), (math.nan, "k"), (math.inf, "k")):
+            k2, v2 = k.clone(), v.clone()
+            (v2 if where == "v" else k2)[at, 1, 3] = value
+            B.flame_kv_prompt(cfg, q, k2, v2, ints(off), dirty)
+            assert torch.equal(dirty[:at], clean[:at]) and torch.equal(dirty[200:], clean[200:]), (at, value, where)
+            assert torch.equal(dirty[:, :2], clean[:, :2])              # query heads of the other key head
+            if where == "v":
+                changed = dirty[at:200, 2:, 3].float()
+                assert bool((changed.isnan() if math.isnan(value) else changed == value).all()), (at, value)
+                others = [i for i in range(dim) if i != 3]
+                assert torch.equal(dirty[:, :, others], clean[:, :, others])
+            elif math.isnan(value):
+                assert bool(dirty[at:200, 2:].isnan().all())
+
+
+def test_prompt_of_large_logits(B):
+    """Logits of hundreds, of both signs: the maximum is taken out before the exponential, wherever in the row it comes."""
+    import torch
+    gen = generator(4)
+    for dtype, dim in (("bf16", 64), ("f16", 128), ("f32", 32)):
+        q, k, v = 30 * rand(gen, dtype, 400, 2, dim), 3 * rand(gen, dtype, 400, 2, dim), rand(gen, dtype, 400, 2, dim)
+        out = torch.empty_like(q)
+        B.flame_kv_prompt(B.make_kv_config(dtype, 2, 2, dim), q, k, v, ints([0, 400]), out)
+        check_attention(host(out), host(q), host(k), host(v), dtype, what=dtype)
+
+
+# ---------------------------------------------------------------------------------------------- extend and decode
+def workspace_for(B, cfg, n_seqs, n_tokens=None):
+    import torch
+    return torch.full((B.flame_kv_workspace_bytes(cfg, n_seqs, n_tokens),), 0xff, dtype=torch.uint8, device=DEV)     # it holds nothing between calls: NaN
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim", HEADS + [("bf16", 32, 1, 64), ("f16", 40, 2, 32), ("f32", 20, 1, 64)])
+@pytest.mark.parametrize("page,head_major", [(16, False), (24, True), (1, False), (300, True)])
+def test_decode(B, dtype, hq, hkv, dim, page, head_major):
+    import torch
+    gen, lens = generator(page), [1, 0, 31, 32, 33, 700, 64, 129]
+    c = Cache(B, gen, dtype, hq, hkv, dim, lens, page, head_major)
+    q = rand(gen, dtype, len(lens), hq, dim)
+    out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kv_decode(c.cfg, c.packed, q, ints(lens), out, workspace_for(B, c.cfg, len(lens)), faults=faults)
+    assert int(faults[0]) == 0
+    for b, n in enumerate(lens):
+        check_attention(host(out[b:b + 1]), host(q[b:b + 1]), *c.rows(b, n), dtype, what=(b, n))
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 8, 2, 64), ("f16", 4, 4, 128), ("f32", 4, 2, 64), ("bf16", 16, 2, 128), ("f16", 6, 3, 32)])
+@pytest.mark.parametrize("new,lens,page", [([1, 3, 0, 7, 2], [1, 400, 20, 65, 2], 16), ([40, 200, 1], [40, 333, 600], 24), ([5, 9], [3, 0], 8), ([130], [1000], 64)], ids=str)
+def test_extend(B, dtype, hq, hkv, dim, new, lens, page):
+    import torch
+    gen = generator(len(new))
+    c = Cache(B, gen, dtype, hq, hkv, dim, lens, page)
+    off, n = offsets(new), sum(new)
+    q = rand(gen, dtype, n + 4, hq, dim)
+    out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kv_extend(c.cfg, c.packed, q, ints(off), ints(lens), out, workspace_for(B, c.cfg, len(lens), n + 4), faults=faults)
+    assert int(faults[0]) == 0 and bool((out[n:] == 7.0).all())
+    for b, n_b in enumerate(lens):
+        s = slice(off[b], off[b + 1])
+        check_attention(host(out[s]), host(q[s]), *c.rows(b, n_b), dtype, what=(b, n_b))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_bad_pages_and_lengths(B, dtype):
+    """Keys in a page that the table does not name are not seen; lengths are cut to what the table has room for; both are reported."""
+    import torch
+    gen, lens = generator(5), [150, 90]
+    c = Cache(B, gen, dtype, 4, 2, 64, lens, 16)
+    q = rand(gen, dtype, 6, 4, 64)
+    for entry in (-1, c.n_pages, 2 ** 31 - 1, -2 ** 31):
+        table = c.table_host.copy()
+        table[0, 3] = entry
+        packed = B.pack_kv_cache(c.cfg, c.k, c.v, ints(table))
+        seen = np.arange(150) // 16 != 3
+        keys, values = c.rows(0, 150)
+        for new in (1, 5):
+            rows = q[:2] if new == 1 else q
+            out, faults = torch.empty_like(rows), torch.zeros(1, dtype=torch.int32, device=DEV)
+            if new == 1:
+                B.flame_kv_decode(c.cfg, packed, rows, ints(lens), out, workspace_for(B, c.cfg, 2), faults=faults)
+            else:
+                B.flame_kv_extend(c.cfg, packed, rows, ints([0, 5, 6]), ints(lens), out, workspace_for(B, c.cfg, 2, 6), faults=faults)
+            assert int(faults[0]) == 1
+            check_attention(host(out[:new]), host(rows[:new]), keys, values, dtype, seen=seen, what=(entry, new))
+            check_attention(host(out[new:]), host(rows[new:]), *c.rows(1, 90), dtype, what=(entry, new))
+    # every page bad: nothing is seen, zeros
+    packed = B.pack_kv_cache(c.cfg, c.k, c.v, torch.full_like(c.table, -1))
+    out = torch.full_like(q[:2], 7.0)
+    B.flame_kv_decode(c.cfg, packed, q[:2], ints(lens), out, workspace_for(B, c.cfg, 2))
+    assert not out.any()
+    # lengths: below 0 is 0, beyond the row's room is the room
+    width = c.table_host.shape[1]
+    table = np.resize(c.table_host[0, :9], (2, width)).astype(np.int32)
+    packed = B.pack_kv_cache(c.cfg, c.k, c.v, ints(table))
+    faults = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kv_decode(c.cfg, packed, q[:2], ints([-5, 2 ** 31 - 1]), out, workspace_for(B, c.cfg, 2), faults=faults)
+    assert int(faults[0]) == 2 and not out[0].any()
+    page, slot, _ = kv_oracle.page_rows(table[1], 16, c.n_pages, 16 * width)
+    check_attention(host(out[1:]), host(q[1:2]), host(c.k)[page, slot], host(c.v)[page, slot], dtype, what="room")
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_unused_slots_and_unseen_tokens_do_not_count(B, dtype):
+    """Slots behind the last token, pages of others and tokens that a row does not see hold NaN: no output changes a bit."""
+    import torch
+    gen, lens = generator(6), [100, 37, 1]
+    c = Cache(B, gen, dtype, 4, 2, 128, lens, 16)
+    q, ws = rand(gen, dtype, 9, 4, 128), workspace_for(B, c.cfg, 3, 9)
+    clean, dirty = torch.empty_like(q), torch.empty_like(q)
+    off = ints([0, 4, 8, 9])
+    B.flame_kv_extend(c.cfg, c.packed, q, off, ints(lens), clean, ws)
+    single = torch.empty_like(q[:3])
+    B.flame_kv_decode(c.cfg, c.packed, q[:3], ints(lens), single, ws)
+    owned = np.zeros((c.n_pages, 16), bool)
+    for b, n in enumerate(lens):
+        page, slot, _ = kv_oracle.page_rows(c.table_host[b], 16, c.n_pages, n)
+        owned[page, slot] = True
+    for pool in (c.k, c.v):
+        pool[torch.from_numpy(~owned).to(DEV)] = math.nan
+    B.flame_kv_extend(c.cfg, c.packed, q, off, ints(lens), dirty, ws)
+    again = torch.empty_like(single)
+    B.flame_kv_decode(c.cfg, c.packed, q[:3], ints(lens), again, ws)
+    assert torch.equal(clean, dirty) and torch.equal(single, again)
+    # the newest token of sequence 0: of its four rows only the last sees it
+    page, slot, _ = kv_oracle.page_rows(c.table_host[0], 16, c.n_pages, 100)
+    for pool in (c.v, c.k):
+        pool[int(page[99]), int(slot[99])] = math.nan
+        B.flame_kv_extend(c.cfg, c.packed, q, off, ints(lens), dirty, ws)
+        assert torch.equal(clean[:3], dirty[:3]) and torch.equal(clean[4:], dirty[4:]) and bool(dirty[3].isnan().all())
+
+
+def test_pools_beyond_32_bits(B):
+    """Pools of 5 GiB: a sequence in the last pages of them."""
+    import torch
+    gen, pages = generator(7), 81920
+    cfg = B.make_kv_config("bf16", 8, 4, 128)
+    k, v = (torch.empty(pages, 64, 4, 128, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    names = [81919, 40000, 81900, 2, 70000]
+    for pool in (k, v):
+        for p in names:
+            pool[p] = rand(gen, "bf16", 64, 4, 128)
+    cache, n = B.pack_kv_cache(cfg, k, v, ints([names])), 300
+    new, q = rand(gen, "bf16", 2, 4, 128), rand(gen, "bf16", 2, 8, 128)
+    B.flame_kv_append(cfg, cache, new, new, ints([0, 2]), ints([n]))
+    keys = torch.cat([k[p] for p in names])[:n]
+    values = torch.cat([v[p] for p in names])[:n]
+    assert torch.equal(keys[n - 2:], new) and torch.equal(values[n - 2:], new)
+    out = torch.empty_like(q)
+    B.flame_kv_extend(cfg, cache, q, ints([0, 2]), ints([n]), out, workspace_for(B, cfg, 1, 2))
+    check_attention(host(out), host(q), host(keys), host(values), "bf16")
+    B.flame_kv_decode(cfg, cache, q[1:], ints([n]), out[1:], workspace_for(B, cfg, 1))
+    check_attention(host(out[1:]), host(q[1:]), host(keys), host(values), "bf16")
+
+
+# ---------------------------------------------------------------------------------------------- together
+@pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 8, 2, 64), ("f16", 8, 8, 128), ("f32", 4, 2, 32)])
+def test_a_history_that_grows(B, dtype, hq, hkv, dim):
+    """As a server runs them: prompts go into the cache and are attended to from there, then in pieces, then token by token; every row is that of attention within the whole sequence."""
+    import torch
+    gen, steps = generator(8), [[70, 0, 33], [1, 50, 1], [1, 1, 1], [0, 1, 130], [1, 1, 1]]
+    total = np.sum(steps, 0)
+    c = Cache(B, gen, dtype, hq, hkv, dim, [int(n) for n in total], 16)
+    rot = B.make_kv_rotation(B.flame_kv_rotation_frequencies(dim))
+    q, k, v = ([rand(gen, dtype, int(n), h, dim) for n in total] for h in (hq, hkv, hkv))
+    got = [[] for _ in total]
+    turned_q = [[] for _ in total]
+    done = np.zeros(3, int)
+    for new in steps:
+        done = done + new
+        rows_q = torch.cat([q[b][done[b] - new[b]:done[b]] for b in range(3)])
+        rows_k = torch.cat([k[b][done[b] - new[b]:done[b]] for b in range(3)])
+        rows_v = torch.cat([v[b][done[b] - new[b]:done[b]] for b in range(3)])
+        off, lens, now_q, out = ints(offsets(new)), ints(done), torch.empty_like(rows_q), torch.empty_like(rows_q)
+        B.flame_kv_append(c.cfg, c.packed, rows_k, rows_v, off, lens, q=rows_q, q_out=now_q, rotation=rot)
+        if new == [1, 1, 1]:
+            B.flame_kv_decode(c.cfg, c.packed, now_q, lens, out, workspace_for(B, c.cfg, 3))
+        else:
+            B.flame_kv_extend(c.cfg, c.packed, now_q, off, lens, out, workspace_for(B, c.cfg, 3, len(now_q)))
+        at = 0
+        for b, m in enumerate(new):
+            got[b].append(out[at:at + m])
+            turned_q[b].append(now_q[at:at + m])
+            at += m
+    for b, n in enumerate(total):
+        keys, values = c.rows(b, int(n))
+        assert np.array_equal(values, host(v[b]))
+        check_attention(host(torch.cat(got[b])), host(torch.cat(turned_q[b])), keys, values, dtype, what=b)
+    # and the prompt operator on the same rows, in no cache
+    rows = [torch.cat(x) for x in turned_q]
+    keys = [torch.from_numpy(c.rows(b, int(n))[0]).to(DEV).to(torch_type(dtype)) for b, n in enumerate(total)]
+    out = torch.empty_like(torch.cat(rows))
+    B.flame_kv_prompt(c.cfg, torch.cat(rows), torch.cat(keys), torch.cat(v), ints(offsets(total)), out)
+    off = offsets(total)
+    for b, n in enumerate(total):
+        s = slice(off[b], off[b + 1])
+        check_attention(host(out[s]), host(rows[b]), host(keys[b]), host(v[b]), dtype, what=("prompt", b))
+
+
+def test_graphs_follow_the_device_arrays(B):
+    """A decoding step (append, attend) captured once and replayed while the lengths grow; two graphs share a workspace; eager work in between."""
+    import torch
+    gen, lens0, steps = generator(9), [5, 130, 0, 1000], 6
+    c = Cache(B, gen, "bf16", 8, 2, 64, lens0, 16, room=steps)
+    twin = Cache(B, generator(9), "bf16", 8, 2, 64, lens0, 16, room=steps)
+    rot = B.make_kv_rotation(B.flame_kv_rotation_frequencies(64))
+    lens, off = ints(lens0), ints([0, 1, 2, 3, 4])
+    q, k, v = (torch.zeros(4, h, 64, device=DEV, dtype=torch.bfloat16) for h in (8, 2, 2))
+    out, turned, ext = torch.empty_like(q), torch.empty_like(q), torch.empty_like(q)
+    ws = workspace_for(B, c.cfg, 4, 4)
+    ws = torch.full((max(ws.numel(), B.flame_kv_workspace_bytes(c.cfg, 4)),), 0xff, dtype=torch.uint8, device=DEV)
+    side = torch.cuda.Stream()
+    graphs = []
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for op in ("decode", "extend"):
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g, stream=side):
+                if op == "decode":
+                    B.flame_kv_append(c.cfg, c.packed, k, v, off, lens, q=q, q_out=turned, rotation=rot)
+                    B.flame_kv_decode(c.cfg, c.packed, turned, lens, out, ws)
+                else:
+                    B.flame_kv_extend(c.cfg, c.packed, turned, off, lens, ext, ws)
+            graphs.append(g)
+    torch.cuda.synchronize()
+    for step in range(steps):
+        lens.copy_(ints([n + step + 1 for n in lens0]))
+        for x in (q, k, v):
+            x.copy_(torch.randn(x.shape, generator=gen, device=DEV))
+        for g in graphs:
+            g.replay()
+        torch.cuda.synchronize()
+        # eager, on a cache of its own
+        out2, turned2, ext2 = torch.empty_like(q), torch.empty_like(q), torch.empty_like(q)
+        ws2 = torch.full_like(ws, 0xff)
+        B.flame_kv_append(twin.cfg, twin.packed, k, v, off, lens, q=q, q_out=turned2, rotation=rot)
+        B.flame_kv_decode(twin.cfg, twin.packed, turned2, lens, out2, ws2)
+        B.flame_kv_extend(twin.cfg, twin.packed, turned2, off, lens, ext2, ws2)
+        torch.cuda.synchronize()
+        assert torch.equal(out, out2) and torch.equal(turned, turned2) and torch.equal(ext, ext2) and torch.equal(c.k, twin.k), step
+        for b in range(4):
+            check_attention(host(out[b:b + 1]), host(turned[b:b + 1]), *c.rows(b, lens0[b] + step + 1), "bf16", what=(step, b))
+
+
+def test_other_streams_and_a_padded_batch(B):
+    """Work on a stream of its own; sequences of a padded batch that have no rows (length 0, offsets that stand still) and offsets that end before the rows do."""
+    import torch
+    gen, lens = generator(10), [300, 0, 45, 0]
+    c = Cache(B, gen, "f16", 4, 2, 64, lens, 32)
+    q = rand(gen, "f16", 12, 4, 64)
+    off = ints([0, 3, 3, 5, 5])
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        out = torch.full_like(q, 7.0)
+        ws = workspace_for(B, c.cfg, 4, 12)
+    lens_dev = ints(lens)
+    torch.cuda.synchronize()
+    B.flame_kv_extend(c.cfg, c.packed, q, off, lens_dev, out, ws, stream=side)
+    side.synchronize()
+    assert bool((out[5:] == 7.0).all())
+    check_attention(host(out[:3]), host(q[:3]), *c.rows(0, 300), "f16")
+    check_attention(host(out[3:5]), host(q[3:5]), *c.rows(2, 45), "f16")
+
+
+def test_the_same_call_gives_the_same_bits(B):
+    """The same call twice gives the same bits, at sizes where the work is split and joined."""
+    import torch
+    gen, lens = generator(11), [5000, 17, 3000]
+    c = Cache(B, gen, "bf16", 16, 2, 128, lens, 16)
+    q = rand(gen, "bf16", 3, 16, 128)
+    outs = []
+    for _ in range(3):
+        out = torch.empty_like(q)
+        B.flame_kv_decode(c.cfg, c.packed, q, ints(lens), out, workspace_for(B, c.cfg, 3))
+        outs.append(out)
+    assert torch.equal(outs[0], outs[1]) and torch.equal(outs[0], outs[2])
+    for b, n in enumerate(lens):
+        check_attention(host(outs[0][b:b + 1]), host(q[b:b + 1]), *c.rows(b, n), "bf16", what=b)
+
+
+def test_refusals_on_the_device(B):
+    import torch
+    cfg = B.make_kv_config("bf16", 8, 2, 64)
+    pool = torch.zeros(4, 16, 2, 64, device=DEV, dtype=torch.bfloat16)
+    q, kv, i = torch.zeros(3, 8, 64, device=DEV, dtype=torch.bfloat16), torch.zeros(3, 2, 64, device=DEV, dtype=torch.bfloat16), ints([0, 1, 2, 3])
+    table = ints(np.zeros((3, 2)))
+    cache = B.pack_kv_cache(cfg, pool, pool.clone(), table)
+    lens = ints([1, 1, 1])
+    wide = torch.zeros(3, 8, 68, device=DEV, dtype=torch.bfloat16)[..., :64]
+    for bad, kind in ((lambda: B.flame_kv_append(cfg, cache, kv.cpu(), kv, i, lens), ValueError), (lambda: B.flame_kv_append(cfg, cache, kv, kv, i.cpu(), lens), ValueError),
+                      (lambda: B.flame_kv_append(cfg, cache, kv, kv, i[:3], lens), ValueError), (lambda: B.flame_kv_prompt(cfg, q, kv, kv, i, q[:1].expand(3, 8, 64)), ValueError),
+                      (lambda: B.flame_kv_prompt(cfg, wide, kv, kv, i, q), B.FlameGRError), (lambda: B.flame_kv_decode(B.make_kv_config("f16", 8, 2, 64), cache, q.half(), lens, q.half()), ValueError),
+                      (lambda: B.flame_kv_decode(cfg, cache, torch.zeros(4, 8, 64, device=DEV, dtype=torch.bfloat16), ints([1] * 4), torch.zeros(4, 8, 64, device=DEV, dtype=torch.bfloat16)), ValueError),
+                      (lambda: B.pack_kv_cache(cfg, pool, pool.transpose(1, 2).contiguous().transpose(1, 2), table), ValueError),
+                      (lambda: B.pack_kv_cache(cfg, pool[:1].expand(4, 16, 2, 64), pool[:1].expand(4, 16, 2, 64), table), ValueError),
+                      (lambda: B.flame_kv_decode(cfg, cache, q, lens, torch.empty_like(q), torch.zeros(8, device="cpu")), ValueError)):
+        with pytest.raises(kind):
+            bad()
+    # heads and rows of one: whatever stride torch gives such a dimension is not looked at
+    one = B.make_kv_config("bf16", 1, 1, 64)
+    x = torch.as_strided(rand(generator(1), "bf16", 400), (5, 1, 64), (64, 3, 1))
+    out = torch.empty(5, 1, 64, device=DEV, dtype=torch.bfloat16)
+    B.flame_kv_prompt(one, x, x, x, ints([0, 5]), out)
+    check_attention(host(out), host(x), host(x), host(x), "bf16")

@@ -1,0 +1,196 @@
+"""The operators on a paged key/value cache without a GPU: exported symbols, where tokens lie in pages (bad page-table entries among them), refusals of the C entries and of the
+binding, the frequencies of the rotation, and the oracle of attention against a brute force."""
+import ctypes as C
+import os
+import re
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+from oracle import kv_oracle
+from paper_2509_22681_amd import binding as B
+from paper_2509_22681_amd import build as build_mod
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+INDEX = r"""
+#include "kv_index.h"
+#include <cstdio>
+#include <cstdlib>
+#include <initializer_list>
+using namespace flame;
+static void die(const char *what, long a, long b) { std::printf("%s %ld %ld\n", what, a, b); std::exit(1); }
+int main() {
+  KvPages p{};
+  for (int32_t d = 1; d <= 65536; d += d < 300 ? 1 : 97) {
+    kv_set_page_size(&p, d);
+    const uint32_t top = 0x7fffffffu;
+    for (uint32_t q = 0; q < 40; ++q)                      // both sides of a multiple, near 0 and near 2^31
+      for (uint32_t base : {q * (uint32_t)d, (top / d - q % (top / d)) * (uint32_t)d})
+        for (int e = -1; e <= 1; ++e) {
+          const int64_t n = (int64_t)base + e;
+          if (n < 0 || n > top) continue;
+          if (kv_page_index(p, (uint32_t)n) != n / d) die("division", d, n);
+        }
+    uint32_t x = 12345u + d;
+    for (int i = 0; i < 200; ++i) {
+      x = x * 1664525u + 1013904223u;
+      if (kv_page_index(p, x >> 1) != (x >> 1) / (uint32_t)d) die("division", d, x >> 1);
+    }
+  }
+  kv_set_page_size(&p, 24);
+  p.n_pages = 5; p.page = (int64_t)3 << 32; p.slot = 1000;
+  const int32_t table[7] = {4, 0, -1, 5, 2, INT32_MIN, INT32_MAX};
+  for (int t = 0; t < 7 * 24; ++t) {
+    const int32_t page = table[t / 24];
+    const int64_t want = page >= 0 && page < 5 ? page * ((int64_t)3 << 32) + t % 24 * 1000 : -1;
+    if (kv_token_offset(p, table, t) != want) die("offset", t, (long)want);
+  }
+  for (int32_t n : {INT32_MIN, -1, 0, 1, 99, 100, 101, INT32_MAX})
+    if (kv_clip(n, 100) != (n < 0 ? 0 : n > 100 ? 100 : n)) die("clip", n, 0);
+  return 0;
+}
+"""
+
+
+def test_tokens_lie_where_the_table_says(tmp_path):
+    src = tmp_path / "index.cpp"
+    src.write_text(INDEX)
+    exe = str(tmp_path / "index")
+    subprocess.run(["g++", "-std=c++17", "-O1", "-fsanitize=undefined", "-fno-sanitize-recover=all", "-I", build_mod.CSRC, str(src), "-o", exe], check=True)
+    done = subprocess.run([exe], capture_output=True, text=True)
+    assert done.returncode == 0, done.stdout + done.stderr
+
+
+def test_library_exports_the_header():
+    with open(os.path.join(ROOT, "include", "flame_kv.h")) as f:
+        declared = set(re.findall(r"^(?:int|const char \*)\s*(flame_kv_[a-z_]+)\(", f.read(), re.M))
+    assert declared == set(B.KV_EXPORTS)
+    for name in declared:
+        assert hasattr(B._lib, name), name
+
+
+# Arguments that pass every check, with addresses that nothing reads: a refused call enqueues nothing, and only refused calls are made here.
+A = 1 << 20
+
+
+def args(**change):
+    d = dict(dtype=1, hq=8, hkv=2, dim=64, scale=0.0, row_stride=512, head_stride=64, data=A, n_seqs=3, n_tokens=10, n_keys=10, pool=A, slot_stride=128, page_stride=2048, n_pages=4,
+             page_size=16, table=A, pages_per_seq=8, offsets=A, kv_lens=A, workspace=A, bytes=1 << 62, rot_dim=64, frequencies=np.ones(64), q=True)
+    d.update(change)
+    return d
+
+
+def call(op, **change):
+    d = args(**change)
+    cfg = None if d.get("cfg", 1) is None else C.byref(B.flame_kv_config(d["dtype"], d["hq"], d["hkv"], d["dim"], d["scale"]))
+    rows = C.byref(B.flame_kv_rows(d["data"], d["row_stride"], d["head_stride"])) if d.get("rows", 1) else None
+    cache = C.byref(B.flame_kv_cache(d["pool"], d["pool"], d["page_stride"], d["slot_stride"], 64, d["n_pages"], d["page_size"], d["table"], 8, d["pages_per_seq"])) if d.get("cache", 1) else None
+    f = d["frequencies"]
+    rot = C.byref(B.flame_kv_rotation(d["rot_dim"], 0, None if f is None else f.ctypes.data_as(C.POINTER(C.c_double))))
+    if op == "append":
+        return B._lib.flame_kv_append(cfg, cache, rows, rows, rows, rows if d["q"] else None, rot, d["offsets"], d["kv_lens"], d["n_seqs"], d["n_tokens"], None, None)
+    if op == "prompt":
+        return B._lib.flame_kv_prompt(cfg, rows, rows, rows, d["offsets"], None, d["n_seqs"], d["n_tokens"], d["n_keys"], rows, None, None)
+    if op == "extend":
+        return B._lib.flame_kv_extend(cfg, cache, rows, d["offsets"], d["kv_lens"], d["n_seqs"], d["n_tokens"], rows, d["workspace"], d["bytes"], None, None)
+    return B._lib.flame_kv_decode(cfg, cache, rows, d["kv_lens"], d["n_seqs"], rows, d["workspace"], d["bytes"], None, None)
+
+
+OPS = ("append", "prompt", "extend", "decode")
+INVALID, UNSUPPORTED = -1, -5
+REFUSED = [(OPS, dict(cfg=None), INVALID), (OPS, dict(dtype=3), INVALID), (OPS, dict(dtype=-1), INVALID), (OPS, dict(hq=7), INVALID), (OPS, dict(hq=0), INVALID), (OPS, dict(hkv=0), INVALID),
+           (OPS, dict(dim=48), UNSUPPORTED), (OPS, dict(dim=256), UNSUPPORTED), (OPS, dict(hq=8192), UNSUPPORTED), (OPS, dict(scale=-1.0), INVALID),
+           (OPS, dict(scale=float("nan")), INVALID), (OPS, dict(scale=float("inf")), INVALID), (OPS, dict(n_seqs=-1), INVALID), (OPS, dict(rows=0), INVALID), (OPS, dict(data=None), INVALID),
+           (OPS, dict(data=A + 8), INVALID), (OPS, dict(row_stride=516), INVALID), (OPS, dict(head_stride=68), INVALID), (OPS[:3], dict(n_tokens=-1), INVALID),
+           (OPS[:3], dict(n_tokens=1 << 23), INVALID), (OPS[:3], dict(offsets=None), INVALID), (("append", "extend", "decode"), dict(kv_lens=None), INVALID),
+           (("append", "extend", "decode"), dict(cache=0), INVALID), (("append", "extend", "decode"), dict(pool=None), INVALID), (("append", "extend", "decode"), dict(pool=A + 2), INVALID),
+           (("append", "extend", "decode"), dict(slot_stride=4), INVALID), (("append", "extend", "decode"), dict(n_pages=0), INVALID), (("append", "extend", "decode"), dict(page_size=0), INVALID),
+           (("append", "extend", "decode"), dict(page_size=65537), INVALID), (("append", "extend", "decode"), dict(pages_per_seq=0), INVALID),
+           (("append", "extend", "decode"), dict(pages_per_seq=1 << 28), INVALID), (("append", "extend", "decode"), dict(table=None), INVALID), (("prompt",), dict(n_keys=-1), INVALID),
+           (("append",), dict(rot_dim=8), INVALID), (("append",), dict(rot_dim=80), INVALID), (("append",), dict(rot_dim=-16), INVALID), (("append",), dict(frequencies=None), INVALID),
+           (("append",), dict(frequencies=np.full(64, np.inf)), INVALID), (("append",), dict(q=False), INVALID)]
+
+
+@pytest.mark.parametrize("ops,change,code", REFUSED)
+def test_refusals_of_the_c_entries(ops, change, code):
+    for op in ops:
+        assert call(op, **change) == code, (op, change)
+        assert B._lib.flame_kv_last_error(), (op, change)
+
+
+def test_a_workspace_that_is_too_small_is_refused():
+    # (where a call of this shape needs one)
+    for op, n in (("extend", 10), ("decode", 3)):
+        need = B.flame_kv_workspace_bytes(B.make_kv_config("bf16", 8, 2, 64), 3, n)
+        assert need >= 0
+        if need > 0:
+            assert call(op, bytes=need - 1) == -2
+            assert call(op, workspace=None) == INVALID
+            assert call(op, workspace=A + 4) == INVALID
+        assert call(op, bytes=-1) == -2
+
+
+def test_empty_calls_enqueue_nothing():
+    for op in OPS:
+        assert call(op, n_seqs=0, rows=0, cache=0) == 0, op
+    for op in OPS[:3]:
+        assert call(op, n_tokens=0, rows=0, cache=0) == 0, op
+
+
+def test_workspace_refusals():
+    cfg = B.make_kv_config("bf16", 8, 2, 64)
+    for bad in (lambda: B.flame_kv_workspace_bytes(B.make_kv_config("bf16", 8, 3, 64), 1), lambda: B.flame_kv_workspace_bytes(cfg, -1), lambda: B.flame_kv_workspace_bytes(cfg, 1, -1)):
+        with pytest.raises(B.FlameGRError) as e:
+            bad()
+        assert e.value.code == INVALID
+    assert B.flame_kv_workspace_bytes(cfg, 0) >= 0
+
+
+def test_frequencies():
+    for r, base in ((2, 10.0), (64, 10000.0), (128, 1e6)):
+        want = np.array([float(base) ** (-2.0 * j / r) for j in range(r // 2)])
+        assert np.allclose(B.flame_kv_rotation_frequencies(r, base), want, rtol=1e-14, atol=0)
+    for r, base in ((0, 10.0), (3, 10.0), (64, 0.0), (64, float("inf")), (64, -2.0)):
+        with pytest.raises(B.FlameGRError):
+            B.flame_kv_rotation_frequencies(r, base)
+
+
+def test_refusals_of_the_binding():
+    cfg = B.make_kv_config("bf16", 8, 2, 64)
+    q, kv, i = torch.zeros(5, 8, 64, dtype=torch.bfloat16), torch.zeros(5, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
+    pool, table = torch.zeros(4, 16, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32)
+    for bad in (lambda: B._kv_rows(cfg, q[:, :7], 8, "q"), lambda: B._kv_rows(cfg, q.float(), 8, "q"), lambda: B._kv_rows(cfg, q[..., :32], 8, "q"),
+                lambda: B._kv_rows(cfg, q[0], 8, "q"), lambda: B._kv_ints(i.long(), 3, "i"), lambda: B._kv_ints(i, 4, "i"), lambda: B._kv_ints(i[None], 1, "i"),
+                lambda: B._kv_ints(torch.zeros(6, dtype=torch.int32)[::2], 3, "i"), lambda: B.pack_kv_cache(cfg, pool[..., :32], pool[..., :32], table),
+                lambda: B.pack_kv_cache(cfg, pool, pool.float(), table), lambda: B.pack_kv_cache(cfg, pool, pool[:3], table), lambda: B.pack_kv_cache(cfg, pool, pool, table.long()),
+                lambda: B.pack_kv_cache(cfg, pool, pool, table[0]), lambda: B.pack_kv_cache(cfg, pool, pool, table),      # (the last: host memory)
+                lambda: B.flame_kv_append(cfg, None, kv, kv[:4], i, i), lambda: B.flame_kv_append(cfg, None, kv, kv, i, i, q=q), lambda: B.flame_kv_append(cfg, None, kv, kv, i, i, q_out=q),
+                lambda: B.flame_kv_prompt(cfg, q, kv, kv[:4], i, q), lambda: B.flame_kv_prompt(cfg, q, kv, kv, i, q[:4]), lambda: B.flame_kv_extend(cfg, None, q, i, i, q[:4]),
+                lambda: B.flame_kv_decode(cfg, None, q, i, q), lambda: B._kv_torch_dtype(B.make_kv_config(7, 8, 2, 64))):
+        with pytest.raises(ValueError):
+            bad()
+
+
+def test_oracle_of_attention_against_a_brute_force():
+    rng = np.random.default_rng(0)
+    for m, n, hq, hkv, dim in ((3, 7, 4, 2, 8), (5, 3, 2, 1, 4), (1, 0, 2, 2, 4), (4, 4, 3, 3, 6)):
+        q, k, v = rng.standard_normal((m, hq, dim)), rng.standard_normal((n, hkv, dim)), rng.standard_normal((n, hkv, dim))
+        got = kv_oracle.attend(q, k, v, 0.7)[0]
+        for i in range(m):
+            for h in range(hq):
+                top = [np.exp(0.7 * sum(q[i, h, j] * k[c, h * hkv // hq, j] for j in range(dim))) for c in range(n) if c <= n - m + i]
+                for j in range(dim):
+                    want = sum(w * v[c, h * hkv // hq, j] for c, w in enumerate(top)) / sum(top) if top else 0.0
+                    assert abs(got[i, h, j] - want) < 1e-12
+    x, p, f = rng.standard_normal((4, 2, 10)), np.array([0, 1, 7, 100]), np.array([1.0, 0.25, 0.03])
+    for inter in (False, True):
+        y = kv_oracle.rotate(x, p, f, inter)
+        assert np.array_equal(y[..., 6:], x[..., 6:])
+        for t in range(4):
+            for j in range(3):
+                a, b = (2 * j, 2 * j + 1) if inter else (j, j + 3)
+                z = (x[t, :, a] + 1j * x[t, :, b]) * np.exp(1j * p[t] * f[j])
+                assert np.allclose(y[t, :, a], z.real) and np.allclose(y[t, :, b], z.imag)
