@@ -41,7 +41,9 @@ struct KvAttention {
 
 hipError_t launch_kv_append(const KvBatch &batch, const KvPages &pages, const KvRows &k, const KvRows &v, const KvRows *q, const KvRows *q_out,
                             const KvRotation &rotation, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, hipStream_t stream);
-hipError_t launch_kv_attention(const KvAttention &a, void *workspace, hipStream_t stream);
-int64_t kv_workspace_bytes(int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, int32_t n_seqs, int64_t n_tokens);
+hipError_t launch_kv_attention(const KvAttention &a, hipStream_t stream);
+// few query rows: split over the keys (kv_split.hip)
+hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream);
+int64_t kv_split_workspace_bytes(int32_t head_dim);
 
 }  // namespace flame

@@ -89,6 +89,10 @@ void take_heads(const flame_kv_config *c, KvAttention *a) {
   a->scale = c->scale == 0.f ? 1.f / std::sqrt((float)c->head_dim) : c->scale;
 }
 
+// Calls of a few rows per sequence split the keys over the chip.
+bool splits(const flame_kv_config *c, int32_t n_seqs, int64_t n_rows) { return n_rows * (c->n_q_heads / c->n_kv_heads) <= (int64_t)64 * n_seqs; }
+int64_t workspace_bytes_for(const flame_kv_config *c, int32_t n_seqs, int64_t n_rows) { return splits(c, n_seqs, n_rows) ? kv_split_workspace_bytes(c->head_dim) : 0; }
+
 int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_rows,
                  const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream) {
   KvAttention a{};
@@ -96,12 +100,12 @@ int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const 
   if (int rc = take_rows(cfg, out, &a.out)) return rc;
   if (int rc = take_pages(cfg, cache, &a.pages)) return rc;
   if (!kv_lens) return bad("kv_lens is NULL");
-  const int64_t need = kv_workspace_bytes(cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim, cfg->dtype, n_seqs, n_rows);
+  const int64_t need = workspace_bytes_for(cfg, n_seqs, n_rows);
   if (need > 0 && (!workspace || !aligned(workspace))) return bad("the workspace is NULL or not 16-byte aligned");
   if (workspace_bytes < need) return bad("the workspace is smaller than flame_kv_workspace_bytes", FLAME_GR_CAPACITY_EXCEEDED);
   a.batch = KvBatch{offsets, kv_lens, n_seqs, n_rows, faults};
   take_heads(cfg, &a);
-  return done(launch_kv_attention(a, workspace, (hipStream_t)stream));
+  return done(need > 0 ? launch_kv_split(a, workspace, (hipStream_t)stream) : launch_kv_attention(a, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -123,7 +127,7 @@ int flame_kv_workspace_bytes(const flame_kv_config *cfg, int32_t n_seqs, int64_t
   if (int rc = check_config(cfg)) return rc;
   if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
   if (!bytes) return bad("bytes is NULL");
-  *bytes = kv_workspace_bytes(cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim, cfg->dtype, n_seqs, n_tokens);
+  *bytes = workspace_bytes_for(cfg, n_seqs, n_tokens);
   return FLAME_GR_OK;
 }
 
@@ -169,7 +173,7 @@ int flame_kv_prompt(const flame_kv_config *cfg, const flame_kv_rows *q, const fl
   a.k_offsets = k_offsets;
   a.n_keys = n_keys;
   take_heads(cfg, &a);
-  return done(launch_kv_attention(a, nullptr, (hipStream_t)stream));
+  return done(launch_kv_attention(a, (hipStream_t)stream));
 }
 
 int flame_kv_extend(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *q_offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_tokens,

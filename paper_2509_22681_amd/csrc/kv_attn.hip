@@ -71,7 +71,7 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvAttention a) {
     for (int i = 0; i < N; ++i) s += has ? q[i] * (float)((const T *)kp)[f + i] : 0.f;
     s = wave_sum(s) * scale;
     const float m_new = fmaxf(m, s);
-    const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_new), w = __builtin_amdgcn_exp2f(s - m_new);
+    const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_new), w = s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s - m_new);
     l = l * keep + w;
     m = m_new;
 #pragma unroll
@@ -84,9 +84,7 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvAttention a) {
 
 }  // namespace
 
-int64_t kv_workspace_bytes(int32_t, int32_t, int32_t, int32_t, int32_t, int64_t) { return 0; }
-
-hipError_t launch_kv_attention(const KvAttention &a, void *, hipStream_t stream) {
+hipError_t launch_kv_attention(const KvAttention &a, hipStream_t stream) {
   const unsigned blocks = (unsigned)((a.batch.n_rows * a.n_q_heads + 3) / 4);
   kv_with_type(a.dtype, [&](auto t) {
     using T = decltype(t);

@@ -1,5 +1,7 @@
 // Device helpers of the operators on a paged key/value cache: whose row is this, how long is its sequence, where does a token lie.
 #pragma once
+#include <type_traits>
+
 #include "device_common.h"
 #include "kv.h"
 
@@ -38,6 +40,12 @@ template <typename F> inline void kv_with_type(int32_t dtype, F f) {
   if (dtype == FLAME_KV_F32) f(0.f);
   else if (dtype == FLAME_KV_BF16) f((bf16_t)0.f);
   else f((half_t)0.f);
+}
+
+template <typename F> inline void kv_with_width(int32_t head_dim, F f) {
+  if (head_dim == 32) f(std::integral_constant<int, 32>{});
+  else if (head_dim == 64) f(std::integral_constant<int, 64>{});
+  else f(std::integral_constant<int, 128>{});
 }
 
 // One rounding of an fp32 result, to nearest; an fp16 one past the largest finite value becomes infinite, as in IEEE arithmetic.

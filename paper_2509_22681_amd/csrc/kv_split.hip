@@ -1,0 +1,482 @@
+// Softmax attention of few query rows over long paged caches: the work is split over the keys and joined.
+//
+// Bound by memory: a sequence's keys and values are read once, 2 n Hkv D values, and each takes part in 4 G operations per query token
+// (G query heads share a key head), far below what the matrix pipe does in that time.  So everything serves the loads:
+//   - A unit is a block of 16 query rows of one sequence and key head (row = token * G + head of the group; a decoding step
+//     with G <= 16 has one unit per key head, whose keys and values are then read once), and a tile 32 of its keys (16 in fp32).  The tiles of all units form one
+//     line, which kWorkers wavefronts cut into equal parts: every wavefront streams the same number of bytes whatever the lengths of the sequences, one long sequence fills the chip,
+//     and nothing depends on the host knowing the lengths.  A wavefront works alone: no barriers, no LDS traffic but for the
+//     row offsets.
+//   - Keys and values go from memory straight into the registers of the matrix operands, one tile ahead of the arithmetic (16 KB
+//     in flight per wavefront at D = 128).  Products are transposed, S^T[key][row] = K Q^T and O^T[feature][row] += V^T P^T.  With the keys of two 16-row blocks dealt out as
+//     8 (m / 4) + m % 4 and 4 more, the weights that a lane gets from the first product are those of keys 8 g..8 g + 7 (g = lane / 16), which is
+//     what the second product wants from it; and a lane that reads D/16 features of these eight keys holds the A operand of the second product up to a
+//     transposition within its own registers (byte permutes of word pairs), feature D/16 * m + j in product j.
+// A unit that ends within its wavefront is written; the others leave maximum, sum and unnormalised rows in the workspace, for a second kernel that
+// adds up a unit's parts in the order of their keys.  Every part and every join has a fixed order: the same call gives the same bits.
+#include "kv_device.h"
+
+namespace flame {
+
+namespace {
+
+constexpr int kWorkers = 2048;      // wavefronts: two per SIMD, as their registers allow
+constexpr int kRows = 16;           // query rows of a unit
+
+template <typename T, int DH> struct SplitShape {
+  static constexpr bool F32 = sizeof(T) == 4;
+  static constexpr int KT = F32 ? 16 : 32;          // keys of a tile
+  static constexpr int VF = DH / 16;                // features of a lane in the second product
+};
+
+// What a wavefront knows of a sequence.
+struct SplitSeq {
+  int64_t first;      // its first query row
+  int rows, blocks;   // query rows times G, and units per key head
+  int n, back;        // keys; keys that the row before the first one would see
+  int tiles;          // of one unit
+};
+
+template <int KT> __device__ __forceinline__ SplitSeq split_sequence(const KvAttention &a, int b, bool report) {
+  SplitSeq s;
+  s.n = kv_clip_length(a.batch.kv_lens[b], a.pages.capacity, a.batch.faults, report);
+  int64_t m = 1, full = 1;
+  s.first = b;
+  if (a.batch.offsets) {
+    const int64_t first = a.batch.offsets[b], end = a.batch.offsets[b + 1];
+    s.first = first;
+    full = end - first;
+    const bool wrong = first < 0 || full < 0 || end > a.batch.n_rows;
+    if (wrong && report) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
+    m = first < 0 || full < 0 ? 0 : max((int64_t)0, min(full, a.batch.n_rows - first));
+  }
+  const int group = a.n_q_heads / a.n_kv_heads;
+  s.back = (int)max(s.n - full, -((int64_t)1 << 30));
+  s.rows = (int)(m * group);                        // (rows times heads is below 2^25)
+  s.blocks = (s.rows + kRows - 1) / kRows;
+  s.tiles = s.rows ? max(1, (s.n + KT - 1) / KT) : 0;   // (a unit without keys writes zeros)
+  return s;
+}
+
+__device__ __forceinline__ int64_t split_scan(int64_t v) {        // inclusive sums over the wavefront
+  const auto step = [&](auto moved) { v += moved; };
+  const auto dpp = [&](auto ctrl, auto mask) {
+    const int lo = __builtin_amdgcn_update_dpp(0, (int)v, decltype(ctrl)::value, decltype(mask)::value, 0xf, false);
+    const int hi = __builtin_amdgcn_update_dpp(0, (int)(v >> 32), decltype(ctrl)::value, decltype(mask)::value, 0xf, false);
+    return (int64_t)(((uint64_t)(uint32_t)hi << 32) | (uint32_t)lo);
+  };
+  step(dpp(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{}));   // row_shr:1
+  step(dpp(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{}));
+  step(dpp(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{}));
+  step(dpp(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{}));
+  step(dpp(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{}));   // the last lane of a row to the next row
+  step(dpp(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{}));   // lane 31 to the upper half
+  return v;
+}
+
+__device__ __forceinline__ int64_t split_lane(int64_t v, int lane) {
+  return (int64_t)(((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32) | (uint32_t)__builtin_amdgcn_readlane((int)v, lane));
+}
+
+// Tiles of all units, and of those the sequence that holds tile `at` (at < 0: not asked) with its first tile.  at >= total: sequence n_seqs.
+struct SplitPlace {
+  int64_t total, first_tile;
+  int seq;
+};
+
+template <int KT, typename F> __device__ __forceinline__ SplitPlace split_find(const KvAttention &a, int lane, F target) {
+  SplitPlace p{0, 0, a.batch.n_seqs};
+  int lo = 0, n = a.batch.n_seqs;
+  int64_t base = 0, at = 0;
+  for (bool top = true;; top = false) {
+    const int chunk = (n + 63) / 64;
+    int64_t mine = 0;
+    for (int i = 0; i < chunk; ++i) {
+      const int k = lane * chunk + i;
+      if (k >= n) break;
+      const SplitSeq s = split_sequence<KT>(a, lo + k, top && blockIdx.x == 0 && threadIdx.x < 64);
+      mine += (int64_t)s.blocks * s.tiles;
+    }
+    mine *= a.n_kv_heads;
+    const int64_t sums = split_scan(mine);
+    if (top) {
+      p.total = split_lane(sums, 63);
+      at = target(p.total);
+      if (at >= p.total) return p;
+    }
+    const uint64_t beyond = __builtin_amdgcn_ballot_w64(base + sums > at);
+    if (!beyond) return p;                            // (only if the lengths changed under the call)
+    const int l = __builtin_ctzll(beyond);
+    base += split_lane(sums, l) - split_lane(mine, l);
+    lo += l * chunk;
+    n = min(chunk, n - l * chunk);
+    if (n <= 1) {
+      p.seq = lo;
+      p.first_tile = base;
+      return p;
+    }
+  }
+}
+
+// Parts of a worker: the one it begins with, and one that goes on behind its end.
+template <int DH> __host__ __device__ constexpr int split_part_floats() { return kRows * DH + 2 * kRows; }
+
+__device__ __forceinline__ float split_max(float v) {             // over the four lanes that share a query row
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return pair_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float split_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return pair_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+template <typename T> struct Matrix16;
+template <> struct Matrix16<bf16_t> {
+  typedef bf16x8 frag;
+  static __device__ __forceinline__ f32x4 mul(frag x, frag y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
+  static constexpr uint32_t kExponent = 0x7f80, kFraction = 0x007f, kOne = 0x3f80;
+};
+template <> struct Matrix16<half_t> {
+  typedef f16x8 frag;
+  static __device__ __forceinline__ f32x4 mul(frag x, frag y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0); }
+  static constexpr uint32_t kExponent = 0x7c00, kFraction = 0x03ff, kOne = 0x3c00;
+};
+
+template <typename T, int DH>
+__global__ __launch_bounds__(256, 2) void kv_split_kernel(KvAttention a, float *__restrict__ parts) {
+  typedef SplitShape<T, DH> S;
+  constexpr int KT = S::KT, VF = S::VF;
+  constexpr bool F32 = S::F32;
+  constexpr int KB = KT / 16;                                     // 16-key blocks of a tile
+  constexpr int KS = DH * (int)sizeof(T) / 64;                    // 64-byte steps of a key row: 16 bytes per lane each
+  constexpr int VK = KT / 4;                                      // keys of a lane in the second product
+  constexpr int VB = VF * (int)sizeof(T);                         // bytes of a lane per value row: 4..32
+  constexpr int VW = VB / 4;
+  typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+  __shared__ int64_t offset_s[4][2][KT];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l16 = lane & 15, g = lane >> 4;
+  const int worker = blockIdx.x * 4 + wave;
+  int64_t per = 0;
+  SplitPlace place = split_find<KT>(a, lane, [&](int64_t total) {
+    per = (total + kWorkers - 1) / kWorkers;
+    return (int64_t)worker * per;
+  });
+  int64_t tile = (int64_t)worker * per;                           // on the line of all tiles
+  const int64_t tile_end = min(tile + per, place.total);
+  const float scale = a.scale * kLog2e;
+  const int group = a.n_q_heads / a.n_kv_heads;
+  int seq = place.seq;
+  int64_t seq_tile = place.first_tile;
+  bool begins = true;                                             // the unit is the worker's first
+  while (tile < tile_end && seq < a.batch.n_seqs) {
+    SplitSeq s = split_sequence<KT>(a, seq, false);
+    int64_t in_seq = tile - seq_tile;
+    const int64_t seq_tiles = (int64_t)a.n_kv_heads * s.blocks * s.tiles;
+    if (in_seq >= seq_tiles) {                                    // (sequences without rows have none)
+      seq_tile += seq_tiles;
+      ++seq;
+      continue;
+    }
+    const int unit = (int)(in_seq / s.tiles), t0 = (int)(in_seq - (int64_t)unit * s.tiles);
+    const int t1 = (int)min((int64_t)s.tiles, t0 + (tile_end - tile));
+    const int kvh = unit / s.blocks, block = unit - kvh * s.blocks;
+    const int32_t *table = a.pages.table + seq * a.pages.table_stride;
+    const char *kp = a.pages.k + kvh * a.pages.head, *vp = a.pages.v + kvh * a.pages.head;
+    // my query row (the column of the accumulators), and the keys it sees
+    const int row = block * kRows + l16;
+    const bool row_there = row < s.rows;
+    const int token = (row_there ? row : block * kRows) / group, head = kvh * group + (row_there ? row : block * kRows) - token * group;
+    const int sees = s.back + token + 1;
+    const int sees_least = s.back + block * kRows / group + 1;    // of the block's first row
+    word4 fq[KS];
+    {
+      const char *q = a.q.p + (s.first + token) * a.q.row + head * a.q.head;
+#pragma unroll
+      for (int i = 0; i < KS; ++i) fq[i] = *(const word4 *)(q + i * 64 + g * 16);
+    }
+    f32x4 o[VF];
+#pragma unroll
+    for (int j = 0; j < VF; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    float m = -INFINITY, l = 0.f;
+
+    // Row offsets of a tile: key k by lane k; keys behind the last one repeat it, keys in pages that the table does not name get the pool's first row, and neither counts.
+    auto look_up = [&](int t) -> int64_t {
+      const int key = min(t * KT + (lane & (KT - 1)), s.n - 1);
+      return key < 0 ? -1 : kv_token_offset(a.pages, table, (uint32_t)key);
+    };
+    struct Tile {
+      word4 k[KB][KS];
+      uint32_t v[VK][VW];
+      uint64_t there;                                             // lanes' keys that count
+    };
+    auto request = [&](Tile &x, int t, int64_t offset) {
+      if (offset < 0 && s.n > 0 && lane < KT) kv_fault(a.batch.faults, FLAME_KV_FAULT_PAGE);
+      x.there = __builtin_amdgcn_ballot_w64(offset >= 0 && t * KT + (lane & (KT - 1)) < s.n);
+      int64_t *at = offset_s[wave][t & 1];
+      if (lane < KT) at[lane] = max(offset, (int64_t)0);
+      __builtin_amdgcn_wave_barrier();
+#pragma unroll
+      for (int b = 0; b < KB; ++b) {
+        const char *row_at = kp + at[F32 ? l16 : 8 * (l16 >> 2) + 4 * b + (l16 & 3)];
+#pragma unroll
+        for (int i = 0; i < KS; ++i) x.k[b][i] = *(const word4 *)(row_at + i * 64 + g * 16);
+      }
+#pragma unroll
+      for (int i = 0; i < VK; ++i) {
+        const char *row_at = vp + at[VK * g + i];
+        if constexpr (VB == 32) {
+          // fp32, 128 features: lanes side by side take 16 bytes each of either half
+          const word4 x0 = *(const word4 *)(row_at + l16 * 16), x1 = *(const word4 *)(row_at + 256 + l16 * 16);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) { x.v[i][w] = x0[w]; x.v[i][4 + w] = x1[w]; }
+        } else {
+          struct alignas(VB) Words { uint32_t w[VW]; };
+          const Words y = *(const Words *)(row_at + l16 * VB);
+#pragma unroll
+          for (int w = 0; w < VW; ++w) x.v[i][w] = y.w[w];
+        }
+      }
+    };
+    auto add = [&](const Tile &x, int t) {
+      f32x4 z[KB];
+#pragma unroll
+      for (int b = 0; b < KB; ++b) z[b] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int i = 0; i < KS; ++i)
+#pragma unroll
+        for (int b = 0; b < KB; ++b) {
+          if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[b] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.k[b][i][j]), __uint_as_float(fq[i][j]), z[b], 0, 0, 0);
+          } else {
+            typedef typename Matrix16<T>::frag frag;
+            z[b] = Matrix16<T>::mul(__builtin_bit_cast(frag, x.k[b][i]), __builtin_bit_cast(frag, fq[i]), z[b]);
+          }
+        }
+      // element e of block b: key VK g + 4 b + e of the tile
+      const int k0 = t * KT + VK * g;
+      const uint32_t here = (uint32_t)(x.there >> (VK * g)) & ((1u << VK) - 1);
+      const bool masked = x.there != ~0ull || t * KT + KT > sees_least;
+      float w[VK];
+#pragma unroll
+      for (int i = 0; i < VK; ++i) w[i] = z[i >> 2][i & 3] * scale;
+      if (masked) {
+#pragma unroll
+        for (int i = 0; i < VK; ++i) w[i] = (here >> i & 1) && k0 + i < sees ? w[i] : -INFINITY;
+      }
+      float top = w[0];
+#pragma unroll
+      for (int i = 1; i < VK; ++i) top = fmaxf(top, w[i]);
+      const float m_new = fmaxf(m, split_max(top));
+      const float m_at = m_new == -INFINITY ? 0.f : m_new;       // (nothing seen yet: all weights are 2^-inf)
+      if (__builtin_amdgcn_ballot_w64(m_new != m)) {
+        const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_at);
+        l *= keep;
+#pragma unroll
+        for (int j = 0; j < VF; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) o[j][e] *= keep;
+        m = m_new;
+      }
+#pragma unroll
+      for (int i = 0; i < VK; ++i) {
+        w[i] = __builtin_amdgcn_exp2f(w[i] - m_at);
+        l += w[i];
+      }
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < VK; ++i) {
+          const bool counts = (here >> i & 1);
+          const bool seen = counts && k0 + i < sees;
+#pragma unroll
+          for (int j = 0; j < VF; ++j) {
+            const float v = counts ? __uint_as_float(x.v[i][j]) : 0.f;
+            if (masked && __builtin_amdgcn_ballot_w64(!(fabsf(v) <= 3.4e38f))) {
+              // an infinite or NaN value in a tile that some row does not see all of: rows that do not see it must not meet it in a product
+              const bool finite = fabsf(v) <= 3.4e38f;
+              o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(finite ? v : 0.f, w[i], o[j], 0, 0, 0);
+              const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+              const f32x4 up = __builtin_amdgcn_mfma_f32_16x16x4f32(finite || v == -INFINITY ? 0.f : 1.f, seen ? 1.f : 0.f, none, 0, 0, 0);
+              const f32x4 down = __builtin_amdgcn_mfma_f32_16x16x4f32(finite || v == INFINITY ? 0.f : 1.f, seen ? 1.f : 0.f, none, 0, 0, 0);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[j][e] += (up[e] > 0.f ? INFINITY : 0.f) + (down[e] > 0.f ? -INFINITY : 0.f);
+            } else {
+              o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, w[i], o[j], 0, 0, 0);
+            }
+          }
+        }
+      } else {
+        typedef Matrix16<T> M;
+        typedef typename M::frag frag;
+        frag p, ones;
+#pragma unroll
+        for (int i = 0; i < VK; ++i) {
+          p[i] = (T)w[i];
+          ones[i] = (T)((here >> i & 1) && k0 + i < sees ? 1.f : 0.f);
+        }
+#pragma unroll
+        for (int j = 0; j < VF; ++j) {
+          // feature VF l16 + j of keys VK g..VK g + 7: the lower or upper halves of word j / 2 of the eight rows
+          uint32_t f[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][j >> 1], x.v[2 * i][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+          if (masked) {
+            bool odd = false;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              f[i] &= ((here >> (2 * i) & 1) ? 0xffffu : 0u) | ((here >> (2 * i + 1) & 1) ? 0xffff0000u : 0u);
+              odd |= (f[i] & M::kExponent) == M::kExponent || (f[i] >> 16 & M::kExponent) == M::kExponent;
+            }
+            if (__builtin_amdgcn_ballot_w64(odd)) {
+              // an infinite or NaN value in a tile that some row does not see all of: rows that do not see it must not meet it in a product
+              uint32_t up[4], down[4];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) {
+                uint32_t keep = 0, u = 0, d = 0;
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                  const uint32_t v = f[i] >> (16 * h) & 0xffff;
+                  const bool finite = (v & M::kExponent) != M::kExponent, nan = !finite && (v & M::kFraction);
+                  keep |= finite ? v << (16 * h) : 0u;
+                  u |= !finite && (nan || !(v >> 15)) ? M::kOne << (16 * h) : 0u;
+                  d |= !finite && (nan || v >> 15) ? M::kOne << (16 * h) : 0u;
+                }
+                f[i] = keep; up[i] = u; down[i] = d;
+              }
+              const f32x4 none = {0.f, 0.f, 0.f, 0.f};
+              const f32x4 us = M::mul(__builtin_bit_cast(frag, word4{up[0], up[1], up[2], up[3]}), ones, none);
+              const f32x4 ds = M::mul(__builtin_bit_cast(frag, word4{down[0], down[1], down[2], down[3]}), ones, none);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[j][e] += (us[e] > 0.f ? INFINITY : 0.f) + (ds[e] > 0.f ? -INFINITY : 0.f);
+            }
+          }
+          o[j] = M::mul(__builtin_bit_cast(frag, word4{f[0], f[1], f[2], f[3]}), p, o[j]);
+        }
+      }
+    };
+    if (s.n > 0) {
+      Tile x[2];
+      int64_t next = look_up(t0);
+      request(x[0], t0, next);
+      next = look_up(min(t0 + 1, t1 - 1));
+      for (int t = t0; t < t1; t += 2) {
+        if (t + 1 < t1) request(x[1], t + 1, next);
+        next = look_up(min(t + 2, t1 - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        add(x[0], t);
+        __builtin_amdgcn_sched_barrier(0);
+        if (t + 1 < t1) {
+          if (t + 2 < t1) request(x[0], t + 2, next);
+          next = look_up(min(t + 3, t1 - 1));
+          __builtin_amdgcn_sched_barrier(0);
+          add(x[1], t + 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      }
+    }
+    l = split_sum(l);
+    // accumulator element e of product j: feature VF (4 g + e) + j of my row (fp32 with 128 features: 4 (4 g + e) + j % 4 of half j / 4)
+    auto feature = [&](int e, int j) { return VB == 32 ? 64 * (j >> 2) + 4 * (4 * g + e) + (j & 3) : VF * (4 * g + e) + j; };
+    if (t0 == 0 && t1 == s.tiles) {
+      if (row_there) {
+        T *out = (T *)(a.out.p + (s.first + token) * a.out.row + head * a.out.head);
+        const bool nothing = m == -INFINITY && l == 0.f;              // (NaN logits leave l NaN)
+        const float inv = 1.f / l;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+#pragma unroll
+          for (int j = 0; j < VF; ++j) out[feature(e, j)] = kv_round<T>(nothing ? 0.f : o[j][e] * inv);
+      }
+    } else if (row_there) {
+      float *part = parts + ((int64_t)worker * 2 + (begins ? 0 : 1)) * split_part_floats<DH>();
+      if (g == 0) {
+        part[l16] = m;
+        part[kRows + l16] = l;
+      }
+      float *to = part + 2 * kRows + l16 * DH;
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int j = 0; j < VF; ++j) to[feature(e, j)] = o[j][e];
+    }
+    tile += t1 - t0;
+    begins = false;
+  }
+}
+
+// One wavefront per query row and key head's row block: adds up the parts of its unit, if it was cut.
+template <typename T, int DH>
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttention a, const float *__restrict__ parts) {
+  constexpr int KT = SplitShape<T, DH>::KT;
+  const int lane = threadIdx.x & 63;
+  const int group = a.n_q_heads / a.n_kv_heads;
+  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t q_row = item / a.n_q_heads;
+  const int head = (int)(item - q_row * a.n_q_heads), kvh = head / group;
+  if (q_row >= a.batch.n_rows) return;
+  int seq = (int)q_row;
+  if (a.batch.offsets) {
+    seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, q_row, lane);
+    if (seq >= a.batch.n_seqs) return;
+  }
+  const SplitSeq s = split_sequence<KT>(a, seq, false);
+  const int row = (int)(q_row - s.first) * group + head - kvh * group;
+  if (q_row < s.first || row >= s.rows) return;
+  // tiles of all units and of the sequences before this one
+  int64_t total = 0, before = 0;
+  for (int b = lane; b < a.batch.n_seqs; b += 64) {
+    const SplitSeq x = split_sequence<KT>(a, b, false);
+    const int64_t tiles = (int64_t)x.blocks * x.tiles;
+    total += tiles;
+    before += b < seq ? tiles : 0;
+  }
+  total = split_lane(split_scan(total), 63) * a.n_kv_heads;
+  before = split_lane(split_scan(before), 63) * a.n_kv_heads;
+  const int64_t per = (total + kWorkers - 1) / kWorkers;
+  const int64_t first = before + (int64_t)(kvh * s.blocks + row / kRows) * s.tiles, last = first + s.tiles - 1;
+  const int w0 = (int)(first / per), w1 = (int)(last / per);
+  if (w0 == w1) return;                                           // it was not cut
+  constexpr int N = DH >= 64 ? DH / 64 : 1;
+  const int f = lane * N;
+  const int r = row % kRows;
+  float m = -INFINITY, l = 0.f, o[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) o[i] = 0.f;
+  for (int w = w0; w <= w1; ++w) {
+    const float *part = parts + ((int64_t)w * 2 + (w == w0 && first > (int64_t)w0 * per ? 1 : 0)) * split_part_floats<DH>();
+    const float mw = part[r], lw = part[kRows + r];
+    const float m_new = fmaxf(m, mw), m_at = m_new == -INFINITY ? 0.f : m_new;
+    const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_at), take = mw == m_new ? 1.f : __builtin_amdgcn_exp2f(mw - m_at);
+    l = l * keep + lw * take;
+#pragma unroll
+    for (int i = 0; i < N; ++i) o[i] = o[i] * keep + (f + i < DH ? part[2 * kRows + r * DH + f + i] : 0.f) * take;
+    m = m_new;
+  }
+  if (f >= DH) return;
+  T *out = (T *)(a.out.p + q_row * a.out.row + head * a.out.head);
+  const float inv = 1.f / l;
+#pragma unroll
+  for (int i = 0; i < N; ++i) out[f + i] = kv_round<T>(m == -INFINITY && l == 0.f ? 0.f : o[i] * inv);
+}
+
+}  // namespace
+
+int64_t kv_split_workspace_bytes(int32_t head_dim) {
+  return (int64_t)kWorkers * 2 * 4 * (head_dim == 32 ? split_part_floats<32>() : head_dim == 64 ? split_part_floats<64>() : split_part_floats<128>());
+}
+
+hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream) {
+  const unsigned joins = (unsigned)((a.batch.n_rows * a.n_q_heads + 3) / 4);
+  kv_with_type(a.dtype, [&](auto t) {
+    using T = decltype(t);
+    kv_with_width(a.head_dim, [&](auto width) {
+      constexpr int DH = decltype(width)::value;
+      kv_split_kernel<T, DH><<<kWorkers / 4, 256, 0, stream>>>(a, (float *)workspace);
+      kv_join_kernel<T, DH><<<joins, 256, 0, stream>>>(a, (const float *)workspace);
+    });
+  });
+  return hipGetLastError();
+}
+
+}  // namespace flame
