@@ -48,6 +48,18 @@ template <typename F> inline void kv_with_width(int32_t head_dim, F f) {
   else f(std::integral_constant<int, 128>{});
 }
 
+// Infinities and NaN in a word of one fp32 or two 16-bit values.
+template <typename T> constexpr uint32_t kv_exponent() { return sizeof(T) == 4 ? 0x7f800000u : std::is_same<T, bf16_t>::value ? 0x7f80u : 0x7c00u; }
+template <typename T> __device__ __forceinline__ bool not_finite(uint32_t w) {
+  constexpr uint32_t E = kv_exponent<T>();
+  return sizeof(T) == 4 ? (w & E) == E : (w & E) == E || (w >> 16 & E) == E;
+}
+template <typename T> __device__ __forceinline__ uint32_t only_finite(uint32_t w) {
+  constexpr uint32_t E = kv_exponent<T>();
+  if (sizeof(T) == 4) return (w & E) == E ? 0u : w;
+  return ((w & E) == E ? 0u : w & 0xffffu) | ((w >> 16 & E) == E ? 0u : w & 0xffff0000u);
+}
+
 // One rounding of an fp32 result, to nearest; an fp16 one past the largest finite value becomes infinite, as in IEEE arithmetic.
 template <typename T> __device__ __forceinline__ T kv_round(float v) { return (T)v; }
 

@@ -134,12 +134,10 @@ template <typename T> struct Matrix16;
 template <> struct Matrix16<bf16_t> {
   typedef bf16x8 frag;
   static __device__ __forceinline__ f32x4 mul(frag x, frag y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0); }
-  static constexpr uint32_t kExponent = 0x7f80, kFraction = 0x007f, kOne = 0x3f80;
 };
 template <> struct Matrix16<half_t> {
   typedef f16x8 frag;
   static __device__ __forceinline__ f32x4 mul(frag x, frag y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0); }
-  static constexpr uint32_t kExponent = 0x7c00, kFraction = 0x03ff, kOne = 0x3c00;
 };
 
 template <typename T, int DH>
@@ -238,7 +236,7 @@ __global__ __launch_bounds__(256, 2) void kv_split_kernel(KvAttention a, float *
         }
       }
     };
-    auto add = [&](const Tile &x, int t) {
+    auto add = [&](Tile &x, int t) {
       f32x4 z[KB];
 #pragma unroll
       for (int b = 0; b < KB; ++b) z[b] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -256,14 +254,15 @@ __global__ __launch_bounds__(256, 2) void kv_split_kernel(KvAttention a, float *
         }
       // element e of block b: key VK g + 4 b + e of the tile
       const int k0 = t * KT + VK * g;
-      const uint32_t here = (uint32_t)(x.there >> (VK * g)) & ((1u << VK) - 1);
+      const uint32_t here = (uint32_t)(x.there >> (VK * g)) & ((1u << VK) - 1);                       // of my VK keys those that count,
+      const uint32_t seen = here & ((1u << max(0, min(VK, sees - k0))) - 1);                         // and those of them that my row sees
       const bool masked = x.there != ~0ull || t * KT + KT > sees_least;
       float w[VK];
 #pragma unroll
       for (int i = 0; i < VK; ++i) w[i] = z[i >> 2][i & 3] * scale;
       if (masked) {
 #pragma unroll
-        for (int i = 0; i < VK; ++i) w[i] = (here >> i & 1) && k0 + i < sees ? w[i] : -INFINITY;
+        for (int i = 0; i < VK; ++i) w[i] = seen >> i & 1 ? w[i] : -INFINITY;
       }
       float top = w[0];
 #pragma unroll
@@ -284,95 +283,87 @@ __global__ __launch_bounds__(256, 2) void kv_split_kernel(KvAttention a, float *
         w[i] = __builtin_amdgcn_exp2f(w[i] - m_at);
         l += w[i];
       }
-      if constexpr (F32) {
+      if (masked) {
+        // Values of keys that do not count are zeros, and infinite or NaN ones, which a row that does not see them must not meet in a product, are taken out and
+        // added to the rows that do see them.
+        bool odd = false;
 #pragma unroll
-        for (int i = 0; i < VK; ++i) {
-          const bool counts = (here >> i & 1);
-          const bool seen = counts && k0 + i < sees;
+        for (int i = 0; i < VK; ++i)
+#pragma unroll
+          for (int n = 0; n < VW; ++n) {
+            x.v[i][n] = here >> i & 1 ? x.v[i][n] : 0u;
+            odd |= not_finite<T>(x.v[i][n]);
+          }
+        if (__builtin_amdgcn_ballot_w64(odd)) {
+          const f32x4 none = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int j = 0; j < VF; ++j) {
-            const float v = counts ? __uint_as_float(x.v[i][j]) : 0.f;
-            if (masked && __builtin_amdgcn_ballot_w64(!(fabsf(v) <= 3.4e38f))) {
-              // an infinite or NaN value in a tile that some row does not see all of: rows that do not see it must not meet it in a product
-              const bool finite = fabsf(v) <= 3.4e38f;
-              o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(finite ? v : 0.f, w[i], o[j], 0, 0, 0);
-              const f32x4 none = {0.f, 0.f, 0.f, 0.f};
-              const f32x4 up = __builtin_amdgcn_mfma_f32_16x16x4f32(finite || v == -INFINITY ? 0.f : 1.f, seen ? 1.f : 0.f, none, 0, 0, 0);
-              const f32x4 down = __builtin_amdgcn_mfma_f32_16x16x4f32(finite || v == INFINITY ? 0.f : 1.f, seen ? 1.f : 0.f, none, 0, 0, 0);
+            f32x4 up = none, down = none;
+            if constexpr (F32) {
 #pragma unroll
-              for (int e = 0; e < 4; ++e) o[j][e] += (up[e] > 0.f ? INFINITY : 0.f) + (down[e] > 0.f ? -INFINITY : 0.f);
+              for (int i = 0; i < VK; ++i) {
+                const float v = __uint_as_float(x.v[i][j]), one = (float)(seen >> i & 1);
+                up = __builtin_amdgcn_mfma_f32_16x16x4f32(v != v || v == INFINITY ? 1.f : 0.f, one, up, 0, 0, 0);
+                down = __builtin_amdgcn_mfma_f32_16x16x4f32(v != v || v == -INFINITY ? 1.f : 0.f, one, down, 0, 0, 0);
+              }
             } else {
-              o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(v, w[i], o[j], 0, 0, 0);
-            }
-          }
-        }
-      } else {
-        typedef Matrix16<T> M;
-        typedef typename M::frag frag;
-        frag p, ones;
+              typename Matrix16<T>::frag u, d, ones;
 #pragma unroll
-        for (int i = 0; i < VK; ++i) {
-          p[i] = (T)w[i];
-          ones[i] = (T)((here >> i & 1) && k0 + i < sees ? 1.f : 0.f);
+              for (int i = 0; i < VK; ++i) {
+                const float v = (float)__builtin_bit_cast(T, (uint16_t)(x.v[i][j >> 1] >> (16 * (j & 1))));
+                u[i] = (T)(v != v || v == INFINITY ? 1.f : 0.f);
+                d[i] = (T)(v != v || v == -INFINITY ? 1.f : 0.f);
+                ones[i] = (T)(float)(seen >> i & 1);
+              }
+              up = Matrix16<T>::mul(u, ones, none);
+              down = Matrix16<T>::mul(d, ones, none);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[j][e] += (up[e] > 0.f ? INFINITY : 0.f) + (down[e] > 0.f ? -INFINITY : 0.f);
+          }
+#pragma unroll
+          for (int i = 0; i < VK; ++i)
+#pragma unroll
+            for (int n = 0; n < VW; ++n) x.v[i][n] = only_finite<T>(x.v[i][n]);
         }
+      }
+      if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < VK; ++i)
+#pragma unroll
+          for (int j = 0; j < VF; ++j) o[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(x.v[i][j]), w[i], o[j], 0, 0, 0);
+      } else {
+        typedef typename Matrix16<T>::frag frag;
+        frag p;
+#pragma unroll
+        for (int i = 0; i < VK; ++i) p[i] = (T)w[i];
 #pragma unroll
         for (int j = 0; j < VF; ++j) {
           // feature VF l16 + j of keys VK g..VK g + 7: the lower or upper halves of word j / 2 of the eight rows
-          uint32_t f[4];
+          word4 f;
 #pragma unroll
           for (int i = 0; i < 4; ++i) f[i] = __builtin_amdgcn_perm(x.v[2 * i + 1][j >> 1], x.v[2 * i][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
-          if (masked) {
-            bool odd = false;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              f[i] &= ((here >> (2 * i) & 1) ? 0xffffu : 0u) | ((here >> (2 * i + 1) & 1) ? 0xffff0000u : 0u);
-              odd |= (f[i] & M::kExponent) == M::kExponent || (f[i] >> 16 & M::kExponent) == M::kExponent;
-            }
-            if (__builtin_amdgcn_ballot_w64(odd)) {
-              // an infinite or NaN value in a tile that some row does not see all of: rows that do not see it must not meet it in a product
-              uint32_t up[4], down[4];
-#pragma unroll
-              for (int i = 0; i < 4; ++i) {
-                uint32_t keep = 0, u = 0, d = 0;
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                  const uint32_t v = f[i] >> (16 * h) & 0xffff;
-                  const bool finite = (v & M::kExponent) != M::kExponent, nan = !finite && (v & M::kFraction);
-                  keep |= finite ? v << (16 * h) : 0u;
-                  u |= !finite && (nan || !(v >> 15)) ? M::kOne << (16 * h) : 0u;
-                  d |= !finite && (nan || v >> 15) ? M::kOne << (16 * h) : 0u;
-                }
-                f[i] = keep; up[i] = u; down[i] = d;
-              }
-              const f32x4 none = {0.f, 0.f, 0.f, 0.f};
-              const f32x4 us = M::mul(__builtin_bit_cast(frag, word4{up[0], up[1], up[2], up[3]}), ones, none);
-              const f32x4 ds = M::mul(__builtin_bit_cast(frag, word4{down[0], down[1], down[2], down[3]}), ones, none);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) o[j][e] += (us[e] > 0.f ? INFINITY : 0.f) + (ds[e] > 0.f ? -INFINITY : 0.f);
-            }
-          }
-          o[j] = M::mul(__builtin_bit_cast(frag, word4{f[0], f[1], f[2], f[3]}), p, o[j]);
+          o[j] = Matrix16<T>::mul(__builtin_bit_cast(frag, f), p, o[j]);
         }
       }
     };
     if (s.n > 0) {
-      Tile x[2];
-      int64_t next = look_up(t0);
-      request(x[0], t0, next);
-      next = look_up(min(t0 + 1, t1 - 1));
+      Tile x, y;
+      request(x, t0, look_up(t0));
+      int64_t next = look_up(min(t0 + 1, t1 - 1));
+#pragma unroll 1
       for (int t = t0; t < t1; t += 2) {
-        if (t + 1 < t1) request(x[1], t + 1, next);
+        request(y, min(t + 1, t1 - 1), next);
         next = look_up(min(t + 2, t1 - 1));
         __builtin_amdgcn_sched_barrier(0);
-        add(x[0], t);
+        add(x, t);
         __builtin_amdgcn_sched_barrier(0);
-        if (t + 1 < t1) {
-          if (t + 2 < t1) request(x[0], t + 2, next);
-          next = look_up(min(t + 3, t1 - 1));
-          __builtin_amdgcn_sched_barrier(0);
-          add(x[1], t + 1);
-          __builtin_amdgcn_sched_barrier(0);
-        }
+        if (t + 1 >= t1) break;
+        request(x, min(t + 2, t1 - 1), next);
+        next = look_up(min(t + 3, t1 - 1));
+        __builtin_amdgcn_sched_barrier(0);
+        add(y, t + 1);
+        __builtin_amdgcn_sched_barrier(0);
       }
     }
     l = split_sum(l);
@@ -405,17 +396,18 @@ __global__ __launch_bounds__(256, 2) void kv_split_kernel(KvAttention a, float *
   }
 }
 
-// One wavefront per query row and key head's row block: adds up the parts of its unit, if it was cut.
+// One workgroup per query row and head: adds up the parts of its unit, if it was cut.  Bound by latency: DH / 4 lanes share a part, so that
+// 8 to 32 parts are read at once.
 template <typename T, int DH>
 __global__ __launch_bounds__(256) void kv_join_kernel(KvAttention a, const float *__restrict__ parts) {
   constexpr int KT = SplitShape<T, DH>::KT;
+  constexpr int L = DH / 4, P = 256 / L;                          // lanes of a part, parts at once
+  __shared__ float m_s[P], l_s[P], o_s[P][DH + 4];
   const int lane = threadIdx.x & 63;
   const int group = a.n_q_heads / a.n_kv_heads;
-  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t q_row = item / a.n_q_heads;
-  const int head = (int)(item - q_row * a.n_q_heads), kvh = head / group;
-  if (q_row >= a.batch.n_rows) return;
-  int seq = (int)q_row;
+  const int q_row = blockIdx.x / a.n_q_heads;
+  const int head = blockIdx.x - q_row * a.n_q_heads, kvh = head / group;
+  int seq = q_row;
   if (a.batch.offsets) {
     seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, q_row, lane);
     if (seq >= a.batch.n_seqs) return;
@@ -437,27 +429,37 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttention a, const float
   const int64_t first = before + (int64_t)(kvh * s.blocks + row / kRows) * s.tiles, last = first + s.tiles - 1;
   const int w0 = (int)(first / per), w1 = (int)(last / per);
   if (w0 == w1) return;                                           // it was not cut
-  constexpr int N = DH >= 64 ? DH / 64 : 1;
-  const int f = lane * N;
-  const int r = row % kRows;
-  float m = -INFINITY, l = 0.f, o[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) o[i] = 0.f;
-  for (int w = w0; w <= w1; ++w) {
-    const float *part = parts + ((int64_t)w * 2 + (w == w0 && first > (int64_t)w0 * per ? 1 : 0)) * split_part_floats<DH>();
+  const int r = row % kRows, p = threadIdx.x / L, f = threadIdx.x % L * 4;
+  const bool later = first > (int64_t)w0 * per;                   // in the first worker it is not the unit that the worker begins with
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int w = w0 + p; w <= w1; w += P) {
+    const float *part = parts + ((int64_t)w * 2 + (w == w0 && later ? 1 : 0)) * split_part_floats<DH>();
     const float mw = part[r], lw = part[kRows + r];
+    const f32x4 ow = *(const f32x4 *)(part + 2 * kRows + r * DH + f);
     const float m_new = fmaxf(m, mw), m_at = m_new == -INFINITY ? 0.f : m_new;
     const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_at), take = mw == m_new ? 1.f : __builtin_amdgcn_exp2f(mw - m_at);
     l = l * keep + lw * take;
 #pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = o[i] * keep + (f + i < DH ? part[2 * kRows + r * DH + f + i] : 0.f) * take;
+    for (int i = 0; i < 4; ++i) o[i] = o[i] * keep + ow[i] * take;
     m = m_new;
   }
-  if (f >= DH) return;
-  T *out = (T *)(a.out.p + q_row * a.out.row + head * a.out.head);
-  const float inv = 1.f / l;
+  *(f32x4 *)&o_s[p][f] = o;
+  if (f == 0) { m_s[p] = m; l_s[p] = l; }
+  __syncthreads();
+  if (threadIdx.x >= DH) return;
+  float top = -INFINITY, sum = 0.f, out = 0.f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) out[f + i] = kv_round<T>(m == -INFINITY && l == 0.f ? 0.f : o[i] * inv);
+  for (int i = 0; i < P; ++i) top = fmaxf(top, m_s[i]);
+  const float at = top == -INFINITY ? 0.f : top;
+#pragma unroll
+  for (int i = 0; i < P; ++i) {
+    const float take = m_s[i] == top ? 1.f : __builtin_amdgcn_exp2f(m_s[i] - at);
+    sum += l_s[i] * take;
+    out += o_s[i][threadIdx.x] * take;
+  }
+  ((T *)(a.out.p + (int64_t)q_row * a.out.row + head * a.out.head))[threadIdx.x] = kv_round<T>(top == -INFINITY && sum == 0.f ? 0.f : out / sum);
 }
 
 }  // namespace
@@ -467,7 +469,7 @@ int64_t kv_split_workspace_bytes(int32_t head_dim) {
 }
 
 hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream) {
-  const unsigned joins = (unsigned)((a.batch.n_rows * a.n_q_heads + 3) / 4);
+  const unsigned joins = (unsigned)(a.batch.n_rows * a.n_q_heads);
   kv_with_type(a.dtype, [&](auto t) {
     using T = decltype(t);
     kv_with_width(a.head_dim, [&](auto width) {
