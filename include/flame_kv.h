@@ -78,7 +78,7 @@ typedef struct {
   int32_t n_pages, page_size; /* page_size: any, 1..65536 */
   const int32_t *page_table; /* device [n_seqs][table_stride], the first pages_per_seq entries of a row in use */
   int64_t table_stride;
-  int32_t pages_per_seq;
+  int32_t pages_per_seq;     /* pages_per_seq * page_size: up to 2^31 - 65536 */
 } flame_kv_cache;
 
 typedef struct {

@@ -19,9 +19,10 @@ int done(hipError_t e) {
   return bad(hipGetErrorString(e), FLAME_GR_HIP_ERROR);
 }
 
-// A grid dimension may have 2^32 - 1 threads in all, and offsets are 32 bits: this many rows times heads is far beyond both a call's use and its memory.
-constexpr int64_t kMaxRowHeads = (int64_t)1 << 25;
-constexpr int32_t kMaxSequences = 1 << 22;
+// A grid dimension may have 2^32 - 1 threads.  Attention of packed rows has two of them per row and head, and 256 per sequence and head; split attention, of as many rows as
+// sequences or a few times that, 256 per row and head.
+constexpr int64_t kMaxRowHeads = (int64_t)1 << 25, kMaxSplitRowHeads = ((int64_t)1 << 24) - 1, kMaxSequenceHeads = ((int64_t)1 << 23) - 1;
+constexpr int64_t kMaxKeys = ((int64_t)1 << 31) - 65536;     // of a sequence: room for a tile's end behind them in 32 bits
 
 int64_t element(int32_t dtype) { return dtype == FLAME_KV_F32 ? 4 : 2; }
 bool aligned(const void *p) { return ((uintptr_t)p & 15) == 0; }
@@ -37,7 +38,7 @@ int check_config(const flame_kv_config *c) {
 }
 
 int check_batch(const flame_kv_config *c, int32_t n_seqs, int64_t n_rows) {
-  if (n_seqs < 0 || n_seqs > kMaxSequences) return bad("n_seqs out of range");
+  if (n_seqs < 0 || (int64_t)n_seqs * c->n_q_heads > kMaxSequenceHeads) return bad("sequences times heads must be in [0, 2^23)");
   if (n_rows < 0 || n_rows * c->n_q_heads > kMaxRowHeads) return bad("rows times heads must be in [0, 2^25]");
   return FLAME_GR_OK;
 }
@@ -54,7 +55,7 @@ int take_pages(const flame_kv_config *c, const flame_kv_cache *cache, KvPages *o
   if (!cache) return bad("the cache is NULL");
   if (!cache->k || !cache->v || !cache->page_table) return bad("a pointer of the cache is NULL");
   if (cache->n_pages < 1 || cache->page_size < 1 || cache->page_size > 65536) return bad("n_pages must be positive and page_size in [1, 65536]");
-  if (cache->pages_per_seq < 1 || (int64_t)cache->pages_per_seq * cache->page_size > INT32_MAX) return bad("pages_per_seq must be positive, and a sequence within 2^31 - 1 tokens");
+  if (cache->pages_per_seq < 1 || (int64_t)cache->pages_per_seq * cache->page_size > kMaxKeys) return bad("pages_per_seq must be positive, and a sequence within 2^31 - 65536 tokens");
   const int64_t size = element(c->dtype);
   if (!aligned(cache->k) || !aligned(cache->v) || (cache->page_stride * size) % 16 || (cache->slot_stride * size) % 16 || (cache->head_stride * size) % 16)
     return bad("the cache must be 16-byte aligned, with strides of multiples of 16 bytes");
@@ -90,7 +91,9 @@ void take_heads(const flame_kv_config *c, KvAttention *a) {
 }
 
 // Calls of a few rows per sequence split the keys over the chip.
-bool splits(const flame_kv_config *c, int32_t n_seqs, int64_t n_rows) { return n_rows * (c->n_q_heads / c->n_kv_heads) <= (int64_t)64 * n_seqs; }
+bool splits(const flame_kv_config *c, int32_t n_seqs, int64_t n_rows) {
+  return n_rows * (c->n_q_heads / c->n_kv_heads) <= (int64_t)64 * n_seqs && n_rows * c->n_q_heads <= kMaxSplitRowHeads;
+}
 int64_t workspace_bytes_for(const flame_kv_config *c, int32_t n_seqs, int64_t n_rows) { return splits(c, n_seqs, n_rows) ? kv_split_workspace_bytes(c->head_dim) : 0; }
 
 int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_rows,
@@ -159,7 +162,7 @@ int flame_kv_prompt(const flame_kv_config *cfg, const flame_kv_rows *q, const fl
   g_kv_error = "";
   if (int rc = check_config(cfg)) return rc;
   if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
-  if (n_keys < 0 || n_keys > INT32_MAX) return bad("n_keys out of range");
+  if (n_keys < 0 || n_keys > kMaxKeys) return bad("n_keys out of range");
   if (n_seqs == 0 || n_tokens == 0) return FLAME_GR_OK;
   KvAttention a{};
   if (int rc = take_rows(cfg, q, &a.q)) return rc;

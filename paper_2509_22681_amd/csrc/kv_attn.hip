@@ -1,32 +1,359 @@
 // Causal softmax attention of packed query rows with grouped heads, over packed keys or a paged cache.
 //
-// One wavefront per query row and head runs through the row's keys once, one key at a time, with the running maximum and sum of the softmax:
-// the lanes share the features.
+// Bound by the matrix pipe and the vector work of the softmax beside it.  A workgroup takes 128 query rows of one sequence and key head, row = token * G + head of the
+// group (the G query heads that share a key head are rows of one tile: short sequences fill it, and the mask cuts through fewer key tiles), four wavefronts of 32 rows each.  It
+// walks the keys in tiles of 64, two stages in LDS, brought there by LDS-DMA loads one tile ahead.  Products are transposed as in attn_mfma.hip,
+//     S^T[key][row] = K Q^T        A operand = K rows, B operand = Q rows
+//     O^T[feature][row] += V^T P^T A operand = V^T rows, B operand = P^T
+// so that the first product's accumulator, where a lane has one row and 16 of 32 keys, is the second product's B operand as it stands: elements 8 s + i of a lane in half h are keys
+// 16 s + 8 (i / 4) + 4 h + i % 4.  V lies in the cache key by key, and the A operand wants eight keys of a feature per lane: the transposing LDS read (ds_read_b64_tr_b16) gives
+// each of 16 lanes one column of four 16-bit rows, so two of them make a fragment.
+//
+// LDS rows are unpadded, as the DMA fills 1 KB of consecutive bytes, and swizzled by XOR: K in 16-byte chunks with the low bits of the key, V in 32-byte chunks so that the four
+// rows and two neighbouring chunks that 32 lanes of a transposing read touch lie in the eight different 32-byte slots of 256 bytes.
+//
+// Where a key lies: one wavefront looks the tile's 64 keys up, two tiles ahead, and leaves their byte offsets in LDS for the requests of all; packed keys take the same way.  Any page
+// size and any strides cost the same.
+//
+// Masked keys: their logits are -infinity, and their values meet weights of zero.  That is harmless while they are finite.  If a workgroup's
+// results are not all finite at the end, it runs its keys once more with the values of masked tiles taken apart (see `careful`), so that infinities and NaN reach exactly the rows that see them.
+#include "kernels.h"
 #include "kv_device.h"
 
 namespace flame {
 
 namespace {
 
-template <typename T, int DH>
+constexpr int QT = 128;             // query rows of a workgroup
+constexpr int KT = 64;              // keys of a tile
+
+template <typename T> struct Matrix32;
+template <> struct Matrix32<bf16_t> {
+  typedef bf16x8 frag;
+  static __device__ __forceinline__ f32x16 mul(frag x, frag y, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0); }
+};
+template <> struct Matrix32<half_t> {
+  typedef f16x8 frag;
+  static __device__ __forceinline__ f32x16 mul(frag x, frag y, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(x, y, c, 0, 0, 0); }
+};
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+
+template <typename T, int DH, bool PAGED>
+__global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
+  typedef typename Matrix32<T>::frag frag;
+  constexpr int KS = DH / 16, DB = DH / 32, CH = DH / 8;          // k-steps, feature blocks, 16-byte chunks of a row
+  constexpr int TILE = KT * DH * 2;                               // bytes of a K or V tile
+  constexpr int STAGE = 2 * TILE;
+  constexpr int RPI = 64 / CH, NI = TILE / 1024 / 4;              // rows of a 1 KB request, requests of a wavefront per tile of K or V
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  __shared__ int64_t at_s[3][PAGED ? 1 : 2][KT];                  // byte offsets of a tile's keys (packed: and values)
+  __shared__ uint64_t there_s[3];                                 // which of them count
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int l32 = lane & 31, lh = lane >> 5;
+  const int group = a.n_q_heads / a.n_kv_heads;
+
+  // Which tile: those of sequence b begin at slot offsets[b] * G / QT + b, where there is room for them whatever the lengths; the last ones, with most keys, go first.
+  const int kvh = blockIdx.x % a.n_kv_heads;
+  const int64_t slot = gridDim.x / a.n_kv_heads - 1 - blockIdx.x / a.n_kv_heads;
+  int seq;
+  {
+    int lo = 0, n = a.batch.n_seqs;                               // the last sequence whose slots begin at or before this one
+    while (n > 1) {
+      const int step = (n + 63) / 64;
+      const int b = lo + min((lane + 1) * step, n - 1);
+      const bool after = (lane + 1) * step >= n || (int64_t)a.batch.offsets[b] * group / QT + b > slot;
+      const int c = __builtin_ctzll(__builtin_amdgcn_ballot_w64(after) | 1ull << 63);
+      lo += c * step;
+      n = max(1, min(step, n - c * step));
+    }
+    seq = min(lo, a.batch.n_seqs - 1);
+  }
+  const int64_t first = a.batch.offsets[seq], end = a.batch.offsets[seq + 1];
+  const bool wrong = first < 0 || end < first || end > a.batch.n_rows;
+  if (wrong && threadIdx.x == 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
+  if (first < 0 || end < first) return;
+  const int64_t tile = slot - (first * group / QT + seq);
+  const int rows = (int)max((int64_t)0, min(end, a.batch.n_rows) - first) * group;
+  if (tile < 0 || tile * QT >= rows) return;
+  const int row0 = (int)tile * QT;
+
+  int n;
+  const char *kp, *vp;
+  const int32_t *table = nullptr;
+  if (PAGED) {
+    n = kv_clip_length(a.batch.kv_lens[seq], a.pages.capacity, a.batch.faults, threadIdx.x == 0);
+    kp = a.pages.k + kvh * a.pages.head;
+    vp = a.pages.v + kvh * a.pages.head;
+    table = a.pages.table + seq * a.pages.table_stride;
+  } else {
+    const int32_t *ko = a.k_offsets ? a.k_offsets : a.batch.offsets;
+    const int64_t k_first = ko[seq], k_end = ko[seq + 1];
+    if ((k_first < 0 || k_end < k_first || k_end > a.n_keys) && threadIdx.x == 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
+    n = k_first < 0 ? 0 : (int)max((int64_t)0, min(k_end, a.n_keys) - k_first);
+    kp = a.k.p + k_first * a.k.row + kvh * a.k.head;
+    vp = a.v.p + k_first * a.v.row + kvh * a.v.head;
+  }
+  // keys seen: by the row before the first one of the sequence, by the last row of the workgroup, by the first and last of my wavefront, by my row
+  const int64_t back = n - (end - first);
+  auto seen_by = [&](int row) { return (int)max((int64_t)0, back + row / group + 1); };
+  const int n_seen = seen_by(min(row0 + QT, rows) - 1), n_tiles = (n_seen + KT - 1) / KT;
+  const int wave_row = row0 + wave * 32;
+  const bool active = wave_row < rows;
+  const int my_row = active ? min(wave_row + l32, rows - 1) : row0, token = my_row / group, head = kvh * group + my_row - token * group;
+  const int sees = seen_by(my_row), wave_least = active ? seen_by(wave_row) : 0, wave_most = active ? seen_by(min(wave_row + 31, rows - 1)) : 0;
+  const bool row_there = active && wave_row + l32 < rows;
+
+  typedef __attribute__((address_space(1))) const void gvoid;
+  typedef __attribute__((address_space(3))) void lvoid;
+  auto look_up = [&](int t, int64_t (&to)[2]) {                   // of key `lane` of tile t; -1: none
+    const int key = t * KT + lane;
+    const int near = min(key, n - 1);
+    if (PAGED) {
+      to[0] = kv_token_offset(a.pages, table, (uint32_t)near);
+    } else {
+      to[0] = near * a.k.row;
+      to[1] = near * a.v.row;
+    }
+  };
+  auto publish = [&](int t, const int64_t (&from)[2]) {
+    const int64_t k_at = from[0];
+    if (PAGED && k_at < 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_PAGE);
+    at_s[t % 3][0][lane] = max(k_at, (int64_t)0);
+    if (!PAGED) at_s[t % 3][PAGED ? 0 : 1][lane] = from[1];
+    const uint64_t there = __builtin_amdgcn_ballot_w64((!PAGED || k_at >= 0) && t * KT + lane < n);
+    if (lane == 0) there_s[t % 3] = there;
+  };
+  // Request j of a tile is rows j RPI..; lane p brings the chunk that belongs at byte 16 p of it.
+  const int in_row = lane / CH, chunk = lane % CH;
+  auto request = [&](int t) {
+    char *stage = lds + (t & 1) * STAGE;
+    const int64_t *ka = at_s[t % 3][0], *va = at_s[t % 3][PAGED ? 0 : 1];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int j = wave + 4 * i, r = j * RPI + in_row;
+      const int kc = DH == 128 ? chunk ^ (r & 15) : DH == 64 ? chunk ^ (r >> 1 & 7) : chunk ^ (r >> 2 & 3);
+      const int vc = DH == 128 ? chunk ^ (4 * (r & 3)) : DH == 64 ? chunk ^ (4 * (r >> 1 & 1)) : chunk;
+      __builtin_amdgcn_global_load_lds((gvoid *)(kp + ka[r] + kc * 16), (lvoid *)(stage + j * 1024), 16, 0, 0);
+      __builtin_amdgcn_global_load_lds((gvoid *)(vp + va[r] + vc * 16), (lvoid *)(stage + TILE + j * 1024), 16, 0, 0);
+    }
+  };
+
+  frag fq[KS];
+  {
+    const char *q = a.q.p + (first + token) * a.q.row + head * a.q.head;
+#pragma unroll
+    for (int s = 0; s < KS; ++s) fq[s] = *(const frag *)(q + s * 32 + lh * 16);
+  }
+  const float scale = a.scale * kLog2e;
+  // K: row l32 (+ 32) of the tile, chunk 2 s + lh
+  const int k_key = DH == 128 ? l32 & 15 : DH == 64 ? l32 >> 1 & 7 : l32 >> 2 & 3;
+  const int ka0 = l32 * (DH * 2) + ((k_key ^ lh) << 4);           // ^ (s << 5)
+  // V: lane l of a transposing read addresses key 4 lh + (l % 16) / 4, features 16 (l / 16 % 2) + 4 (l % 4), and gets feature l % 32 of four keys
+  const int v_row = 4 * lh + (lane >> 2 & 3);
+  const int v_key = DH == 128 ? 4 * (v_row & 3) : DH == 64 ? 4 * (v_row >> 1 & 1) : 0;   // (rows 8 further have the same)
+  const int va0 = v_row * (DH * 2) + ((((lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ v_key) << 4) + (lane & 1) * 8;   // ^ (b << 6), + 8 rows each
+
+  f32x16 o[DB];
+  float m, l;
+  auto tile_step = [&](int t, bool careful) {
+    const char *sk = lds + (t & 1) * STAGE, *sv = sk + TILE;
+    const int k0 = t * KT;
+    if (k0 >= wave_most) return;
+    const uint64_t there = there_s[t % 3];
+    const uint32_t there_lo = __builtin_amdgcn_readfirstlane((int)there), there_hi = __builtin_amdgcn_readfirstlane((int)(there >> 32));
+    const bool masked = k0 + KT > wave_least || (there_lo & there_hi) != 0xffffffffu;
+    f32x16 z[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) z[j][e] = 0.f;
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const frag fk = *(const frag *)(sk + j * (32 * DH * 2) + (ka0 ^ (s << 5)));
+        z[j] = Matrix32<T>::mul(fk, fq[s], z[j]);
+      }
+    // element e of block j: key 32 j + 8 (e / 4) + 4 lh + e % 4
+    uint32_t seen[2] = {~0u, ~0u};                                // of the keys of a block, by their place in it
+    if (masked) {
+      const int left = sees - k0;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const int here = min(32, max(0, left - 32 * j));
+        seen[j] = (j ? there_hi : there_lo) & (here == 32 ? ~0u : (1u << here) - 1);
+        const uint32_t mine = seen[j] >> (4 * lh);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) z[j][e] = mine >> (8 * (e >> 2) + (e & 3)) & 1 ? z[j][e] : -INFINITY;
+      }
+    }
+    auto max3 = [](float x, float y, float w) { return fmaxf(fmaxf(x, y), w); };
+    float l1[10], l2[4];
+#pragma unroll
+    for (int k = 0; k < 10; ++k) {
+      const int e = 3 * k;
+      l1[k] = max3(z[e >> 4][e & 15], z[(e + 1) >> 4][(e + 1) & 15], z[(e + 2) >> 4][(e + 2) & 15]);
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) l2[k] = max3(l1[3 * k], l1[3 * k + 1], l1[3 * k + 2]);
+    l2[3] = max3(l1[9], z[1][14], z[1][15]);
+    const float top = pair_max(fmaxf(max3(l2[0], l2[1], l2[2]), l2[3])) * scale;
+    const float m_new = fmaxf(m, top);
+    if (__builtin_amdgcn_ballot_w64(m_new != m)) {
+      const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+      l *= keep;
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[b][e] *= keep;
+      m = m_new;
+    }
+    const float nm = m == -INFINITY ? 0.f : -m;                   // (nothing seen yet: all weights are 2^-inf)
+    frag p[4];
+    float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], scale, nm));
+        sum[e & 3] += w;
+        p[2 * j + (e >> 3)][e & 7] = (T)w;
+      }
+    l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+#pragma unroll
+      for (int b = 0; b < DB; ++b) {
+        typedef __attribute__((address_space(3))) s16x4 *ltr;
+        const char *va = sv + s * (16 * DH * 2) + (va0 ^ (b << 6));
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr)va), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr)(va + 8 * DH * 2));
+        s16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
+        if (careful && masked) {
+          // Values of keys that do not count are zeros; infinite and NaN ones are taken out and added to the rows that see them.
+          const uint32_t keys = (s >> 1 ? there_hi : there_lo) >> (16 * (s & 1) + 4 * lh), mine = seen[s >> 1] >> (16 * (s & 1) + 4 * lh);
+          bool odd = false;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const int bit = 8 * (i >> 2) + (i & 3);
+            v[i] = keys >> bit & 1 ? v[i] : (short)0;
+            odd |= ((uint32_t)(uint16_t)v[i] & kv_exponent<T>()) == kv_exponent<T>();
+          }
+          if (__builtin_amdgcn_ballot_w64(odd)) {
+            frag up, down, ones;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+              const short bits = v[i];
+              const float f = (float)__builtin_bit_cast(T, bits);
+              const bool finite = ((uint32_t)(uint16_t)v[i] & kv_exponent<T>()) != kv_exponent<T>();
+              up[i] = (T)(!finite && !(f < 0.f) ? 1.f : 0.f);
+              down[i] = (T)(!finite && !(f > 0.f) ? 1.f : 0.f);
+              ones[i] = (T)(float)(mine >> (8 * (i >> 2) + (i & 3)) & 1);
+              v[i] = finite ? v[i] : (short)0;
+            }
+            f32x16 none;
+#pragma unroll
+            for (int e = 0; e < 16; ++e) none[e] = 0.f;
+            const f32x16 us = Matrix32<T>::mul(up, ones, none), ds = Matrix32<T>::mul(down, ones, none);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) o[b][e] += (us[e] > 0.f ? INFINITY : 0.f) + (ds[e] > 0.f ? -INFINITY : 0.f);
+          }
+        }
+        o[b] = Matrix32<T>::mul(__builtin_bit_cast(frag, v), p[s], o[b]);
+      }
+  };
+
+  auto run = [&](bool careful) {
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[b][e] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+    int64_t next[2] = {0, 0};
+    if (wave == 0) {
+      look_up(0, next);
+      publish(0, next);
+      look_up(1, next);
+      publish(1, next);
+      look_up(2, next);
+    }
+    __syncthreads();
+    request(0);
+    for (int t = 0; t < n_tiles; ++t) {
+      asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+      __syncthreads();                                            // tile t has landed, and everybody has left tile t - 1
+      if (t + 1 < n_tiles) request(t + 1);
+      if (wave == 0) {
+        publish(t + 2, next);
+        look_up(t + 3, next);
+      }
+      tile_step(t, careful);
+    }
+  };
+  if (n_tiles > 0) {
+    run(false);
+    bool odd = false;
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) odd |= !(fabsf(o[b][e]) <= 3.4e38f);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    if (__syncthreads_or(odd)) {
+      run(true);
+      __syncthreads();
+    }
+  } else {
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) o[b][e] = 0.f;
+    m = -INFINITY;
+    l = 0.f;
+  }
+  l = pair_sum(l);
+  const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
+  // Rows to memory: each wavefront turns its 32 x DH patch in LDS, 16-byte chunks XORed with the row.
+  char *patch = lds + wave * (32 * DH * 2);
+#pragma unroll
+  for (int b = 0; b < DB; ++b)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      // features 32 b + 8 i + 4 lh + 0..3 of row l32
+      s16x4 x;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) x[e] = __builtin_bit_cast(short, kv_round<T>(o[b][4 * i + e] * inv));
+      *(s16x4 *)(patch + l32 * (DH * 2) + (((4 * b + i) ^ (l32 & (CH - 1))) << 4) + lh * 8) = x;
+    }
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll
+  for (int i = 0; i < 32 / RPI; ++i) {
+    const int r = i * RPI + in_row, row = wave_row + r;
+    if (row < rows) {
+      const int tk = row / group, h = kvh * group + row - tk * group;
+      *(s16x8 *)(a.out.p + (first + tk) * a.out.row + h * a.out.head + chunk * 16) = *(const s16x8 *)(patch + r * (DH * 2) + ((chunk ^ (r & (CH - 1))) << 4));
+    }
+  }
+  (void)row_there;
+}
+
+// fp32: one wavefront per query row and head runs through the row's keys once, one key at a time; the lanes share the features.
+template <int DH>
 __global__ __launch_bounds__(256) void kv_attention_kernel(KvAttention a) {
+  typedef float T;
   constexpr int N = DH >= 64 ? DH / 64 : 1;           // features per lane
   const int lane = threadIdx.x & 63;
   const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t row = item / a.n_q_heads;
   const int h = (int)(item % a.n_q_heads), kvh = h / (a.n_q_heads / a.n_kv_heads);
   if (row >= a.batch.n_rows) return;
-  int seq = (int)row;
-  int64_t first = row, end = row + 1;
-  if (a.batch.offsets) {
-    seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, row, lane);
-    if (seq >= a.batch.n_seqs) return;
-    first = a.batch.offsets[seq];
-    end = a.batch.offsets[seq + 1];
-    if (row < first || first < 0 || end > a.batch.n_rows) {
-      if (lane == 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
-      if (row < first || first < 0) return;
-    }
+  const int seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, row, lane);
+  if (seq >= a.batch.n_seqs) return;
+  const int64_t first = a.batch.offsets[seq], end = a.batch.offsets[seq + 1];
+  if (row < first || first < 0 || end > a.batch.n_rows) {
+    if (lane == 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
+    if (row < first || first < 0) return;
   }
   int64_t n, k_first = 0;
   if (a.pages.table) {
@@ -82,17 +409,34 @@ __global__ __launch_bounds__(256) void kv_attention_kernel(KvAttention a) {
   for (int i = 0; i < N; ++i) ((T *)(a.out.p + row * a.out.row + h * a.out.head))[f + i] = kv_round<T>(m == -INFINITY && l == 0.f ? 0.f : o[i] / l);
 }
 
+template <typename T, int DH, bool PAGED> hipError_t launch_flash(const KvAttention &a, hipStream_t stream) {
+  static std::atomic<uint64_t> raised{0};
+  constexpr int kBytes = 4 * KT * DH * 2;                         // two stages of K and V
+  const hipError_t e = raise_lds_limit(reinterpret_cast<const void *>(&kv_flash_kernel<T, DH, PAGED>), kBytes, raised);
+  if (e != hipSuccess) return e;
+  const int64_t slots = a.batch.n_rows * (a.n_q_heads / a.n_kv_heads) / QT + a.batch.n_seqs;
+  kv_flash_kernel<T, DH, PAGED><<<(unsigned)(slots * a.n_kv_heads), 256, kBytes, stream>>>(a);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 hipError_t launch_kv_attention(const KvAttention &a, hipStream_t stream) {
-  const unsigned blocks = (unsigned)((a.batch.n_rows * a.n_q_heads + 3) / 4);
+  if (a.dtype == FLAME_KV_F32) {
+    const unsigned blocks = (unsigned)((a.batch.n_rows * a.n_q_heads + 3) / 4);
+    kv_with_width(a.head_dim, [&](auto width) { kv_attention_kernel<decltype(width)::value><<<blocks, 256, 0, stream>>>(a); });
+    return hipGetLastError();
+  }
+  hipError_t e = hipErrorUnknown;
   kv_with_type(a.dtype, [&](auto t) {
     using T = decltype(t);
-    if (a.head_dim == 32) kv_attention_kernel<T, 32><<<blocks, 256, 0, stream>>>(a);
-    else if (a.head_dim == 64) kv_attention_kernel<T, 64><<<blocks, 256, 0, stream>>>(a);
-    else kv_attention_kernel<T, 128><<<blocks, 256, 0, stream>>>(a);
+    if constexpr (sizeof(T) == 2)
+      kv_with_width(a.head_dim, [&](auto width) {
+        constexpr int DH = decltype(width)::value;
+        e = a.pages.table ? launch_flash<T, DH, true>(a, stream) : launch_flash<T, DH, false>(a, stream);
+      });
   });
-  return hipGetLastError();
+  return e;
 }
 
 }  // namespace flame
