@@ -25,9 +25,10 @@ namespace flame {
 namespace {
 
 constexpr int QT = 128;             // query rows of a workgroup
-constexpr int KT = 64;              // keys of a tile
+// keys of a tile: as many as leave two workgroups on a compute unit
+template <typename T, int DH> constexpr int key_tile() { return DH * sizeof(T) == 512 ? 32 : 64; }
 
-template <typename T> struct Matrix32;
+template <typename T> struct Matrix32;              // (fp32 products are 32x32x2: the third dimension is the lane's half)
 template <> struct Matrix32<bf16_t> {
   typedef bf16x8 frag;
   static __device__ __forceinline__ f32x16 mul(frag x, frag y, f32x16 c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(x, y, c, 0, 0, 0); }
@@ -42,9 +43,11 @@ typedef short s16x8 __attribute__((ext_vector_type(8)));
 
 template <typename T, int DH, bool PAGED>
 __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
-  typedef typename Matrix32<T>::frag frag;
-  constexpr int KS = DH / 16, DB = DH / 32, CH = DH / 8;          // k-steps, feature blocks, 16-byte chunks of a row
-  constexpr int TILE = KT * DH * 2;                               // bytes of a K or V tile
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int KT = key_tile<T, DH>(), NJ = KT / 32;             // keys of a tile, 32-key blocks of it
+  constexpr int RB = DH * (int)sizeof(T), CH = RB / 16;           // bytes of a row, and 16-byte chunks
+  constexpr int KS = RB / 32, DB = DH / 32;                       // steps of 32 bytes along a row (16 per lane), feature blocks
+  constexpr int TILE = KT * RB;                                   // bytes of a K or V tile
   constexpr int STAGE = 2 * TILE;
   constexpr int RPI = 64 / CH, NI = TILE / 1024 / 4;              // rows of a 1 KB request, requests of a wavefront per tile of K or V
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -103,13 +106,11 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
   const bool active = wave_row < rows;
   const int my_row = active ? min(wave_row + l32, rows - 1) : row0, token = my_row / group, head = kvh * group + my_row - token * group;
   const int sees = seen_by(my_row), wave_least = active ? seen_by(wave_row) : 0, wave_most = active ? seen_by(min(wave_row + 31, rows - 1)) : 0;
-  const bool row_there = active && wave_row + l32 < rows;
 
   typedef __attribute__((address_space(1))) const void gvoid;
   typedef __attribute__((address_space(3))) void lvoid;
   auto look_up = [&](int t, int64_t (&to)[2]) {                   // of key `lane` of tile t; -1: none
-    const int key = t * KT + lane;
-    const int near = min(key, n - 1);
+    const int near = min(t * KT + lane, n - 1);
     if (PAGED) {
       to[0] = kv_token_offset(a.pages, table, (uint32_t)near);
     } else {
@@ -119,12 +120,18 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
   };
   auto publish = [&](int t, const int64_t (&from)[2]) {
     const int64_t k_at = from[0];
-    if (PAGED && k_at < 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_PAGE);
-    at_s[t % 3][0][lane] = max(k_at, (int64_t)0);
-    if (!PAGED) at_s[t % 3][PAGED ? 0 : 1][lane] = from[1];
-    const uint64_t there = __builtin_amdgcn_ballot_w64((!PAGED || k_at >= 0) && t * KT + lane < n);
+    const bool mine = lane < KT;
+    if (PAGED && mine && k_at < 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_PAGE);
+    if (mine) {
+      at_s[t % 3][0][lane] = max(k_at, (int64_t)0);
+      if (!PAGED) at_s[t % 3][PAGED ? 0 : 1][lane] = from[1];
+    }
+    const uint64_t there = __builtin_amdgcn_ballot_w64(!mine || ((!PAGED || k_at >= 0) && t * KT + lane < n));
     if (lane == 0) there_s[t % 3] = there;
   };
+  // swizzle: what the chunk index of a row is XORed with (fp32 values are read a row at a time, side by side: no need)
+  auto k_key_of = [](int r) { return RB >= 256 ? r & 15 : RB == 128 ? r >> 1 & 7 : r >> 2 & 3; };
+  auto v_key_of = [](int r) { return F32 || RB == 64 ? 0 : RB == 256 ? 4 * (r & 3) : 4 * (r >> 1 & 1); };
   // Request j of a tile is rows j RPI..; lane p brings the chunk that belongs at byte 16 p of it.
   const int in_row = lane / CH, chunk = lane % CH;
   auto request = [&](int t) {
@@ -133,27 +140,26 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const int j = wave + 4 * i, r = j * RPI + in_row;
-      const int kc = DH == 128 ? chunk ^ (r & 15) : DH == 64 ? chunk ^ (r >> 1 & 7) : chunk ^ (r >> 2 & 3);
-      const int vc = DH == 128 ? chunk ^ (4 * (r & 3)) : DH == 64 ? chunk ^ (4 * (r >> 1 & 1)) : chunk;
+      const int kc = chunk ^ k_key_of(r), vc = chunk ^ v_key_of(r);
       __builtin_amdgcn_global_load_lds((gvoid *)(kp + ka[r] + kc * 16), (lvoid *)(stage + j * 1024), 16, 0, 0);
       __builtin_amdgcn_global_load_lds((gvoid *)(vp + va[r] + vc * 16), (lvoid *)(stage + TILE + j * 1024), 16, 0, 0);
     }
   };
 
-  frag fq[KS];
+  typedef uint32_t word4 __attribute__((ext_vector_type(4)));
+  word4 fq[KS];
   {
     const char *q = a.q.p + (first + token) * a.q.row + head * a.q.head;
 #pragma unroll
-    for (int s = 0; s < KS; ++s) fq[s] = *(const frag *)(q + s * 32 + lh * 16);
+    for (int s = 0; s < KS; ++s) fq[s] = *(const word4 *)(q + s * 32 + lh * 16);
   }
   const float scale = a.scale * kLog2e;
   // K: row l32 (+ 32) of the tile, chunk 2 s + lh
-  const int k_key = DH == 128 ? l32 & 15 : DH == 64 ? l32 >> 1 & 7 : l32 >> 2 & 3;
-  const int ka0 = l32 * (DH * 2) + ((k_key ^ lh) << 4);           // ^ (s << 5)
+  const int ka0 = l32 * RB + ((k_key_of(l32) ^ lh) << 4);         // ^ (s << 5)
   // V: lane l of a transposing read addresses key 4 lh + (l % 16) / 4, features 16 (l / 16 % 2) + 4 (l % 4), and gets feature l % 32 of four keys
-  const int v_row = 4 * lh + (lane >> 2 & 3);
-  const int v_key = DH == 128 ? 4 * (v_row & 3) : DH == 64 ? 4 * (v_row >> 1 & 1) : 0;   // (rows 8 further have the same)
-  const int va0 = v_row * (DH * 2) + ((((lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ v_key) << 4) + (lane & 1) * 8;   // ^ (b << 6), + 8 rows each
+  // (rows 8 and 16 further have the same swizzle).  fp32: lane l reads features DB (l % 32).. of key 4 lh
+  const int v_row = 4 * lh + (F32 ? 0 : lane >> 2 & 3);
+  const int va0 = v_row * RB + (F32 ? l32 * DB * 4 : ((((lane >> 4 & 1) * 2 + (lane >> 1 & 1)) ^ v_key_of(v_row)) << 4) + (lane & 1) * 8);   // ^ (b << 6), + 8 rows each
 
   f32x16 o[DB];
   float m, l;
@@ -164,24 +170,30 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
     const uint64_t there = there_s[t % 3];
     const uint32_t there_lo = __builtin_amdgcn_readfirstlane((int)there), there_hi = __builtin_amdgcn_readfirstlane((int)(there >> 32));
     const bool masked = k0 + KT > wave_least || (there_lo & there_hi) != 0xffffffffu;
-    f32x16 z[2];
+    f32x16 z[NJ];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) z[j][e] = 0.f;
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const frag fk = *(const frag *)(sk + j * (32 * DH * 2) + (ka0 ^ (s << 5)));
-        z[j] = Matrix32<T>::mul(fk, fq[s], z[j]);
+      for (int j = 0; j < NJ; ++j) {
+        const word4 fk = *(const word4 *)(sk + j * (32 * RB) + (ka0 ^ (s << 5)));
+        if constexpr (F32) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) z[j] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(fk[i]), __uint_as_float(fq[s][i]), z[j], 0, 0, 0);
+        } else {
+          typedef typename Matrix32<T>::frag frag;
+          z[j] = Matrix32<T>::mul(__builtin_bit_cast(frag, fk), __builtin_bit_cast(frag, fq[s]), z[j]);
+        }
       }
     // element e of block j: key 32 j + 8 (e / 4) + 4 lh + e % 4
     uint32_t seen[2] = {~0u, ~0u};                                // of the keys of a block, by their place in it
     if (masked) {
       const int left = sees - k0;
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
+      for (int j = 0; j < NJ; ++j) {
         const int here = min(32, max(0, left - 32 * j));
         seen[j] = (j ? there_hi : there_lo) & (here == 32 ? ~0u : (1u << here) - 1);
         const uint32_t mine = seen[j] >> (4 * lh);
@@ -190,16 +202,15 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
       }
     }
     auto max3 = [](float x, float y, float w) { return fmaxf(fmaxf(x, y), w); };
-    float l1[10], l2[4];
+    float tops[NJ];                                               // as a tree of three-input maxima
 #pragma unroll
-    for (int k = 0; k < 10; ++k) {
-      const int e = 3 * k;
-      l1[k] = max3(z[e >> 4][e & 15], z[(e + 1) >> 4][(e + 1) & 15], z[(e + 2) >> 4][(e + 2) & 15]);
+    for (int j = 0; j < NJ; ++j) {
+      float x[5];
+#pragma unroll
+      for (int k = 0; k < 5; ++k) x[k] = max3(z[j][3 * k], z[j][3 * k + 1], z[j][3 * k + 2]);
+      tops[j] = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], z[j][15]), j ? tops[0] : -INFINITY);
     }
-#pragma unroll
-    for (int k = 0; k < 3; ++k) l2[k] = max3(l1[3 * k], l1[3 * k + 1], l1[3 * k + 2]);
-    l2[3] = max3(l1[9], z[1][14], z[1][15]);
-    const float top = pair_max(fmaxf(max3(l2[0], l2[1], l2[2]), l2[3])) * scale;
+    const float top = pair_max(tops[NJ - 1]) * scale;
     const float m_new = fmaxf(m, top);
     if (__builtin_amdgcn_ballot_w64(m_new != m)) {
       const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
@@ -211,8 +222,48 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
       m = m_new;
     }
     const float nm = m == -INFINITY ? 0.f : -m;                   // (nothing seen yet: all weights are 2^-inf)
-    frag p[4];
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
+    if constexpr (F32) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          z[j][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], scale, nm));
+          sum[e & 3] += z[j][e];
+        }
+      l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+#pragma unroll
+      for (int j = 0; j < NJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          const int bit = 8 * (e >> 2) + (e & 3);
+          struct alignas(4 * DB) Values { float f[DB]; } v = *(const Values *)(sv + (32 * j + bit) * RB + va0);
+          if (careful && masked) {
+            // Values of keys that do not count are zeros; infinite and NaN ones are taken out and added to the rows that see them.
+            const bool counts = (j ? there_hi : there_lo) >> (4 * lh + bit) & 1;
+            const float one = (float)(seen[j] >> (4 * lh + bit) & 1);
+#pragma unroll
+            for (int b = 0; b < DB; ++b) {
+              const float f = counts ? v.f[b] : 0.f;
+              const bool finite = fabsf(f) <= 3.4028235e38f;
+              v.f[b] = finite ? f : 0.f;
+              if (__builtin_amdgcn_ballot_w64(!finite)) {
+                f32x16 none;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) none[i] = 0.f;
+                const f32x16 us = __builtin_amdgcn_mfma_f32_32x32x2f32(!finite && !(f < 0.f) ? 1.f : 0.f, one, none, 0, 0, 0);
+                const f32x16 ds = __builtin_amdgcn_mfma_f32_32x32x2f32(!finite && !(f > 0.f) ? 1.f : 0.f, one, none, 0, 0, 0);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[b][i] += (us[i] > 0.f ? INFINITY : 0.f) + (ds[i] > 0.f ? -INFINITY : 0.f);
+              }
+            }
+          }
+#pragma unroll
+          for (int b = 0; b < DB; ++b) o[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(v.f[b], z[j][e], o[b], 0, 0, 0);
+        }
+    } else {
+    typedef typename Matrix32<T>::frag frag;
+    frag p[4];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -227,8 +278,8 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
         typedef __attribute__((address_space(3))) s16x4 *ltr;
-        const char *va = sv + s * (16 * DH * 2) + (va0 ^ (b << 6));
-        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr)va), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr)(va + 8 * DH * 2));
+        const char *va = sv + s * (16 * RB) + (va0 ^ (b << 6));
+        const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr)va), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr)(va + 8 * RB));
         s16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
         if (careful && masked) {
           // Values of keys that do not count are zeros; infinite and NaN ones are taken out and added to the rows that see them.
@@ -262,6 +313,7 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
         }
         o[b] = Matrix32<T>::mul(__builtin_bit_cast(frag, v), p[s], o[b]);
       }
+    }
   };
 
   auto run = [&](bool careful) {
@@ -315,103 +367,44 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
   l = pair_sum(l);
   const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
   // Rows to memory: each wavefront turns its 32 x DH patch in LDS, 16-byte chunks XORed with the row.
-  char *patch = lds + wave * (32 * DH * 2);
+  char *patch = lds + wave * (32 * RB);
+  static_assert(4 * 32 * RB <= 2 * STAGE, "the patches fit in the stages");
+  if constexpr (F32) {
 #pragma unroll
-  for (int b = 0; b < DB; ++b)
+    for (int e = 0; e < 16; ++e) {
+      // features DB m..DB m + DB - 1 of row l32, m = 8 (e / 4) + 4 lh + e % 4
+      const int at = (8 * (e >> 2) + 4 * lh + (e & 3)) * DB * 4;
+      struct alignas(4 * DB) Values { float f[DB]; } x;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      // features 32 b + 8 i + 4 lh + 0..3 of row l32
-      s16x4 x;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[e] = __builtin_bit_cast(short, kv_round<T>(o[b][4 * i + e] * inv));
-      *(s16x4 *)(patch + l32 * (DH * 2) + (((4 * b + i) ^ (l32 & (CH - 1))) << 4) + lh * 8) = x;
+      for (int b = 0; b < DB; ++b) x.f[b] = o[b][e] * inv;
+      *(Values *)(patch + l32 * RB + (((at >> 4) ^ (l32 & (CH - 1))) << 4) + (at & 15)) = x;
     }
+  } else {
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        // features 32 b + 8 i + 4 lh + 0..3 of row l32
+        s16x4 x;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] = __builtin_bit_cast(short, kv_round<T>(o[b][4 * i + e] * inv));
+        *(s16x4 *)(patch + l32 * RB + (((4 * b + i) ^ (l32 & (CH - 1))) << 4) + lh * 8) = x;
+      }
+  }
   __builtin_amdgcn_wave_barrier();
 #pragma unroll
   for (int i = 0; i < 32 / RPI; ++i) {
     const int r = i * RPI + in_row, row = wave_row + r;
     if (row < rows) {
       const int tk = row / group, h = kvh * group + row - tk * group;
-      *(s16x8 *)(a.out.p + (first + tk) * a.out.row + h * a.out.head + chunk * 16) = *(const s16x8 *)(patch + r * (DH * 2) + ((chunk ^ (r & (CH - 1))) << 4));
+      *(word4 *)(a.out.p + (first + tk) * a.out.row + h * a.out.head + chunk * 16) = *(const word4 *)(patch + r * RB + ((chunk ^ (r & (CH - 1))) << 4));
     }
   }
-  (void)row_there;
-}
-
-// fp32: one wavefront per query row and head runs through the row's keys once, one key at a time; the lanes share the features.
-template <int DH>
-__global__ __launch_bounds__(256) void kv_attention_kernel(KvAttention a) {
-  typedef float T;
-  constexpr int N = DH >= 64 ? DH / 64 : 1;           // features per lane
-  const int lane = threadIdx.x & 63;
-  const int64_t item = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t row = item / a.n_q_heads;
-  const int h = (int)(item % a.n_q_heads), kvh = h / (a.n_q_heads / a.n_kv_heads);
-  if (row >= a.batch.n_rows) return;
-  const int seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, row, lane);
-  if (seq >= a.batch.n_seqs) return;
-  const int64_t first = a.batch.offsets[seq], end = a.batch.offsets[seq + 1];
-  if (row < first || first < 0 || end > a.batch.n_rows) {
-    if (lane == 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
-    if (row < first || first < 0) return;
-  }
-  int64_t n, k_first = 0;
-  if (a.pages.table) {
-    n = kv_clip_length(a.batch.kv_lens[seq], a.pages.capacity, a.batch.faults, lane == 0);
-  } else {
-    const int32_t *ko = a.k_offsets ? a.k_offsets : a.batch.offsets;
-    k_first = ko[seq];
-    n = ko[seq + 1] - k_first;
-    if (k_first < 0 || n < 0 || k_first + n > a.n_keys) {
-      if (lane == 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
-      n = k_first < 0 ? 0 : max((int64_t)0, min(n, a.n_keys - k_first));
-    }
-  }
-  const int64_t seen = n - end + row + 1;             // keys that the row sees
-  const int f = lane * N;
-  const bool has = f < DH;
-  float q[N], o[N];
-#pragma unroll
-  for (int i = 0; i < N; ++i) {
-    q[i] = has ? (float)((const T *)(a.q.p + row * a.q.row + h * a.q.head))[f + i] : 0.f;
-    o[i] = 0.f;
-  }
-  const float scale = a.scale * kLog2e;
-  float m = -INFINITY, l = 0.f;
-  const int32_t *table = a.pages.table ? a.pages.table + seq * a.pages.table_stride : nullptr;
-  for (int64_t c = 0; c < seen; ++c) {
-    const char *kp, *vp;
-    if (table) {
-      const int64_t at = kv_token_offset(a.pages, table, (uint32_t)c);
-      if (at < 0) {
-        if (lane == 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_PAGE);
-        continue;
-      }
-      kp = a.pages.k + at + kvh * a.pages.head;
-      vp = a.pages.v + at + kvh * a.pages.head;
-    } else {
-      kp = a.k.p + (k_first + c) * a.k.row + kvh * a.k.head;
-      vp = a.v.p + (k_first + c) * a.v.row + kvh * a.v.head;
-    }
-    float s = 0.f;
-#pragma unroll
-    for (int i = 0; i < N; ++i) s += has ? q[i] * (float)((const T *)kp)[f + i] : 0.f;
-    s = wave_sum(s) * scale;
-    const float m_new = fmaxf(m, s);
-    const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_new), w = s == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(s - m_new);
-    l = l * keep + w;
-    m = m_new;
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = o[i] * keep + w * (has ? (float)((const T *)vp)[f + i] : 0.f);
-  }
-  if (!has) return;
-#pragma unroll
-  for (int i = 0; i < N; ++i) ((T *)(a.out.p + row * a.out.row + h * a.out.head))[f + i] = kv_round<T>(m == -INFINITY && l == 0.f ? 0.f : o[i] / l);
 }
 
 template <typename T, int DH, bool PAGED> hipError_t launch_flash(const KvAttention &a, hipStream_t stream) {
   static std::atomic<uint64_t> raised{0};
-  constexpr int kBytes = 4 * KT * DH * 2;                         // two stages of K and V
+  constexpr int kBytes = 4 * key_tile<T, DH>() * DH * (int)sizeof(T);                         // two stages of K and V
   const hipError_t e = raise_lds_limit(reinterpret_cast<const void *>(&kv_flash_kernel<T, DH, PAGED>), kBytes, raised);
   if (e != hipSuccess) return e;
   const int64_t slots = a.batch.n_rows * (a.n_q_heads / a.n_kv_heads) / QT + a.batch.n_seqs;
@@ -422,19 +415,13 @@ template <typename T, int DH, bool PAGED> hipError_t launch_flash(const KvAttent
 }  // namespace
 
 hipError_t launch_kv_attention(const KvAttention &a, hipStream_t stream) {
-  if (a.dtype == FLAME_KV_F32) {
-    const unsigned blocks = (unsigned)((a.batch.n_rows * a.n_q_heads + 3) / 4);
-    kv_with_width(a.head_dim, [&](auto width) { kv_attention_kernel<decltype(width)::value><<<blocks, 256, 0, stream>>>(a); });
-    return hipGetLastError();
-  }
   hipError_t e = hipErrorUnknown;
   kv_with_type(a.dtype, [&](auto t) {
     using T = decltype(t);
-    if constexpr (sizeof(T) == 2)
-      kv_with_width(a.head_dim, [&](auto width) {
-        constexpr int DH = decltype(width)::value;
-        e = a.pages.table ? launch_flash<T, DH, true>(a, stream) : launch_flash<T, DH, false>(a, stream);
-      });
+    kv_with_width(a.head_dim, [&](auto width) {
+      constexpr int DH = decltype(width)::value;
+      e = a.pages.table ? launch_flash<T, DH, true>(a, stream) : launch_flash<T, DH, false>(a, stream);
+    });
   });
   return e;
 }
