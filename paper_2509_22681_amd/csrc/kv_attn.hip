@@ -41,6 +41,30 @@ template <> struct Matrix32<half_t> {
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef short s16x8 __attribute__((ext_vector_type(8)));
 
+// Values of 16 keys, transposed: the fragments of all feature blocks, two reads each.  The builtin for this instruction makes the compiler wait for the LDS-DMA
+// loads in flight, which are the next tile's; hence assembly, that waits for its own reads before it ends.
+template <int DB, int RB, int AT> __device__ __forceinline__ void read_values(uint32_t stage, uint32_t at, s16x4 (&v)[DB][2]) {
+#define READ(o, a, n) "ds_read_b64_tr_b16 " o ", " a " offset:" n "\n\t"
+  if constexpr (DB == 4) {
+    asm volatile(READ("%0", "%8", "%12") READ("%1", "%8", "%13") READ("%2", "%9", "%12") READ("%3", "%9", "%13")
+                 READ("%4", "%10", "%12") READ("%5", "%10", "%13") READ("%6", "%11", "%12") READ("%7", "%11", "%13") "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(v[0][0]), "=&v"(v[0][1]), "=&v"(v[1][0]), "=&v"(v[1][1]), "=&v"(v[2][0]), "=&v"(v[2][1]), "=&v"(v[3][0]), "=&v"(v[3][1])
+                 : "v"(stage + at), "v"(stage + (at ^ 64)), "v"(stage + (at ^ 128)), "v"(stage + (at ^ 192)), "n"(AT), "n"(AT + 8 * RB)
+                 : "memory");
+  } else if constexpr (DB == 2) {
+    asm volatile(READ("%0", "%4", "%6") READ("%1", "%4", "%7") READ("%2", "%5", "%6") READ("%3", "%5", "%7") "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(v[0][0]), "=&v"(v[0][1]), "=&v"(v[1][0]), "=&v"(v[1][1])
+                 : "v"(stage + at), "v"(stage + (at ^ 64)), "n"(AT), "n"(AT + 8 * RB)
+                 : "memory");
+  } else {
+    asm volatile(READ("%0", "%2", "%3") READ("%1", "%2", "%4") "s_waitcnt lgkmcnt(0)"
+                 : "=&v"(v[0][0]), "=&v"(v[0][1])
+                 : "v"(stage + at), "n"(AT), "n"(AT + 8 * RB)
+                 : "memory");
+  }
+#undef READ
+}
+
 template <typename T, int DH, bool PAGED>
 __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
   constexpr bool F32 = sizeof(T) == 4;
@@ -163,7 +187,8 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
 
   f32x16 o[DB];
   float m, l;
-  auto tile_step = [&](int t, bool careful) {
+  auto tile_step = [&](int t, auto careful_c) __attribute__((always_inline)) {
+    constexpr bool careful = decltype(careful_c)::value;
     const char *sk = lds + (t & 1) * STAGE, *sv = sk + TILE;
     const int k0 = t * KT;
     if (k0 >= wave_most) return;
@@ -211,15 +236,17 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
       tops[j] = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], z[j][15]), j ? tops[0] : -INFINITY);
     }
     const float top = pair_max(tops[NJ - 1]) * scale;
-    const float m_new = fmaxf(m, top);
-    if (__builtin_amdgcn_ballot_w64(m_new != m)) {
-      const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_new);
+    // The exponent's reference of a row moves only when its largest logit has left it 2^8 behind: weights stay below 2^8, and rescaling is rare.  Each row goes by its own logits,
+    // and one that does not move is multiplied by exactly 1: no row's bits depend on the others.
+    const bool moves = top > (m == -INFINITY ? m : m + 8.f);
+    if (__builtin_amdgcn_ballot_w64(moves)) {
+      const float keep = moves ? __builtin_amdgcn_exp2f(m - top) : 1.f;
       l *= keep;
 #pragma unroll
       for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[b][e] *= keep;
-      m = m_new;
+      m = moves ? top : m;
     }
     const float nm = m == -INFINITY ? 0.f : -m;                   // (nothing seen yet: all weights are 2^-inf)
     float sum[4] = {0.f, 0.f, 0.f, 0.f};
@@ -238,7 +265,7 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
         for (int e = 0; e < 16; ++e) {
           const int bit = 8 * (e >> 2) + (e & 3);
           struct alignas(4 * DB) Values { float f[DB]; } v = *(const Values *)(sv + (32 * j + bit) * RB + va0);
-          if (careful && masked) {
+          if constexpr (careful) {
             // Values of keys that do not count are zeros; infinite and NaN ones are taken out and added to the rows that see them.
             const bool counts = (j ? there_hi : there_lo) >> (4 * lh + bit) & 1;
             const float one = (float)(seen[j] >> (4 * lh + bit) & 1);
@@ -273,6 +300,24 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
         p[2 * j + (e >> 3)][e & 7] = (T)w;
       }
     l += (sum[0] + sum[1]) + (sum[2] + sum[3]);
+    if constexpr (!careful) {
+      typedef __attribute__((address_space(3))) const char *lchar;
+      const uint32_t at = (uint32_t)(uintptr_t)(lchar)sv;
+      auto products = [&](auto step) __attribute__((always_inline)) {
+        constexpr int S = decltype(step)::value;
+        s16x4 v[DB][2];
+        read_values<DB, RB, S * 16 * RB>(at, va0, v);
+#pragma unroll
+        for (int b = 0; b < DB; ++b) {
+          const s16x8 x = __builtin_shufflevector(v[b][0], v[b][1], 0, 1, 2, 3, 4, 5, 6, 7);
+          o[b] = Matrix32<T>::mul(__builtin_bit_cast(frag, x), p[S], o[b]);
+        }
+      };
+      products(std::integral_constant<int, 0>{});
+      products(std::integral_constant<int, 1>{});
+      products(std::integral_constant<int, 2>{});
+      products(std::integral_constant<int, 3>{});
+    } else {
 #pragma unroll
     for (int s = 0; s < 4; ++s)
 #pragma unroll
@@ -281,7 +326,7 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
         const char *va = sv + s * (16 * RB) + (va0 ^ (b << 6));
         const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr)va), y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((ltr)(va + 8 * RB));
         s16x8 v = __builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7);
-        if (careful && masked) {
+        {
           // Values of keys that do not count are zeros; infinite and NaN ones are taken out and added to the rows that see them.
           const uint32_t keys = (s >> 1 ? there_hi : there_lo) >> (16 * (s & 1) + 4 * lh), mine = seen[s >> 1] >> (16 * (s & 1) + 4 * lh);
           bool odd = false;
@@ -314,9 +359,10 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
         o[b] = Matrix32<T>::mul(__builtin_bit_cast(frag, v), p[s], o[b]);
       }
     }
+    }
   };
 
-  auto run = [&](bool careful) {
+  auto run = [&](auto careful) __attribute__((always_inline)) {
 #pragma unroll
     for (int b = 0; b < DB; ++b)
 #pragma unroll
@@ -345,7 +391,7 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
     }
   };
   if (n_tiles > 0) {
-    run(false);
+    run(std::false_type{});
     bool odd = false;
 #pragma unroll
     for (int b = 0; b < DB; ++b)
@@ -353,7 +399,7 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
       for (int e = 0; e < 16; ++e) odd |= !(fabsf(o[b][e]) <= 3.4e38f);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
     if (__syncthreads_or(odd)) {
-      run(true);
+      run(std::true_type{});
       __syncthreads();
     }
   } else {
