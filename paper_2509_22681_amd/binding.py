@@ -144,6 +144,7 @@ _lib.flame_climber_last_error.restype = C.c_char_p
 
 
 class flame_kv_config(C.Structure):
+    torch_dtype = None          # of the tensors (make_kv_config sets it)
     _fields_ = [("dtype", C.c_int32), ("n_q_heads", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("scale", C.c_float)]
 
 
@@ -563,44 +564,50 @@ def _kv_check(rc: int):
 
 def make_kv_config(dtype, n_q_heads, n_kv_heads, head_dim, scale=0.0) -> flame_kv_config:
     """dtype: "f32", "bf16" or "f16"; scale of the logits, 0 for 1 / sqrt(head_dim)."""
-    return flame_kv_config(_KV_DTYPES.get(dtype, dtype), n_q_heads, n_kv_heads, head_dim, scale)
+    cfg = flame_kv_config(_KV_DTYPES.get(dtype, dtype), n_q_heads, n_kv_heads, head_dim, scale)
+    cfg.torch_dtype = _KV_TORCH[cfg.dtype] if 0 <= cfg.dtype < 3 else None
+    return cfg
 
 
-def _kv_torch_dtype(cfg):
-    if not 0 <= cfg.dtype < 3:
-        raise ValueError("dtype must be f32, bf16 or f16")
-    return _KV_TORCH[cfg.dtype]
-
-
-def _kv_rows(cfg, t, heads: int, what: str, written: bool = False) -> flame_kv_rows:
+# A call of a few new tokens takes a few microseconds on the GPU, so these checks count: each attribute of a tensor is asked for once.
+def _kv_rows(cfg, t, heads: int, dev: int, what: str, written: bool = False):
     rows, h, dim = t.shape
     sr, sh, sd = t.stride()
-    if h != heads or dim != cfg.head_dim or t.dtype is not _kv_torch_dtype(cfg):
-        raise ValueError(f"{what} must be [rows, {heads}, {cfg.head_dim}] of {_kv_torch_dtype(cfg)}")
-    if rows and t.get_device() != torch.cuda.current_device():
+    if h != heads or dim != cfg.head_dim or t.dtype is not cfg.torch_dtype:
+        raise ValueError(f"{what} must be [rows, {heads}, {cfg.head_dim}] of {cfg.torch_dtype}")
+    if t.get_device() != dev:
         raise ValueError(f"{what} is not on the current device")
     if sd != 1:
         raise ValueError(f"{what}: the features of a head must lie side by side")
+    # a stride of a dimension of one is never used, whatever torch says it is
+    if rows < 2:
+        sr = 0
+    if h == 1:
+        sh = 0
     if written and ((sr == 0 and rows > 1) or (sh == 0 and h > 1)):
         raise ValueError(f"{what} is written and must not be an expanded tensor")
-    # a stride of a dimension of one is never used, whatever torch says it is
-    return flame_kv_rows(t.data_ptr(), sr if rows > 1 else 0, sh if h > 1 else 0)
+    return C.byref(flame_kv_rows(t.data_ptr(), sr, sh))
 
 
-def _kv_ints(t, n: int, what: str) -> int:
-    if t.dtype is not torch.int32 or t.dim() != 1 or t.shape[0] < n or not t.is_contiguous():
+def _kv_ints(t, n: int, dev: int, what: str) -> int:
+    if t.dtype is not torch.int32 or t.dim() != 1 or t.numel() < n or not t.is_contiguous():
         raise ValueError(f"{what} must be a contiguous int32 tensor of {n} entries")
-    if t.get_device() != torch.cuda.current_device():
+    if t.get_device() != dev:
         raise ValueError(f"{what} is not on the current device")
     return t.data_ptr()
 
 
-def _kv_workspace(workspace):
+def _kv_workspace(workspace, dev: int):
     if workspace is None:
         return None, 0
-    if not workspace.is_contiguous() or workspace.get_device() != torch.cuda.current_device():
+    if not workspace.is_contiguous() or workspace.get_device() != dev:
         raise ValueError("the workspace must be contiguous and on the current device")
-    return _ptr(workspace), workspace.numel() * workspace.element_size()
+    return workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def _kv_stream(stream, dev: int) -> int:
+    # (the number alone: building torch's stream object takes longer than the rest of a call)
+    return torch._C._cuda_getCurrentRawStream(dev) if stream is None else getattr(stream, "cuda_stream", stream)
 
 
 def pack_kv_cache(cfg: flame_kv_config, k_pool, v_pool, page_table) -> flame_kv_cache:
@@ -608,8 +615,8 @@ def pack_kv_cache(cfg: flame_kv_config, k_pool, v_pool, page_table) -> flame_kv_
     laid out [n_pages, n_kv_heads, page_size, head_dim] comes transposed); page_table: device int32 [n_seqs, pages_per_seq].  The struct keeps
     the tensors alive; their contents may change."""
     n_pages, page_size, heads, dim = k_pool.shape
-    if heads != cfg.n_kv_heads or dim != cfg.head_dim or k_pool.dtype is not _kv_torch_dtype(cfg):
-        raise ValueError(f"k_pool must be [n_pages, page_size, {cfg.n_kv_heads}, {cfg.head_dim}] of {_kv_torch_dtype(cfg)}")
+    if heads != cfg.n_kv_heads or dim != cfg.head_dim or k_pool.dtype is not cfg.torch_dtype:
+        raise ValueError(f"k_pool must be [n_pages, page_size, {cfg.n_kv_heads}, {cfg.head_dim}] of {cfg.torch_dtype}")
     if v_pool.shape != k_pool.shape or v_pool.dtype is not k_pool.dtype or v_pool.device != k_pool.device:
         raise ValueError("v_pool must be like k_pool")
     if page_table.dtype is not torch.int32 or page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
@@ -629,12 +636,12 @@ def pack_kv_cache(cfg: flame_kv_config, k_pool, v_pool, page_table) -> flame_kv_
     return c
 
 
-def _kv_cache_for(cfg, cache, n_seqs: int):
+def _kv_cache_for(cfg, cache, n_seqs: int, dev: int):
     if cache.shape != (cfg.dtype, cfg.n_kv_heads, cfg.head_dim):
         raise ValueError("the cache was packed for another configuration")
     if cache.n_seqs < n_seqs:
         raise ValueError("the page table has fewer rows than there are sequences")
-    if cache.device != torch.cuda.current_device():
+    if cache.device != dev:
         raise ValueError("the cache is not on the current device")
     return C.byref(cache)
 
@@ -663,27 +670,25 @@ def flame_kv_workspace_bytes(cfg: flame_kv_config, n_seqs: int, n_tokens: Option
 def flame_kv_append(cfg, cache, k, v, offsets, kv_lens, q=None, q_out=None, rotation=None, faults=None, stream=None) -> None:
     """k, v: device rows [n_tokens, n_kv_heads, head_dim]; offsets [n_seqs + 1] and kv_lens [n_seqs] (with the new tokens): device int32;
     q, q_out: rows [n_tokens, n_q_heads, head_dim]; rotation: make_kv_rotation or None; faults: device int32 [1] or None."""
-    n_seqs, n = kv_lens.shape[0], k.shape[0]
-    if v.shape[0] != n or (q is not None and (q.shape[0] != n or q_out is None or q_out.shape[0] != n)) or (q is None and q_out is not None):
+    n_seqs, n, dev = len(kv_lens), len(k), torch.cuda.current_device()
+    if len(v) != n or (q is None) != (q_out is None) or (q is not None and not len(q) == len(q_out) == n):
         raise ValueError("k, v, q and q_out must have the same rows, and q comes with q_out")
-    qr = qo = None
-    if q is not None:
-        qr, qo = C.byref(_kv_rows(cfg, q, cfg.n_q_heads, "q")), C.byref(_kv_rows(cfg, q_out, cfg.n_q_heads, "q_out", True))
-    rc = _lib.flame_kv_append(C.byref(cfg), _kv_cache_for(cfg, cache, n_seqs), C.byref(_kv_rows(cfg, k, cfg.n_kv_heads, "k")), C.byref(_kv_rows(cfg, v, cfg.n_kv_heads, "v")),
-                              qr, qo, C.byref(rotation) if rotation is not None else None, _kv_ints(offsets, n_seqs + 1, "offsets"), _kv_ints(kv_lens, n_seqs, "kv_lens"),
-                              n_seqs, n, None if faults is None else _kv_ints(faults, 1, "faults"), _stream_ptr(stream))
+    rc = _lib.flame_kv_append(cfg, _kv_cache_for(cfg, cache, n_seqs, dev), _kv_rows(cfg, k, cfg.n_kv_heads, dev, "k"), _kv_rows(cfg, v, cfg.n_kv_heads, dev, "v"),
+                              None if q is None else _kv_rows(cfg, q, cfg.n_q_heads, dev, "q"), None if q is None else _kv_rows(cfg, q_out, cfg.n_q_heads, dev, "q_out", True),
+                              rotation, _kv_ints(offsets, n_seqs + 1, dev, "offsets"), _kv_ints(kv_lens, n_seqs, dev, "kv_lens"), n_seqs, n,
+                              None if faults is None else _kv_ints(faults, 1, dev, "faults"), _kv_stream(stream, dev))
     if rc:
         _kv_check(rc)
 
 
 def flame_kv_prompt(cfg, q, k, v, q_offsets, out, k_offsets=None, faults=None, stream=None) -> None:
     """q, out: device rows [n_tokens, n_q_heads, head_dim]; k, v: [n_keys, n_kv_heads, head_dim]; offsets: device int32 [n_seqs + 1]."""
-    n_seqs, n, n_keys = q_offsets.shape[0] - 1, q.shape[0], k.shape[0]
-    if out.shape[0] != n or v.shape[0] != n_keys:
+    n_seqs, n, n_keys, dev = len(q_offsets) - 1, len(q), len(k), torch.cuda.current_device()
+    if len(out) != n or len(v) != n_keys:
         raise ValueError("out must have the rows of q, and v those of k")
-    rc = _lib.flame_kv_prompt(C.byref(cfg), C.byref(_kv_rows(cfg, q, cfg.n_q_heads, "q")), C.byref(_kv_rows(cfg, k, cfg.n_kv_heads, "k")), C.byref(_kv_rows(cfg, v, cfg.n_kv_heads, "v")),
-                              _kv_ints(q_offsets, n_seqs + 1, "q_offsets"), None if k_offsets is None else _kv_ints(k_offsets, n_seqs + 1, "k_offsets"), n_seqs, n, n_keys,
-                              C.byref(_kv_rows(cfg, out, cfg.n_q_heads, "out", True)), None if faults is None else _kv_ints(faults, 1, "faults"), _stream_ptr(stream))
+    rc = _lib.flame_kv_prompt(cfg, _kv_rows(cfg, q, cfg.n_q_heads, dev, "q"), _kv_rows(cfg, k, cfg.n_kv_heads, dev, "k"), _kv_rows(cfg, v, cfg.n_kv_heads, dev, "v"),
+                              _kv_ints(q_offsets, n_seqs + 1, dev, "q_offsets"), None if k_offsets is None else _kv_ints(k_offsets, n_seqs + 1, dev, "k_offsets"), n_seqs, n, n_keys,
+                              _kv_rows(cfg, out, cfg.n_q_heads, dev, "out", True), None if faults is None else _kv_ints(faults, 1, dev, "faults"), _kv_stream(stream, dev))
     if rc:
         _kv_check(rc)
 
@@ -691,13 +696,13 @@ def flame_kv_prompt(cfg, q, k, v, q_offsets, out, k_offsets=None, faults=None, s
 def flame_kv_extend(cfg, cache, q, q_offsets, kv_lens, out, workspace=None, faults=None, stream=None) -> None:
     """q, out: device rows [n_tokens, n_q_heads, head_dim], the newest tokens of every sequence; q_offsets [n_seqs + 1], kv_lens [n_seqs]: device int32;
     workspace: device tensor of at least flame_kv_workspace_bytes(cfg, n_seqs, n_tokens) bytes."""
-    n_seqs, n = kv_lens.shape[0], q.shape[0]
-    if out.shape[0] != n:
+    n_seqs, n, dev = len(kv_lens), len(q), torch.cuda.current_device()
+    if len(out) != n:
         raise ValueError("out must have the rows of q")
-    wp, wb = _kv_workspace(workspace)
-    rc = _lib.flame_kv_extend(C.byref(cfg), _kv_cache_for(cfg, cache, n_seqs), C.byref(_kv_rows(cfg, q, cfg.n_q_heads, "q")), _kv_ints(q_offsets, n_seqs + 1, "q_offsets"),
-                              _kv_ints(kv_lens, n_seqs, "kv_lens"), n_seqs, n, C.byref(_kv_rows(cfg, out, cfg.n_q_heads, "out", True)), wp, wb,
-                              None if faults is None else _kv_ints(faults, 1, "faults"), _stream_ptr(stream))
+    wp, wb = _kv_workspace(workspace, dev)
+    rc = _lib.flame_kv_extend(cfg, _kv_cache_for(cfg, cache, n_seqs, dev), _kv_rows(cfg, q, cfg.n_q_heads, dev, "q"), _kv_ints(q_offsets, n_seqs + 1, dev, "q_offsets"),
+                              _kv_ints(kv_lens, n_seqs, dev, "kv_lens"), n_seqs, n, _kv_rows(cfg, out, cfg.n_q_heads, dev, "out", True), wp, wb,
+                              None if faults is None else _kv_ints(faults, 1, dev, "faults"), _kv_stream(stream, dev))
     if rc:
         _kv_check(rc)
 
@@ -705,12 +710,12 @@ def flame_kv_extend(cfg, cache, q, q_offsets, kv_lens, out, workspace=None, faul
 def flame_kv_decode(cfg, cache, q, kv_lens, out, workspace=None, faults=None, stream=None) -> None:
     """q, out: device rows [n_seqs, n_q_heads, head_dim], one new token of every sequence; kv_lens: device int32 [n_seqs];
     workspace: device tensor of at least flame_kv_workspace_bytes(cfg, n_seqs) bytes."""
-    n_seqs = kv_lens.shape[0]
-    if q.shape[0] != n_seqs or out.shape[0] != n_seqs:
+    n_seqs, dev = len(kv_lens), torch.cuda.current_device()
+    if len(q) != n_seqs or len(out) != n_seqs:
         raise ValueError("q and out must have one row per sequence")
-    wp, wb = _kv_workspace(workspace)
-    rc = _lib.flame_kv_decode(C.byref(cfg), _kv_cache_for(cfg, cache, n_seqs), C.byref(_kv_rows(cfg, q, cfg.n_q_heads, "q")), _kv_ints(kv_lens, n_seqs, "kv_lens"), n_seqs,
-                              C.byref(_kv_rows(cfg, out, cfg.n_q_heads, "out", True)), wp, wb, None if faults is None else _kv_ints(faults, 1, "faults"), _stream_ptr(stream))
+    wp, wb = _kv_workspace(workspace, dev)
+    rc = _lib.flame_kv_decode(cfg, _kv_cache_for(cfg, cache, n_seqs, dev), _kv_rows(cfg, q, cfg.n_q_heads, dev, "q"), _kv_ints(kv_lens, n_seqs, dev, "kv_lens"), n_seqs,
+                              _kv_rows(cfg, out, cfg.n_q_heads, dev, "out", True), wp, wb, None if faults is None else _kv_ints(faults, 1, dev, "faults"), _kv_stream(stream, dev))
     if rc:
         _kv_check(rc)
 

@@ -542,7 +542,11 @@ def test_refusals_on_the_device(B):
     cache = B.pack_kv_cache(cfg, pool, pool.clone(), table)
     lens = ints([1, 1, 1])
     wide = torch.zeros(3, 8, 68, device=DEV, dtype=torch.bfloat16)[..., :64]
-    for bad, kind in ((lambda: B.flame_kv_append(cfg, cache, kv.cpu(), kv, i, lens), ValueError), (lambda: B.flame_kv_append(cfg, cache, kv, kv, i.cpu(), lens), ValueError),
+    for bad, kind in ((lambda: B.flame_kv_append(cfg, cache, kv, kv[:2], i, lens), ValueError), (lambda: B.flame_kv_append(cfg, cache, kv, kv, i, lens, q=q), ValueError),
+                      (lambda: B.flame_kv_append(cfg, cache, kv, kv, i, lens, q_out=q), ValueError), (lambda: B.flame_kv_append(cfg, cache, kv, kv, i, lens, q=q, q_out=q[:2]), ValueError),
+                      (lambda: B.flame_kv_prompt(cfg, q, kv, kv[:2], i, q), ValueError), (lambda: B.flame_kv_prompt(cfg, q, kv, kv, i, q[:2]), ValueError),
+                      (lambda: B.flame_kv_extend(cfg, cache, q, i, lens, q[:2]), ValueError), (lambda: B.flame_kv_decode(cfg, cache, q, lens, q[:2]), ValueError),
+                      (lambda: B.flame_kv_append(cfg, cache, kv.cpu(), kv, i, lens), ValueError), (lambda: B.flame_kv_append(cfg, cache, kv, kv, i.cpu(), lens), ValueError),
                       (lambda: B.flame_kv_append(cfg, cache, kv, kv, i[:3], lens), ValueError), (lambda: B.flame_kv_prompt(cfg, q, kv, kv, i, q[:1].expand(3, 8, 64)), ValueError),
                       (lambda: B.flame_kv_prompt(cfg, wide, kv, kv, i, q), B.FlameGRError), (lambda: B.flame_kv_decode(B.make_kv_config("f16", 8, 2, 64), cache, q.half(), lens, q.half()), ValueError),
                       (lambda: B.flame_kv_decode(cfg, cache, torch.zeros(4, 8, 64, device=DEV, dtype=torch.bfloat16), ints([1] * 4), torch.zeros(4, 8, 64, device=DEV, dtype=torch.bfloat16)), ValueError),

@@ -162,14 +162,12 @@ def test_refusals_of_the_binding():
     cfg = B.make_kv_config("bf16", 8, 2, 64)
     q, kv, i = torch.zeros(5, 8, 64, dtype=torch.bfloat16), torch.zeros(5, 2, 64, dtype=torch.bfloat16), torch.zeros(3, dtype=torch.int32)
     pool, table = torch.zeros(4, 16, 2, 64, dtype=torch.bfloat16), torch.zeros(2, 3, dtype=torch.int32)
-    for bad in (lambda: B._kv_rows(cfg, q[:, :7], 8, "q"), lambda: B._kv_rows(cfg, q.float(), 8, "q"), lambda: B._kv_rows(cfg, q[..., :32], 8, "q"),
-                lambda: B._kv_rows(cfg, q[0], 8, "q"), lambda: B._kv_ints(i.long(), 3, "i"), lambda: B._kv_ints(i, 4, "i"), lambda: B._kv_ints(i[None], 1, "i"),
-                lambda: B._kv_ints(torch.zeros(6, dtype=torch.int32)[::2], 3, "i"), lambda: B.pack_kv_cache(cfg, pool[..., :32], pool[..., :32], table),
+    for bad in (lambda: B._kv_rows(cfg, q[:, :7], 8, -1, "q"), lambda: B._kv_rows(cfg, q.float(), 8, -1, "q"), lambda: B._kv_rows(cfg, q[..., :32], 8, -1, "q"),
+                lambda: B._kv_rows(cfg, q[0], 8, -1, "q"), lambda: B._kv_ints(i.long(), 3, -1, "i"), lambda: B._kv_ints(i, 4, -1, "i"), lambda: B._kv_ints(i[None], 1, -1, "i"),
+                lambda: B._kv_ints(torch.zeros(6, dtype=torch.int32)[::2], 3, -1, "i"), lambda: B.pack_kv_cache(cfg, pool[..., :32], pool[..., :32], table),
                 lambda: B.pack_kv_cache(cfg, pool, pool.float(), table), lambda: B.pack_kv_cache(cfg, pool, pool[:3], table), lambda: B.pack_kv_cache(cfg, pool, pool, table.long()),
                 lambda: B.pack_kv_cache(cfg, pool, pool, table[0]), lambda: B.pack_kv_cache(cfg, pool, pool, table),      # (the last: host memory)
-                lambda: B.flame_kv_append(cfg, None, kv, kv[:4], i, i), lambda: B.flame_kv_append(cfg, None, kv, kv, i, i, q=q), lambda: B.flame_kv_append(cfg, None, kv, kv, i, i, q_out=q),
-                lambda: B.flame_kv_prompt(cfg, q, kv, kv[:4], i, q), lambda: B.flame_kv_prompt(cfg, q, kv, kv, i, q[:4]), lambda: B.flame_kv_extend(cfg, None, q, i, i, q[:4]),
-                lambda: B.flame_kv_decode(cfg, None, q, i, q), lambda: B._kv_torch_dtype(B.make_kv_config(7, 8, 2, 64))):
+                lambda: B._kv_rows(B.make_kv_config(7, 8, 2, 64), q, 8, -1, "q")):
         with pytest.raises(ValueError):
             bad()
 
