@@ -75,9 +75,9 @@ int take_rotation(const flame_kv_config *c, const flame_kv_rotation *r, KvRotati
   for (int j = 0; j < out->pairs; ++j) {
     if (!std::isfinite(r->frequencies[j])) return bad("a frequency is not finite");
     // revolutions per position, of which only the fraction turns anything
-    const long double turns = (long double)r->frequencies[j] / 6.283185307179586476925286766559005768L;
-    const long double fraction = turns - floorl(turns);
-    out->turns[j] = fraction < 1.0L ? (uint64_t)ldexpl(fraction, 64) : 0;
+    const long double turns = (long double)r->frequencies[j] * (1.0L / 6.283185307179586476925286766559005768L);
+    const long double fraction = turns >= 0.0L && turns < 1.0L ? turns : turns - floorl(turns);
+    out->turns[j] = fraction < 1.0L ? (uint64_t)(fraction * 0x1p64L) : 0;
   }
   return FLAME_GR_OK;
 }

@@ -1,8 +1,12 @@
 // Causal softmax attention of packed query rows with grouped heads, over packed keys or a paged cache.
 //
-// Bound by the matrix pipe and the vector work of the softmax beside it.  A workgroup takes 128 query rows of one sequence and key head, row = token * G + head of the
+// Bound by the matrix pipe and the vector work of the softmax beside it, and in the end by power: one prompt of 32768, 16/2 heads of 128, bf16, runs at 0.97 PFLOP/s and a clock of
+// 2.0 GHz, with the matrix pipe busy 47 % of the cycles (a plain matrix product of 8192 reaches 1.22 PFLOP/s on this chip).  Forms with fewer cycles ran at a lower clock in the same time.
+//
+// A workgroup takes 128 query rows of one sequence and key head, row = token * G + head of the
 // group (the G query heads that share a key head are rows of one tile: short sequences fill it, and the mask cuts through fewer key tiles), four wavefronts of 32 rows each.  It
-// walks the keys in tiles of 64, two stages in LDS, brought there by LDS-DMA loads one tile ahead.  Products are transposed as in attn_mfma.hip,
+// walks the keys in tiles of 64, two stages in LDS, brought there by LDS-DMA loads one tile ahead.  In small launches two or four wavefronts share 32 rows and take a part of each
+// tile's keys, with a maximum, sum and accumulator of their own that are joined at the end (launch_flash_for_size).  Products are transposed as in attn_mfma.hip,
 //     S^T[key][row] = K Q^T        A operand = K rows, B operand = Q rows
 //     O^T[feature][row] += V^T P^T A operand = V^T rows, B operand = P^T
 // so that the first product's accumulator, where a lane has one row and 16 of 32 keys, is the second product's B operand as it stands: elements 8 s + i of a lane in half h are keys
@@ -12,7 +16,7 @@
 // LDS rows are unpadded, as the DMA fills 1 KB of consecutive bytes, and swizzled by XOR: K in 16-byte chunks with the low bits of the key, V in 32-byte chunks so that the four
 // rows and two neighbouring chunks that 32 lanes of a transposing read touch lie in the eight different 32-byte slots of 256 bytes.
 //
-// Where a key lies: one wavefront looks the tile's 64 keys up, two tiles ahead, and leaves their byte offsets in LDS for the requests of all; packed keys take the same way.  Any page
+// Where a key lies: a wavefront looks up 64 keys of a tile, two tiles ahead, and leaves their byte offsets in LDS for the requests of all; packed keys take the same way.  Any page
 // size and any strides cost the same.
 //
 // Masked keys: their logits are -infinity, and their values meet weights of zero.  That is harmless while they are finite.  If a workgroup's
@@ -24,9 +28,16 @@ namespace flame {
 
 namespace {
 
-constexpr int QT = 128;             // query rows of a workgroup
-// keys of a tile: as many as leave two workgroups on a compute unit
-template <typename T, int DH> constexpr int key_tile() { return DH * sizeof(T) == 512 ? 32 : 64; }
+// KP wavefronts share 32 query rows and take KT keys of each tile of KP KT apiece.
+constexpr int kFlashRows = 128;     // query rows of a workgroup are this / KP
+template <typename T, int DH, int KP> constexpr int key_block() { return DH * sizeof(T) >= (KP == 1 ? 512 : KP == 2 ? 256 : 128) ? 32 : 64; }
+// Two stages of K and V, and in the end their place has room for the parts of rows: 4 x 32 rows of DH + 4 floats, a maximum and a sum.
+template <typename T, int DH, int KP> constexpr int flash_lds_bytes() {
+  constexpr int stages = 4 * KP * key_block<T, DH, KP>() * DH * (int)sizeof(T), parts = KP == 1 ? 0 : 4 * 32 * (DH + 6) * 4;
+  return stages > parts ? stages : parts;
+}
+// Workgroups of 4 wavefronts on a compute unit.
+template <typename T, int DH, int KP> constexpr int flash_workgroups() { return flash_lds_bytes<T, DH, KP>() > 72 * 1024 ? 1 : 2; }
 
 template <typename T> struct Matrix32;              // (fp32 products are 32x32x2: the third dimension is the lane's half)
 template <> struct Matrix32<bf16_t> {
@@ -65,18 +76,20 @@ template <int DB, int RB, int AT> __device__ __forceinline__ void read_values(ui
 #undef READ
 }
 
-template <typename T, int DH, bool PAGED>
-__global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
+template <typename T, int DH, bool PAGED, int KP>
+__global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash_kernel(KvAttention a) {
   constexpr bool F32 = sizeof(T) == 4;
-  constexpr int KT = key_tile<T, DH>(), NJ = KT / 32;             // keys of a tile, 32-key blocks of it
+  constexpr int QT = kFlashRows / KP;                             // query rows of a workgroup
+  constexpr int KT = key_block<T, DH, KP>(), NJ = KT / 32;        // a wavefront's keys of a tile, 32-key blocks of them
+  constexpr int KW = KP * KT;                                     // keys of a tile
   constexpr int RB = DH * (int)sizeof(T), CH = RB / 16;           // bytes of a row, and 16-byte chunks
   constexpr int KS = RB / 32, DB = DH / 32;                       // steps of 32 bytes along a row (16 per lane), feature blocks
-  constexpr int TILE = KT * RB;                                   // bytes of a K or V tile
+  constexpr int TILE = KW * RB;                                   // bytes of a K or V tile
   constexpr int STAGE = 2 * TILE;
   constexpr int RPI = 64 / CH, NI = TILE / 1024 / 4;              // rows of a 1 KB request, requests of a wavefront per tile of K or V
   extern __shared__ __attribute__((aligned(1024))) char lds[];
-  __shared__ int64_t at_s[3][PAGED ? 1 : 2][KT];                  // byte offsets of a tile's keys (packed: and values)
-  __shared__ uint64_t there_s[3];                                 // which of them count
+  __shared__ int64_t at_s[3][PAGED ? 1 : 2][KW];                  // byte offsets of a tile's keys (packed: and values)
+  __shared__ uint32_t there_s[3][KW / 32];                        // which of them count
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l32 = lane & 31, lh = lane >> 5;
   const int group = a.n_q_heads / a.n_kv_heads;
@@ -125,16 +138,19 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
   // keys seen: by the row before the first one of the sequence, by the last row of the workgroup, by the first and last of my wavefront, by my row
   const int64_t back = n - (end - first);
   auto seen_by = [&](int row) { return (int)max((int64_t)0, back + row / group + 1); };
-  const int n_seen = seen_by(min(row0 + QT, rows) - 1), n_tiles = (n_seen + KT - 1) / KT;
-  const int wave_row = row0 + wave * 32;
+  const int n_seen = seen_by(min(row0 + QT, rows) - 1), n_tiles = (n_seen + KW - 1) / KW;
+  const int part = KP == 1 ? 0 : wave % KP, wave_row = row0 + wave / KP * 32;
   const bool active = wave_row < rows;
   const int my_row = active ? min(wave_row + l32, rows - 1) : row0, token = my_row / group, head = kvh * group + my_row - token * group;
   const int sees = seen_by(my_row), wave_least = active ? seen_by(wave_row) : 0, wave_most = active ? seen_by(min(wave_row + 31, rows - 1)) : 0;
 
   typedef __attribute__((address_space(1))) const void gvoid;
   typedef __attribute__((address_space(3))) void lvoid;
-  auto look_up = [&](int t, int64_t (&to)[2]) {                   // of key `lane` of tile t; -1: none
-    const int near = min(t * KT + lane, n - 1);
+  // Each wavefront looks after 64 keys of a tile, as far as they go.
+  const int ring = wave * 64 + lane;
+  const bool looks = wave * 64 < KW;
+  auto look_up = [&](int t, int64_t (&to)[2]) {                   // of key `ring` of tile t; -1: none
+    const int near = min(t * KW + ring, n - 1);
     if (PAGED) {
       to[0] = kv_token_offset(a.pages, table, (uint32_t)near);
     } else {
@@ -144,14 +160,14 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
   };
   auto publish = [&](int t, const int64_t (&from)[2]) {
     const int64_t k_at = from[0];
-    const bool mine = lane < KT;
+    const bool mine = ring < KW;
     if (PAGED && mine && k_at < 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_PAGE);
     if (mine) {
-      at_s[t % 3][0][lane] = max(k_at, (int64_t)0);
-      if (!PAGED) at_s[t % 3][PAGED ? 0 : 1][lane] = from[1];
+      at_s[t % 3][0][ring] = max(k_at, (int64_t)0);
+      if (!PAGED) at_s[t % 3][PAGED ? 0 : 1][ring] = from[1];
     }
-    const uint64_t there = __builtin_amdgcn_ballot_w64(!mine || ((!PAGED || k_at >= 0) && t * KT + lane < n));
-    if (lane == 0) there_s[t % 3] = there;
+    const uint64_t there = __builtin_amdgcn_ballot_w64((!PAGED || k_at >= 0) && t * KW + ring < n);
+    if (mine && (lane & 31) == 0) there_s[t % 3][ring / 32] = (uint32_t)(there >> lane);
   };
   // swizzle: what the chunk index of a row is XORed with (fp32 values are read a row at a time, side by side: no need)
   auto k_key_of = [](int r) { return RB >= 256 ? r & 15 : RB == 128 ? r >> 1 & 7 : r >> 2 & 3; };
@@ -189,11 +205,10 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
   float m, l;
   auto tile_step = [&](int t, auto careful_c) __attribute__((always_inline)) {
     constexpr bool careful = decltype(careful_c)::value;
-    const char *sk = lds + (t & 1) * STAGE, *sv = sk + TILE;
-    const int k0 = t * KT;
+    const char *sk = lds + (t & 1) * STAGE + part * (KT * RB), *sv = sk + TILE;
+    const int k0 = t * KW + part * KT;
     if (k0 >= wave_most) return;
-    const uint64_t there = there_s[t % 3];
-    const uint32_t there_lo = __builtin_amdgcn_readfirstlane((int)there), there_hi = __builtin_amdgcn_readfirstlane((int)(there >> 32));
+    const uint32_t there_lo = __builtin_amdgcn_readfirstlane((int)there_s[t % 3][part * NJ]), there_hi = NJ == 2 ? __builtin_amdgcn_readfirstlane((int)there_s[t % 3][part * NJ + NJ - 1]) : ~0u;
     const bool masked = k0 + KT > wave_least || (there_lo & there_hi) != 0xffffffffu;
     f32x16 z[NJ];
 #pragma unroll
@@ -290,9 +305,9 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
         }
     } else {
     typedef typename Matrix32<T>::frag frag;
-    frag p[4];
+    frag p[2 * NJ];
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+    for (int j = 0; j < NJ; ++j)
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float w = __builtin_amdgcn_exp2f(__builtin_fmaf(z[j][e], scale, nm));
@@ -315,11 +330,13 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
       };
       products(std::integral_constant<int, 0>{});
       products(std::integral_constant<int, 1>{});
-      products(std::integral_constant<int, 2>{});
-      products(std::integral_constant<int, 3>{});
+      if constexpr (NJ == 2) {
+        products(std::integral_constant<int, 2>{});
+        products(std::integral_constant<int, 3>{});
+      }
     } else {
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
+    for (int s = 0; s < 2 * NJ; ++s)
 #pragma unroll
       for (int b = 0; b < DB; ++b) {
         typedef __attribute__((address_space(3))) s16x4 *ltr;
@@ -370,7 +387,7 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
     m = -INFINITY;
     l = 0.f;
     int64_t next[2] = {0, 0};
-    if (wave == 0) {
+    if (looks) {
       look_up(0, next);
       publish(0, next);
       look_up(1, next);
@@ -383,7 +400,7 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
       asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
       __syncthreads();                                            // tile t has landed, and everybody has left tile t - 1
       if (t + 1 < n_tiles) request(t + 1);
-      if (wave == 0) {
+      if (looks) {
         publish(t + 2, next);
         look_up(t + 3, next);
       }
@@ -411,10 +428,55 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
     l = 0.f;
   }
   l = pair_sum(l);
+  if constexpr (KP > 1) {
+    // The parts of a row are joined through LDS, in the order of the wavefronts.
+    constexpr int PR = DH + 4;
+    float *po = (float *)lds, *pm = po + 4 * 32 * PR, *pl = pm + 4 * 32;
+    static_assert((4 * 32 * PR + 8 * 32) * 4 <= flash_lds_bytes<T, DH, KP>(), "the parts fit in the stages' place");
+#pragma unroll
+    for (int b = 0; b < DB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int at = 8 * (e >> 2) + 4 * lh + (e & 3);
+        po[(wave * 32 + l32) * PR + (F32 ? DB * at + b : 32 * b + at)] = o[b][e];
+      }
+    if (lh == 0) {
+      pm[wave * 32 + l32] = m;
+      pl[wave * 32 + l32] = l;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < QT * DH / 1024; ++i) {
+      const int at = threadIdx.x + 256 * i, r = at / (DH / 4), f = at % (DH / 4) * 4, first_part = (r / 32 * KP) * 32 + r % 32;
+      const int row = row0 + r;
+      if (row >= rows) continue;
+      float top = -INFINITY, sum = 0.f;
+#pragma unroll
+      for (int w = 0; w < KP; ++w) top = fmaxf(top, pm[first_part + 32 * w]);
+      const float ref = top == -INFINITY ? 0.f : top;
+      f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int w = 0; w < KP; ++w) {
+        const float mw = pm[first_part + 32 * w], take = mw == top ? 1.f : __builtin_amdgcn_exp2f(mw - ref);
+        const f32x4 ow = *(const f32x4 *)(po + (first_part + 32 * w) * PR + f);
+        sum += pl[first_part + 32 * w] * take;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[e] += ow[e] * take;
+      }
+      const float inv = top == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
+      typedef T out4 __attribute__((ext_vector_type(4)));
+      out4 y;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) y[e] = kv_round<T>(x[e] * inv);
+      const int tk = row / group, h = kvh * group + row - tk * group;
+      *(out4 *)(a.out.p + (first + tk) * a.out.row + h * a.out.head + f * sizeof(T)) = y;
+    }
+    return;
+  }
   const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
   // Rows to memory: each wavefront turns its 32 x DH patch in LDS, 16-byte chunks XORed with the row.
   char *patch = lds + wave * (32 * RB);
-  static_assert(4 * 32 * RB <= 2 * STAGE, "the patches fit in the stages");
+  static_assert(KP > 1 || 4 * 32 * RB <= 2 * STAGE, "the patches fit in the stages");
   if constexpr (F32) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -448,14 +510,32 @@ __global__ __launch_bounds__(256, 2) void kv_flash_kernel(KvAttention a) {
   }
 }
 
-template <typename T, int DH, bool PAGED> hipError_t launch_flash(const KvAttention &a, hipStream_t stream) {
+template <typename T, int DH, bool PAGED, int KP> hipError_t launch_flash(const KvAttention &a, hipStream_t stream) {
   static std::atomic<uint64_t> raised{0};
-  constexpr int kBytes = 4 * key_tile<T, DH>() * DH * (int)sizeof(T);                         // two stages of K and V
-  const hipError_t e = raise_lds_limit(reinterpret_cast<const void *>(&kv_flash_kernel<T, DH, PAGED>), kBytes, raised);
+  constexpr int kBytes = flash_lds_bytes<T, DH, KP>();
+  const hipError_t e = raise_lds_limit(reinterpret_cast<const void *>(&kv_flash_kernel<T, DH, PAGED, KP>), kBytes, raised);
   if (e != hipSuccess) return e;
-  const int64_t slots = a.batch.n_rows * (a.n_q_heads / a.n_kv_heads) / QT + a.batch.n_seqs;
-  kv_flash_kernel<T, DH, PAGED><<<(unsigned)(slots * a.n_kv_heads), 256, kBytes, stream>>>(a);
+  const int64_t slots = a.batch.n_rows * (a.n_q_heads / a.n_kv_heads) / (kFlashRows / KP) + a.batch.n_seqs;
+  kv_flash_kernel<T, DH, PAGED, KP><<<(unsigned)(slots * a.n_kv_heads), 256, kBytes, stream>>>(a);
   return hipGetLastError();
+}
+
+// Wavefronts per 32 query rows.  A workgroup of few rows walks its keys in a quarter or half as many steps, but reads them for fewer rows: it pays where whole workgroups, by the
+// bound on their number that rows and sequences give, do not fill the chip.  us with 1 | 2 | 4 at that number (bf16 and fp32, causal prompts):
+//   16 bits, D = 64:  72 (1 x 1024, 8 heads) 22.6 | 14.7 | 12.0   160 (4 x 512) 13.9 | 10.8 | 10.3   264 (1 x 4096) 76 | 49 | 49   288 (4 x 1024) 23.7 | 19.4 | 23.7
+//                     384 (16 x 256) 11.1 | 10.8 | 14.5   1152 (16 x 1024) 45 | 55 | 77
+//   D = 128:          72 (1 x 256, 32/8 heads) 11.7 | 11.0 | 9.5   264 (1 x 1024) 29.8 | 27.0 | 44.6   520 (1 x 2048) 60 | 64 | 124
+//   D = 32:           272 (1 x 2048, 16 heads) 31.5 | 20.2 | 22.8   576 (4 x 1024) 22.7 | 19.8 | 30.0   768 (16 x 256) 9.7 | 13.2 | 21.4
+//   fp32, D = 64:     264 (1 x 4096) 290 | 222 | 198   288 (4 x 1024) 99 | 76 | 68   384 (16 x 256) 34 | 25 | 38   1280 (32 x 512) 128 | 123 | 189
+//   D = 128:          264 (1 x 1024) 146 | 97   544 (4 x 512) 132 | 114   1152 (16 x 256) 124 | 160       D = 32: 576 (4 x 1024) 72 | 68 | 67   768 (16 x 256) 26 | 29 | 33
+template <typename T, int DH, bool PAGED> hipError_t launch_flash_for_size(const KvAttention &a, hipStream_t stream) {
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int64_t kFour = F32 ? 288 : 160, kTwo = F32 ? 640 : DH == 32 ? 576 : 384;
+  const int64_t workgroups = (a.batch.n_rows * (a.n_q_heads / a.n_kv_heads) / kFlashRows + a.batch.n_seqs) * a.n_kv_heads;
+  if constexpr (DH * sizeof(T) < 512)                             // (LDS has no room for four wavefronts' tiles of wider rows)
+    if (workgroups <= kFour) return launch_flash<T, DH, PAGED, 4>(a, stream);
+  if (workgroups <= kTwo) return launch_flash<T, DH, PAGED, 2>(a, stream);
+  return launch_flash<T, DH, PAGED, 1>(a, stream);
 }
 
 }  // namespace
@@ -466,7 +546,7 @@ hipError_t launch_kv_attention(const KvAttention &a, hipStream_t stream) {
     using T = decltype(t);
     kv_with_width(a.head_dim, [&](auto width) {
       constexpr int DH = decltype(width)::value;
-      e = a.pages.table ? launch_flash<T, DH, true>(a, stream) : launch_flash<T, DH, false>(a, stream);
+      e = a.pages.table ? launch_flash_for_size<T, DH, true>(a, stream) : launch_flash_for_size<T, DH, false>(a, stream);
     });
   });
   return e;
