@@ -94,43 +94,77 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   const int l32 = lane & 31, lh = lane >> 5;
   const int group = a.n_q_heads / a.n_kv_heads;
 
-  // Which tile: those of sequence b begin at slot offsets[b] * G / QT + b, where there is room for them whatever the lengths; the last ones, with most keys, go first.
+  // Which tile.  Tiles with most keys go first: the sequences by their number of keys, and each from its end.
+  if (blockIdx.x == 0 && a.batch.faults)
+    for (int b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
+      const int64_t first = a.batch.offsets[b], end = a.batch.offsets[b + 1];
+      if (first < 0 || end < first || end > a.batch.n_rows) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
+      if (PAGED) {
+        kv_clip_length(a.batch.kv_lens[b], a.pages.capacity, a.batch.faults, true);
+      } else if (a.k_offsets) {
+        const int64_t k_first = a.k_offsets[b], k_end = a.k_offsets[b + 1];
+        if (k_first < 0 || k_end < k_first || k_end > a.n_keys) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
+      } else if (first < 0 || end > a.n_keys) {
+        kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
+      }
+    }
   const int kvh = blockIdx.x % a.n_kv_heads;
-  const int64_t slot = gridDim.x / a.n_kv_heads - 1 - blockIdx.x / a.n_kv_heads;
+  const int64_t slot = blockIdx.x / a.n_kv_heads;
   int seq;
-  {
+  int64_t tile;                                                   // counted from the sequence's end
+  if (a.batch.n_seqs <= 64) {
+    // One lane per sequence: the tiles of those that come before it.
+    int64_t tiles = 0;
+    int keys = -1;
+    if (lane < a.batch.n_seqs) {
+      const int64_t b = a.batch.offsets[lane], e = a.batch.offsets[lane + 1];
+      tiles = b < 0 ? 0 : (max((int64_t)0, min(e, a.batch.n_rows) - b) * group + QT - 1) / QT;
+      keys = PAGED ? a.batch.kv_lens[lane] : (int)(e - b);
+    }
+    int64_t before = 0;
+    for (int j = 0; j < a.batch.n_seqs; ++j) {
+      const int other = __builtin_amdgcn_readlane(keys, j);
+      before += other > keys || (other == keys && j < lane) ? (int64_t)__builtin_amdgcn_readlane((int)tiles, j) : 0;
+    }
+    const uint64_t mine = __builtin_amdgcn_ballot_w64(slot >= before && slot < before + tiles);
+    if (!mine) return;
+    seq = __builtin_ctzll(mine);
+    tile = slot - __builtin_amdgcn_readlane((int)before, seq);
+  } else {
+    // Those of sequence b begin at slot offsets[b] * G / QT + b, where there is room for them whatever the lengths; the last sequence goes first.
+    const int64_t back_slot = gridDim.x / a.n_kv_heads - 1 - slot;
     int lo = 0, n = a.batch.n_seqs;                               // the last sequence whose slots begin at or before this one
     while (n > 1) {
       const int step = (n + 63) / 64;
       const int b = lo + min((lane + 1) * step, n - 1);
-      const bool after = (lane + 1) * step >= n || (int64_t)a.batch.offsets[b] * group / QT + b > slot;
+      const bool after = (lane + 1) * step >= n || (int64_t)a.batch.offsets[b] * group / QT + b > back_slot;
       const int c = __builtin_ctzll(__builtin_amdgcn_ballot_w64(after) | 1ull << 63);
       lo += c * step;
       n = max(1, min(step, n - c * step));
     }
     seq = min(lo, a.batch.n_seqs - 1);
+    const int64_t b = a.batch.offsets[seq], e = a.batch.offsets[seq + 1];
+    const int64_t tiles = (max((int64_t)0, min(e, a.batch.n_rows) - b) * group + QT - 1) / QT;
+    tile = tiles - 1 - (back_slot - (b * group / QT + seq));
   }
   const int64_t first = a.batch.offsets[seq], end = a.batch.offsets[seq + 1];
-  const bool wrong = first < 0 || end < first || end > a.batch.n_rows;
-  if (wrong && threadIdx.x == 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
   if (first < 0 || end < first) return;
-  const int64_t tile = slot - (first * group / QT + seq);
   const int rows = (int)max((int64_t)0, min(end, a.batch.n_rows) - first) * group;
-  if (tile < 0 || tile * QT >= rows) return;
-  const int row0 = (int)tile * QT;
+  const int row_tiles = (rows + QT - 1) / QT;
+  if (tile < 0 || tile >= row_tiles) return;
+  const int row0 = (row_tiles - 1 - (int)tile) * QT;
 
   int n;
   const char *kp, *vp;
   const int32_t *table = nullptr;
   if (PAGED) {
-    n = kv_clip_length(a.batch.kv_lens[seq], a.pages.capacity, a.batch.faults, threadIdx.x == 0);
+    n = kv_clip(a.batch.kv_lens[seq], a.pages.capacity);
     kp = a.pages.k + kvh * a.pages.head;
     vp = a.pages.v + kvh * a.pages.head;
     table = a.pages.table + seq * a.pages.table_stride;
   } else {
     const int32_t *ko = a.k_offsets ? a.k_offsets : a.batch.offsets;
     const int64_t k_first = ko[seq], k_end = ko[seq + 1];
-    if ((k_first < 0 || k_end < k_first || k_end > a.n_keys) && threadIdx.x == 0) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
     n = k_first < 0 ? 0 : (int)max((int64_t)0, min(k_end, a.n_keys) - k_first);
     kp = a.k.p + k_first * a.k.row + kvh * a.k.head;
     vp = a.v.p + k_first * a.v.row + kvh * a.v.head;

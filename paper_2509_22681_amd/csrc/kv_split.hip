@@ -4,7 +4,7 @@
 // (G query heads share a key head), far below what the matrix pipe does in that time.  So everything serves the loads:
 //   - A unit is a block of 16 query rows of one sequence and key head (row = token * G + head of the group; a decoding step
 //     with G <= 16 has one unit per key head, whose keys and values are then read once), and a tile 32 of its keys (16 in fp32).  The tiles of all units form one
-//     line, which kWorkers wavefronts cut into equal parts: every wavefront streams the same number of bytes whatever the lengths of the sequences, one long sequence fills the chip,
+//     line, which a fixed number of wavefronts cuts into equal parts: every wavefront streams the same number of bytes whatever the lengths of the sequences, one long sequence fills the chip,
 //     and nothing depends on the host knowing the lengths.  A wavefront works alone: no barriers, no LDS traffic but for the
 //     row offsets.
 //   - Keys and values go from memory straight into the registers of the matrix operands, one tile ahead of the arithmetic (16 KB
@@ -20,7 +20,9 @@ namespace flame {
 
 namespace {
 
-constexpr int kWorkers = 2048;      // wavefronts: two per SIMD, as their registers allow
+// Wavefronts per SIMD, as their registers allow, and in all.
+constexpr int split_occupancy(int dh) { return dh == 128 ? 2 : dh == 64 ? 3 : 4; }
+constexpr int split_workers(int dh) { return 1024 * split_occupancy(dh); }
 constexpr int kRows = 16;           // query rows of a unit
 
 template <typename T, int DH> struct SplitShape {
@@ -141,7 +143,7 @@ template <> struct Matrix16<half_t> {
 };
 
 template <typename T, int DH>
-__global__ __launch_bounds__(256, 2) void kv_split_kernel(KvAttention a, float *__restrict__ parts) {
+__global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAttention a, float *__restrict__ parts) {
   typedef SplitShape<T, DH> S;
   constexpr int KT = S::KT, VF = S::VF;
   constexpr bool F32 = S::F32;
@@ -157,7 +159,7 @@ __global__ __launch_bounds__(256, 2) void kv_split_kernel(KvAttention a, float *
   const int worker = blockIdx.x * 4 + wave;
   int64_t per = 0;
   SplitPlace place = split_find<KT>(a, lane, [&](int64_t total) {
-    per = (total + kWorkers - 1) / kWorkers;
+    per = (total + split_workers(DH) - 1) / split_workers(DH);
     return (int64_t)worker * per;
   });
   int64_t tile = (int64_t)worker * per;                           // on the line of all tiles
@@ -425,7 +427,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttention a, const float
   }
   total = split_lane(split_scan(total), 63) * a.n_kv_heads;
   before = split_lane(split_scan(before), 63) * a.n_kv_heads;
-  const int64_t per = (total + kWorkers - 1) / kWorkers;
+  const int64_t per = (total + split_workers(DH) - 1) / split_workers(DH);
   const int64_t first = before + (int64_t)(kvh * s.blocks + row / kRows) * s.tiles, last = first + s.tiles - 1;
   const int w0 = (int)(first / per), w1 = (int)(last / per);
   if (w0 == w1) return;                                           // it was not cut
@@ -465,7 +467,7 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttention a, const float
 }  // namespace
 
 int64_t kv_split_workspace_bytes(int32_t head_dim) {
-  return (int64_t)kWorkers * 2 * 4 * (head_dim == 32 ? split_part_floats<32>() : head_dim == 64 ? split_part_floats<64>() : split_part_floats<128>());
+  return (int64_t)split_workers(head_dim) * 2 * 4 * (head_dim == 32 ? split_part_floats<32>() : head_dim == 64 ? split_part_floats<64>() : split_part_floats<128>());
 }
 
 hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream) {
@@ -474,7 +476,7 @@ hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t st
     using T = decltype(t);
     kv_with_width(a.head_dim, [&](auto width) {
       constexpr int DH = decltype(width)::value;
-      kv_split_kernel<T, DH><<<kWorkers / 4, 256, 0, stream>>>(a, (float *)workspace);
+      kv_split_kernel<T, DH><<<split_workers(DH) / 4, 256, 0, stream>>>(a, (float *)workspace);
       kv_join_kernel<T, DH><<<joins, 256, 0, stream>>>(a, (const float *)workspace);
     });
   });

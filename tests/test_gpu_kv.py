@@ -328,6 +328,22 @@ def test_extend(B, dtype, hq, hkv, dim, new, lens, page, size):
             check_attention(host(out[s]), host(q[s]), *c.rows(b, n_b), dtype, what=(b, n_b))
 
 
+@pytest.mark.parametrize("dtype,heads,dim", [("bf16", 128, 128), ("bf16", 160, 128), ("f16", 128, 64), ("f16", 160, 64), ("bf16", 150, 32), ("bf16", 200, 32), ("f32", 200, 64), ("f32", 256, 64),
+                                             ("f32", 150, 128), ("f32", 256, 128), ("f32", 200, 32), ("f32", 256, 32)])
+def test_extend_of_many_heads(B, dtype, heads, dim):
+    """Launches of two and one wavefront per 32 rows over pages (300 new tokens: three workgroups a head)."""
+    import torch
+    gen = generator(heads)
+    c = Cache(B, gen, dtype, heads, heads, dim, [340], 24)
+    q = rand(gen, dtype, 300, heads, dim)
+    out = torch.full_like(q, 7.0)
+    B.flame_kv_extend(c.cfg, c.packed, q, ints([0, 300]), ints([340]), out, workspace_for(B, c.cfg, 1, 300))
+    keys, values = c.rows(0, 340)
+    for h in (0, 1, heads // 2, heads - 1):
+        check_attention(host(out[:, h:h + 1]), host(q[:, h:h + 1]), keys[:, h:h + 1], values[:, h:h + 1], dtype, what=h)
+    assert bool(out.isfinite().all()) and not bool((out == 7.0).all(-1).any())
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_bad_pages_and_lengths(B, dtype):
     """Keys in a page that the table does not name are not seen; lengths are cut to what the table has room for; both are reported."""
