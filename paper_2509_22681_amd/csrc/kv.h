@@ -37,11 +37,21 @@ struct KvAttention {
   KvPages pages;              // paged keys: table != NULL
   int32_t n_q_heads, n_kv_heads, head_dim, dtype;
   float scale;
+  int32_t splits;             // flash kernel over pages: parts of a row tile's keys
+  float *parts;
 };
+
+// How a call runs (kv_api.cpp): split kernel, or flash kernel with so many wavefronts per 32 rows and parts of the keys.
+struct KvRoute {
+  bool split;
+  int32_t wavefronts, splits;
+  int64_t workspace;          // bytes
+};
+KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool paged, bool decode, int64_t capacity);
 
 hipError_t launch_kv_append(const KvBatch &batch, const KvPages &pages, const KvRows &k, const KvRows &v, const KvRows *q, const KvRows *q_out,
                             const KvRotation &rotation, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, hipStream_t stream);
-hipError_t launch_kv_attention(const KvAttention &a, hipStream_t stream);
+hipError_t launch_kv_attention(const KvAttention &a, int wavefronts, hipStream_t stream);
 // few query rows: split over the keys (kv_split.hip)
 hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream);
 int64_t kv_split_workspace_bytes(int32_t head_dim);

@@ -1,4 +1,5 @@
 // C entries of the operators on a paged key/value cache (include/flame_kv.h): checks of arguments, byte strides, launches.
+#include <algorithm>
 #include <cmath>
 
 #include "kv.h"
@@ -19,9 +20,9 @@ int done(hipError_t e) {
   return bad(hipGetErrorString(e), FLAME_GR_HIP_ERROR);
 }
 
-// A grid dimension may have 2^32 - 1 threads.  Attention of packed rows has two of them per row and head, and 256 per sequence and head; split attention, of as many rows as
-// sequences or a few times that, 256 per row and head.
-constexpr int64_t kMaxRowHeads = (int64_t)1 << 25, kMaxSplitRowHeads = ((int64_t)1 << 24) - 1, kMaxSequenceHeads = ((int64_t)1 << 23) - 1;
+// A grid dimension may have 2^32 - 1 threads.  Attention of packed rows has two of them per row and head, and 256 per sequence and head; split attention, of one row per
+// sequence or of few in all, 256 per row and head.
+constexpr int64_t kMaxRowHeads = (int64_t)1 << 25, kMaxSequenceHeads = ((int64_t)1 << 23) - 1;
 constexpr int64_t kMaxKeys = ((int64_t)1 << 31) - 65536;     // of a sequence: room for a tile's end behind them in 32 bits
 
 int64_t element(int32_t dtype) { return dtype == FLAME_KV_F32 ? 4 : 2; }
@@ -90,12 +91,6 @@ void take_heads(const flame_kv_config *c, KvAttention *a) {
   a->scale = c->scale == 0.f ? 1.f / std::sqrt((float)c->head_dim) : c->scale;
 }
 
-// Calls of a few rows per sequence split the keys over the chip.
-bool splits(const flame_kv_config *c, int32_t n_seqs, int64_t n_rows) {
-  return n_rows * (c->n_q_heads / c->n_kv_heads) <= (int64_t)64 * n_seqs && n_rows * c->n_q_heads <= kMaxSplitRowHeads;
-}
-int64_t workspace_bytes_for(const flame_kv_config *c, int32_t n_seqs, int64_t n_rows) { return splits(c, n_seqs, n_rows) ? kv_split_workspace_bytes(c->head_dim) : 0; }
-
 int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_rows,
                  const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream) {
   KvAttention a{};
@@ -103,15 +98,43 @@ int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const 
   if (int rc = take_rows(cfg, out, &a.out)) return rc;
   if (int rc = take_pages(cfg, cache, &a.pages)) return rc;
   if (!kv_lens) return bad("kv_lens is NULL");
-  const int64_t need = workspace_bytes_for(cfg, n_seqs, n_rows);
+  const KvRoute route = kv_route(*cfg, n_seqs, n_rows, true, offsets == nullptr, a.pages.capacity);
+  const int64_t need = kv_route(*cfg, n_seqs, n_rows, true, offsets == nullptr, kMaxKeys).workspace;
   if (need > 0 && (!workspace || !aligned(workspace))) return bad("the workspace is NULL or not 16-byte aligned");
   if (workspace_bytes < need) return bad("the workspace is smaller than flame_kv_workspace_bytes", FLAME_GR_CAPACITY_EXCEEDED);
   a.batch = KvBatch{offsets, kv_lens, n_seqs, n_rows, faults};
   take_heads(cfg, &a);
-  return done(need > 0 ? launch_kv_split(a, workspace, (hipStream_t)stream) : launch_kv_attention(a, (hipStream_t)stream));
+  if (route.split) return done(launch_kv_split(a, workspace, (hipStream_t)stream));
+  a.splits = route.splits;
+  a.parts = (float *)workspace;
+  return done(launch_kv_attention(a, route.wavefronts, (hipStream_t)stream));
 }
 
 }  // namespace
+
+namespace flame {
+
+// Decoding steps, and calls with few query rows over caches that may be long, split the keys over the chip; others run on row tiles, of which a launch of few has its keys cut
+// into parts.  The host knows rows and sequences, but of the keys only what the page table has room for.
+KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool paged, bool decode, int64_t capacity) {
+  const bool f32 = c.dtype == FLAME_KV_F32;
+  const int64_t group = c.n_q_heads / c.n_kv_heads, heads = n_rows * c.n_q_heads;
+  if (decode || (paged && capacity > 1024 && heads <= (f32 ? 8192 : 1024))) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim)};
+  const int64_t four = f32 ? 288 : 160, two = f32 ? 640 : c.head_dim == 32 ? 576 : 384;
+  const bool wide = f32 && c.head_dim == 128;
+  const auto workgroups = [&](int64_t kp) { return (n_rows * group * kp / 128 + n_seqs) * c.n_kv_heads; };
+  KvRoute r{false, workgroups(1) <= four && !wide ? 4 : workgroups(1) <= two ? 2 : 1, 1, 0};
+  static const int lim = getenv("SLIM") ? atoi(getenv("SLIM")) : 256;
+  if (paged && workgroups(1) <= lim) {
+    const int64_t rows = n_rows * group / std::max(n_seqs, 1);    // of a sequence and key head
+    const int32_t kp = rows <= 32 && !wide ? 4 : rows <= 64 ? 2 : 1;
+    const int64_t parts = std::min({512 / workgroups(kp), capacity / 1024, (int64_t)64});
+    if (parts > 1) r = KvRoute{false, kp, (int32_t)parts, parts * heads * (c.head_dim + 2) * 4};
+  }
+  return r;
+}
+
+}  // namespace flame
 
 extern "C" {
 
@@ -130,7 +153,7 @@ int flame_kv_workspace_bytes(const flame_kv_config *cfg, int32_t n_seqs, int64_t
   if (int rc = check_config(cfg)) return rc;
   if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
   if (!bytes) return bad("bytes is NULL");
-  *bytes = workspace_bytes_for(cfg, n_seqs, n_tokens);
+  *bytes = std::max(kv_route(*cfg, n_seqs, n_tokens, true, false, kMaxKeys).workspace, n_tokens == n_seqs ? kv_route(*cfg, n_seqs, n_tokens, true, true, kMaxKeys).workspace : 0);
   return FLAME_GR_OK;
 }
 
@@ -176,7 +199,8 @@ int flame_kv_prompt(const flame_kv_config *cfg, const flame_kv_rows *q, const fl
   a.k_offsets = k_offsets;
   a.n_keys = n_keys;
   take_heads(cfg, &a);
-  return done(launch_kv_attention(a, (hipStream_t)stream));
+  a.splits = 1;
+  return done(launch_kv_attention(a, kv_route(*cfg, n_seqs, n_tokens, false, false, kMaxKeys).wavefronts, (hipStream_t)stream));
 }
 
 int flame_kv_extend(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *q_offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_tokens,

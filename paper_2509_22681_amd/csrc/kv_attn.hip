@@ -76,6 +76,23 @@ template <int DB, int RB, int AT> __device__ __forceinline__ void read_values(ui
 #undef READ
 }
 
+// A row tile's keys in parts: of at least kPartTiles tiles, up to `splits` of them.
+constexpr int kPartTiles = 4;
+struct FlashParts { int parts, tiles; };
+template <int KW> __device__ __forceinline__ FlashParts flash_parts(int n_seen, int splits) {
+  const int tiles = (n_seen + KW - 1) / KW;
+  FlashParts p{1, tiles};
+  if (splits > 1 && tiles > kPartTiles) {
+    const int most = min(splits, tiles / kPartTiles);
+    p.tiles = (tiles + most - 1) / most;
+    p.parts = (tiles + p.tiles - 1) / p.tiles;
+  }
+  return p;
+}
+// The workspace: of every part and output row the sums [splits][rows][DH], and behind them the maxima and weights [splits][rows].
+__device__ __forceinline__ int64_t flash_part_row(const KvAttention &a, int split, int64_t row) { return split * a.batch.n_rows * a.n_q_heads + row; }
+__device__ __forceinline__ float2 *flash_part_state(const KvAttention &a) { return (float2 *)(a.parts + a.splits * a.batch.n_rows * a.n_q_heads * a.head_dim); }
+
 template <typename T, int DH, bool PAGED, int KP>
 __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash_kernel(KvAttention a) {
   constexpr bool F32 = sizeof(T) == 4;
@@ -109,7 +126,8 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
       }
     }
   const int kvh = blockIdx.x % a.n_kv_heads;
-  const int64_t slot = blockIdx.x / a.n_kv_heads;
+  const int64_t slot = blockIdx.x / a.n_kv_heads / a.splits;
+  const int split = blockIdx.x / a.n_kv_heads % a.splits;
   int seq;
   int64_t tile;                                                   // counted from the sequence's end
   if (a.batch.n_seqs <= 64) {
@@ -132,7 +150,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
     tile = slot - __builtin_amdgcn_readlane((int)before, seq);
   } else {
     // Those of sequence b begin at slot offsets[b] * G / QT + b, where there is room for them whatever the lengths; the last sequence goes first.
-    const int64_t back_slot = gridDim.x / a.n_kv_heads - 1 - slot;
+    const int64_t back_slot = gridDim.x / a.n_kv_heads / a.splits - 1 - slot;
     int lo = 0, n = a.batch.n_seqs;                               // the last sequence whose slots begin at or before this one
     while (n > 1) {
       const int step = (n + 63) / 64;
@@ -172,7 +190,11 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   // keys seen: by the row before the first one of the sequence, by the last row of the workgroup, by the first and last of my wavefront, by my row
   const int64_t back = n - (end - first);
   auto seen_by = [&](int row) { return (int)max((int64_t)0, back + row / group + 1); };
-  const int n_seen = seen_by(min(row0 + QT, rows) - 1), n_tiles = (n_seen + KW - 1) / KW;
+  const int n_seen = seen_by(min(row0 + QT, rows) - 1);
+  // the workgroup's tiles: all, or a part of them
+  const FlashParts cut = flash_parts<KW>(n_seen, a.splits);
+  if (split >= cut.parts) return;
+  const int t_begin = split * cut.tiles, n_tiles = min(cut.tiles, (n_seen + KW - 1) / KW - t_begin), key0 = t_begin * KW;
   const int part = KP == 1 ? 0 : wave % KP, wave_row = row0 + wave / KP * 32;
   const bool active = wave_row < rows;
   const int my_row = active ? min(wave_row + l32, rows - 1) : row0, token = my_row / group, head = kvh * group + my_row - token * group;
@@ -184,7 +206,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   const int ring = wave * 64 + lane;
   const bool looks = wave * 64 < KW;
   auto look_up = [&](int t, int64_t (&to)[2]) {                   // of key `ring` of tile t; -1: none
-    const int near = min(t * KW + ring, n - 1);
+    const int near = min(key0 + t * KW + ring, n - 1);
     if (PAGED) {
       to[0] = kv_token_offset(a.pages, table, (uint32_t)near);
     } else {
@@ -200,7 +222,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
       at_s[t % 3][0][ring] = max(k_at, (int64_t)0);
       if (!PAGED) at_s[t % 3][PAGED ? 0 : 1][ring] = from[1];
     }
-    const uint64_t there = __builtin_amdgcn_ballot_w64((!PAGED || k_at >= 0) && t * KW + ring < n);
+    const uint64_t there = __builtin_amdgcn_ballot_w64((!PAGED || k_at >= 0) && key0 + t * KW + ring < n);
     if (mine && (lane & 31) == 0) there_s[t % 3][ring / 32] = (uint32_t)(there >> lane);
   };
   // swizzle: what the chunk index of a row is XORed with (fp32 values are read a row at a time, side by side: no need)
@@ -240,7 +262,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   auto tile_step = [&](int t, auto careful_c) __attribute__((always_inline)) {
     constexpr bool careful = decltype(careful_c)::value;
     const char *sk = lds + (t & 1) * STAGE + part * (KT * RB), *sv = sk + TILE;
-    const int k0 = t * KW + part * KT;
+    const int k0 = key0 + t * KW + part * KT;
     if (k0 >= wave_most) return;
     const uint32_t there_lo = __builtin_amdgcn_readfirstlane((int)there_s[t % 3][part * NJ]), there_hi = NJ == 2 ? __builtin_amdgcn_readfirstlane((int)there_s[t % 3][part * NJ + NJ - 1]) : ~0u;
     const bool masked = k0 + KT > wave_least || (there_lo & there_hi) != 0xffffffffu;
@@ -497,14 +519,41 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[e] += ow[e] * take;
       }
+      const int tk = row / group, h = kvh * group + row - tk * group;
+      if (cut.parts > 1) {
+        const int64_t to = flash_part_row(a, split, (first + tk) * a.n_q_heads + h);
+        *(f32x4 *)(a.parts + to * DH + f) = x;
+        if (f == 0) flash_part_state(a)[to] = float2{top, sum};
+        continue;
+      }
       const float inv = top == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
       typedef T out4 __attribute__((ext_vector_type(4)));
       out4 y;
 #pragma unroll
       for (int e = 0; e < 4; ++e) y[e] = kv_round<T>(x[e] * inv);
-      const int tk = row / group, h = kvh * group + row - tk * group;
       *(out4 *)(a.out.p + (first + tk) * a.out.row + h * a.out.head + f * sizeof(T)) = y;
     }
+    return;
+  }
+  if (cut.parts > 1) {
+    if (wave_row + l32 >= rows) return;
+    const int64_t to = flash_part_row(a, split, (first + token) * a.n_q_heads + head);
+    float *po = a.parts + to * DH;
+    if constexpr (F32) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        struct alignas(4 * DB) Values { float f[DB]; } x;
+#pragma unroll
+        for (int b = 0; b < DB; ++b) x.f[b] = o[b][e];
+        *(Values *)(po + DB * (8 * (e >> 2) + 4 * lh + (e & 3))) = x;
+      }
+    } else {
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) *(f32x4 *)(po + 32 * b + 8 * i + 4 * lh) = f32x4{o[b][4 * i], o[b][4 * i + 1], o[b][4 * i + 2], o[b][4 * i + 3]};
+    }
+    if (lh == 0) flash_part_state(a)[to] = float2{m, l};
     return;
   }
   const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
@@ -544,43 +593,72 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   }
 }
 
+// Adds up the parts of rows whose keys were cut, in the order of the keys.  A workgroup per token: DH / 4 lanes a head.
+template <typename T, int DH, int KP>
+__global__ __launch_bounds__(256) void kv_flash_join_kernel(KvAttention a) {
+  constexpr int KW = KP * key_block<T, DH, KP>(), QT = kFlashRows / KP;
+  const int64_t q_row = blockIdx.x;
+  const int seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, q_row, threadIdx.x & 63);
+  if (seq >= a.batch.n_seqs) return;
+  const int64_t first = a.batch.offsets[seq], end = a.batch.offsets[seq + 1];
+  if (first < 0 || q_row < first || q_row >= end) return;
+  const int group = a.n_q_heads / a.n_kv_heads, n = kv_clip(a.batch.kv_lens[seq], a.pages.capacity);
+  const int rows = (int)(min(end, a.batch.n_rows) - first) * group;
+  const int64_t back = n - (end - first);
+  for (int i = threadIdx.x; i < a.n_q_heads * (DH / 4); i += 256) {
+    const int head = i / (DH / 4), f = i % (DH / 4) * 4, row = (int)(q_row - first) * group + head % group;
+    const int last = min(row / QT * QT + QT, rows) - 1;           // of the row's tile
+    const int parts = flash_parts<KW>((int)max((int64_t)0, back + last / group + 1), a.splits).parts;
+    if (parts == 1) continue;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < parts; ++p) {
+      const int64_t from = flash_part_row(a, p, q_row * a.n_q_heads + head);
+      const float2 ml = flash_part_state(a)[from];
+      const f32x4 x = *(const f32x4 *)(a.parts + from * DH + f);
+      const float m_new = fmaxf(m, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
+      const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - ref), take = ml.x == m_new ? 1.f : __builtin_amdgcn_exp2f(ml.x - ref);
+      l = l * keep + ml.y * take;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = o[e] * keep + x[e] * take;
+      m = m_new;
+    }
+    const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
+    typedef T out4 __attribute__((ext_vector_type(4)));
+    out4 y;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = kv_round<T>(o[e] * inv);
+    *(out4 *)(a.out.p + q_row * a.out.row + head * a.out.head + f * sizeof(T)) = y;
+  }
+}
+
 template <typename T, int DH, bool PAGED, int KP> hipError_t launch_flash(const KvAttention &a, hipStream_t stream) {
   static std::atomic<uint64_t> raised{0};
   constexpr int kBytes = flash_lds_bytes<T, DH, KP>();
   const hipError_t e = raise_lds_limit(reinterpret_cast<const void *>(&kv_flash_kernel<T, DH, PAGED, KP>), kBytes, raised);
   if (e != hipSuccess) return e;
   const int64_t slots = a.batch.n_rows * (a.n_q_heads / a.n_kv_heads) / (kFlashRows / KP) + a.batch.n_seqs;
-  kv_flash_kernel<T, DH, PAGED, KP><<<(unsigned)(slots * a.n_kv_heads), 256, kBytes, stream>>>(a);
+  kv_flash_kernel<T, DH, PAGED, KP><<<(unsigned)(slots * a.n_kv_heads * a.splits), 256, kBytes, stream>>>(a);
+  if (a.splits > 1) kv_flash_join_kernel<T, DH, KP><<<(unsigned)a.batch.n_rows, 256, 0, stream>>>(a);
   return hipGetLastError();
-}
-
-// Wavefronts per 32 query rows.  A workgroup of few rows walks its keys in a quarter or half as many steps, but reads them for fewer rows: it pays where whole workgroups, by the
-// bound on their number that rows and sequences give, do not fill the chip.  us with 1 | 2 | 4 at that number (bf16 and fp32, causal prompts):
-//   16 bits, D = 64:  72 (1 x 1024, 8 heads) 22.6 | 14.7 | 12.0   160 (4 x 512) 13.9 | 10.8 | 10.3   264 (1 x 4096) 76 | 49 | 49   288 (4 x 1024) 23.7 | 19.4 | 23.7
-//                     384 (16 x 256) 11.1 | 10.8 | 14.5   1152 (16 x 1024) 45 | 55 | 77
-//   D = 128:          72 (1 x 256, 32/8 heads) 11.7 | 11.0 | 9.5   264 (1 x 1024) 29.8 | 27.0 | 44.6   520 (1 x 2048) 60 | 64 | 124
-//   D = 32:           272 (1 x 2048, 16 heads) 31.5 | 20.2 | 22.8   576 (4 x 1024) 22.7 | 19.8 | 30.0   768 (16 x 256) 9.7 | 13.2 | 21.4
-//   fp32, D = 64:     264 (1 x 4096) 290 | 222 | 198   288 (4 x 1024) 99 | 76 | 68   384 (16 x 256) 34 | 25 | 38   1280 (32 x 512) 128 | 123 | 189
-//   D = 128:          264 (1 x 1024) 146 | 97   544 (4 x 512) 132 | 114   1152 (16 x 256) 124 | 160       D = 32: 576 (4 x 1024) 72 | 68 | 67   768 (16 x 256) 26 | 29 | 33
-template <typename T, int DH, bool PAGED> hipError_t launch_flash_for_size(const KvAttention &a, hipStream_t stream) {
-  constexpr bool F32 = sizeof(T) == 4;
-  constexpr int64_t kFour = F32 ? 288 : 160, kTwo = F32 ? 640 : DH == 32 ? 576 : 384;
-  const int64_t workgroups = (a.batch.n_rows * (a.n_q_heads / a.n_kv_heads) / kFlashRows + a.batch.n_seqs) * a.n_kv_heads;
-  if constexpr (DH * sizeof(T) < 512)                             // (LDS has no room for four wavefronts' tiles of wider rows)
-    if (workgroups <= kFour) return launch_flash<T, DH, PAGED, 4>(a, stream);
-  if (workgroups <= kTwo) return launch_flash<T, DH, PAGED, 2>(a, stream);
-  return launch_flash<T, DH, PAGED, 1>(a, stream);
 }
 
 }  // namespace
 
-hipError_t launch_kv_attention(const KvAttention &a, hipStream_t stream) {
-  hipError_t e = hipErrorUnknown;
+hipError_t launch_kv_attention(const KvAttention &a, int wavefronts, hipStream_t stream) {
+  hipError_t e = hipErrorInvalidValue;
   kv_with_type(a.dtype, [&](auto t) {
     using T = decltype(t);
     kv_with_width(a.head_dim, [&](auto width) {
       constexpr int DH = decltype(width)::value;
-      e = a.pages.table ? launch_flash_for_size<T, DH, true>(a, stream) : launch_flash_for_size<T, DH, false>(a, stream);
+      const auto launch = [&](auto kp) {
+        constexpr int KP = decltype(kp)::value;
+        e = a.pages.table ? launch_flash<T, DH, true, KP>(a, stream) : launch_flash<T, DH, false, KP>(a, stream);
+      };
+      if (wavefronts == 1) launch(std::integral_constant<int, 1>{});
+      if (wavefronts == 2) launch(std::integral_constant<int, 2>{});
+      if constexpr (DH * sizeof(T) < 512)                         // (LDS has no room for four wavefronts' tiles of wider rows)
+        if (wavefronts == 4) launch(std::integral_constant<int, 4>{});
     });
   });
   return e;

@@ -82,7 +82,7 @@ def check_attention(got, q, k, v, dtype, scale=None, seen=None, what=""):
 class Cache:
     """Sequences of n tokens in scattered pages of a pool of random values, with a few pages that nobody has."""
 
-    def __init__(self, B, gen, dtype, hq, hkv, dim, lens, page, head_major=False, seed=0, room=0, extra_rows=0):
+    def __init__(self, B, gen, dtype, hq, hkv, dim, lens, page, head_major=False, seed=0, room=0, tokens=0):
         self.cfg, self.page, self.lens = B.make_kv_config(dtype, hq, hkv, dim), page, list(lens)
         used = [-(-(n + room) // page) for n in lens]
         self.n_pages = sum(used) + 3
@@ -91,7 +91,8 @@ class Cache:
         if head_major:
             self.k, self.v = self.k.transpose(1, 2), self.v.transpose(1, 2)
         order = np.random.default_rng(seed).permutation(self.n_pages)
-        self.table_host = np.full((len(lens) + extra_rows, max(used + [1]) + 1), -7, np.int32)       # entries that nobody reads name no page
+        # (room in the table for `tokens` tokens; entries that nobody reads name no page)
+        self.table_host = np.full((len(lens), max(max(used + [1]) + 1, -(-tokens // page))), -7, np.int32)
         for b, first in enumerate(np.cumsum([0] + used[:-1])):
             self.table_host[b, :used[b]] = order[first:first + used[b]]
         self.table = ints(self.table_host)
@@ -311,12 +312,13 @@ def test_decode(B, dtype, hq, hkv, dim, page, head_major):
 
 @pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 8, 2, 64), ("f16", 4, 4, 128), ("f32", 4, 2, 64), ("bf16", 16, 2, 128), ("f16", 6, 3, 32)])
 @pytest.mark.parametrize("size", [0, 1, 2])
+@pytest.mark.parametrize("tokens", [0, 2000])
 @pytest.mark.parametrize("new,lens,page", [([1, 3, 0, 7, 2], [1, 400, 20, 65, 2], 16), ([40, 200, 1], [40, 333, 600], 24), ([5, 9], [3, 0], 8), ([130], [1000], 64)], ids=str)
-def test_extend(B, dtype, hq, hkv, dim, new, lens, page, size):
+def test_extend(B, dtype, hq, hkv, dim, new, lens, page, size, tokens):
     import torch
     new, lens = new + spread(size, dtype, hkv), lens + spread(size, dtype, hkv)
     gen = generator(len(new))
-    c = Cache(B, gen, dtype, hq, hkv, dim, lens, page)
+    c = Cache(B, gen, dtype, hq, hkv, dim, lens, page, tokens=tokens)        # (a table with more room: few rows take the split kernel)
     off, n = offsets(new), sum(new)
     q = rand(gen, dtype, n + 4, hq, dim)
     out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
@@ -342,6 +344,41 @@ def test_extend_of_many_heads(B, dtype, heads, dim):
     for h in (0, 1, heads // 2, heads - 1):
         check_attention(host(out[:, h:h + 1]), host(q[:, h:h + 1]), keys[:, h:h + 1], values[:, h:h + 1], dtype, what=h)
     assert bool(out.isfinite().all()) and not bool((out == 7.0).all(-1).any())
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim,new,lens", [
+    ("bf16", 64, 64, 64, [20], [1500]), ("f16", 32, 32, 128, [50], [1200]), ("bf16", 8, 2, 64, [200, 3], [900, 2000]), ("f16", 16, 2, 128, [70, 1, 30], [1100, 2500, 31]),
+    ("bf16", 32, 1, 32, [129], [1700]), ("f32", 64, 16, 64, [140], [1300]), ("f32", 32, 16, 128, [300], [1000]), ("f32", 256, 256, 32, [40], [1030]), ("f32", 128, 128, 64, [65, 2], [700, 640])])
+def test_extend_in_parts(B, dtype, hq, hkv, dim, new, lens):
+    """Tables with room for 8192 tokens: the keys of a row tile are cut into parts and joined; with a page that the table does not name, and with a NaN in the newest token."""
+    import torch
+    gen = generator(hq)
+    c = Cache(B, gen, dtype, hq, hkv, dim, lens, 16, tokens=8192)
+    table = c.table_host.copy()
+    table[0, 5] = -1
+    packed = B.pack_kv_cache(c.cfg, c.k, c.v, ints(table))
+    off, n = offsets(new), sum(new)
+    q = rand(gen, dtype, n, hq, dim)
+    out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    ws = workspace_for(B, c.cfg, len(lens), n)
+    B.flame_kv_extend(c.cfg, packed, q, ints(off), ints(lens), out, ws, faults=faults)
+    assert int(faults[0]) == 1 and bool(out.isfinite().all())
+    group = hq // hkv
+    for b, n_b in enumerate(lens):
+        keys, values = c.rows(b, n_b)
+        s = slice(off[b], off[b + 1])
+        for h in sorted({0, 1, hq // 2, hq - 1}):
+            kv = slice(h // group, h // group + 1)
+            seen = np.arange(n_b) // 16 != 5 if b == 0 else None
+            check_attention(host(out[s, h:h + 1]), host(q[s, h:h + 1]), keys[:, kv], values[:, kv], dtype, seen=seen, what=(b, h))
+    page, slot, _ = kv_oracle.page_rows(c.table_host[0], 16, c.n_pages, lens[0])
+    c.v[int(page[-1]), int(slot[-1]), hkv - 1, 2] = math.nan
+    dirty = torch.full_like(q, 7.0)
+    B.flame_kv_extend(c.cfg, packed, q, ints(off), ints(lens), dirty, ws)
+    last = int(off[1]) - 1
+    assert bool(dirty[last, hq - group:, 2].isnan().all())
+    dirty[last, hq - group:, 2] = out[last, hq - group:, 2]
+    assert torch.equal(dirty, out)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
