@@ -118,17 +118,23 @@ namespace flame {
 // into parts.  The host knows rows and sequences, but of the keys only what the page table has room for.
 KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool paged, bool decode, int64_t capacity) {
   const bool f32 = c.dtype == FLAME_KV_F32;
-  const int64_t group = c.n_q_heads / c.n_kv_heads, heads = n_rows * c.n_q_heads;
-  if (decode || (paged && capacity > 1024 && heads <= (f32 ? 8192 : 1024))) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim)};
+  const int64_t group = c.n_q_heads / c.n_kv_heads, heads = n_rows * c.n_q_heads, rows = n_rows * group / std::max(n_seqs, 1);   // rows: of a sequence and key head
+  // The split kernel reads the keys again for every 16 rows, and has no masked rows to carry.  us split | flash in parts, at rows times heads and room for the tokens there are (bf16):
+  //   64 (4 x 2 new, 8/2 heads of 64) 4096: 14 | 18, 16384: 19 | 24    256 (8 new, 32/8 of 128) 26 | 28, 34 | 48    1024 (16 x 2 new, 32/8) 59 | 71, 221 | 265
+  //   1024 (4 x 8 new, 32/8) 34 | 34, 82 | 64    1024 (16 x 8 new, 8/2) 29 | 21, 58 | 37    4096 (128 new, 32/8) 71 | 46, 209 | 83
+  //   fp32: 1024 (32 new, 32/8) 49 | 165, 129 | 187    4096 (4 x 32 new, 32/8) 138 | 172, 499 | 362    room for 512: 1024 (4 x 8 new, 32/8) 21 | 13
+  if (decode || (paged && capacity > 1024 && heads <= (f32 ? 2048 : rows < 16 ? 1024 : 512))) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim)};
   const int64_t four = f32 ? 288 : 160, two = f32 ? 640 : c.head_dim == 32 ? 576 : 384;
   const bool wide = f32 && c.head_dim == 128;
   const auto workgroups = [&](int64_t kp) { return (n_rows * group * kp / 128 + n_seqs) * c.n_kv_heads; };
   KvRoute r{false, workgroups(1) <= four && !wide ? 4 : workgroups(1) <= two ? 2 : 1, 1, 0};
-  static const int lim = getenv("SLIM") ? atoi(getenv("SLIM")) : 256;
-  if (paged && workgroups(1) <= lim) {
-    const int64_t rows = n_rows * group / std::max(n_seqs, 1);    // of a sequence and key head
+  // Parts of at least 512 tokens' room, as many as make one round of the chip's 512 places or two of them full, by the number of workgroups that sequences of equal rows would have.
+  // us whole | in parts (bf16, 32/8 heads of 128): 1 x 128 new over 4096 53 | 43, over 16384 217 | 78; 4 x 128 over 4096 123 | 61, over 16384 531 | 244; 16 x 32 over 16384 469 | 271;
+  // 8/2 heads of 64: 4 x 512 over 4096 50 | 45.  (With 25 parts in place of 16, one and a half rounds, 1 x 128 over 16384 takes 104.)
+  if (paged && workgroups(1) <= 400) {
     const int32_t kp = rows <= 32 && !wide ? 4 : rows <= 64 ? 2 : 1;
-    const int64_t parts = std::min({512 / workgroups(kp), capacity / 1024, (int64_t)64});
+    const int64_t likely = n_seqs * ((rows * kp + 127) / 128) * c.n_kv_heads;
+    const int64_t parts = std::min({(likely > 256 ? 1024 : 512) / std::max(likely, (int64_t)1), capacity / 512, (int64_t)64});
     if (parts > 1) r = KvRoute{false, kp, (int32_t)parts, parts * heads * (c.head_dim + 2) * 4};
   }
   return r;
