@@ -129,28 +129,31 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   const int64_t slot = blockIdx.x / a.n_kv_heads / a.splits;
   const int split = blockIdx.x / a.n_kv_heads % a.splits;
   int seq;
-  int64_t tile;                                                   // counted from the sequence's end
+  int64_t tile, first, end;                                       // tile: counted from the sequence's end
   if (a.batch.n_seqs <= 64) {
     // One lane per sequence: the tiles of those that come before it.
     int64_t tiles = 0;
-    int keys = -1;
+    int b = 0, e = 0, keys = -1;
     if (lane < a.batch.n_seqs) {
-      const int64_t b = a.batch.offsets[lane], e = a.batch.offsets[lane + 1];
-      tiles = b < 0 ? 0 : (max((int64_t)0, min(e, a.batch.n_rows) - b) * group + QT - 1) / QT;
-      keys = PAGED ? a.batch.kv_lens[lane] : (int)(e - b);
+      b = a.batch.offsets[lane];
+      e = a.batch.offsets[lane + 1];
+      tiles = b < 0 ? 0 : ((int64_t)max(0, (int)min((int64_t)e, a.batch.n_rows) - b) * group + QT - 1) / QT;
+      keys = PAGED ? a.batch.kv_lens[lane] : (int)((int64_t)e - b);
     }
-    int64_t before = 0;
+    int before = 0;
     for (int j = 0; j < a.batch.n_seqs; ++j) {
       const int other = __builtin_amdgcn_readlane(keys, j);
-      before += other > keys || (other == keys && j < lane) ? (int64_t)__builtin_amdgcn_readlane((int)tiles, j) : 0;
+      before += other > keys || (other == keys && j < lane) ? __builtin_amdgcn_readlane((int)tiles, j) : 0;
     }
     const uint64_t mine = __builtin_amdgcn_ballot_w64(slot >= before && slot < before + tiles);
     if (!mine) return;
     seq = __builtin_ctzll(mine);
-    tile = slot - __builtin_amdgcn_readlane((int)before, seq);
+    tile = slot - __builtin_amdgcn_readlane(before, seq);
+    first = __builtin_amdgcn_readlane(b, seq);
+    end = __builtin_amdgcn_readlane(e, seq);
   } else {
     // Those of sequence b begin at slot offsets[b] * G / QT + b, where there is room for them whatever the lengths; the last sequence goes first.
-    const int64_t back_slot = gridDim.x / a.n_kv_heads / a.splits - 1 - slot;
+  const int64_t back_slot = gridDim.x / a.n_kv_heads / a.splits - 1 - slot;
     int lo = 0, n = a.batch.n_seqs;                               // the last sequence whose slots begin at or before this one
     while (n > 1) {
       const int step = (n + 63) / 64;
@@ -161,11 +164,11 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
       n = max(1, min(step, n - c * step));
     }
     seq = min(lo, a.batch.n_seqs - 1);
-    const int64_t b = a.batch.offsets[seq], e = a.batch.offsets[seq + 1];
-    const int64_t tiles = (max((int64_t)0, min(e, a.batch.n_rows) - b) * group + QT - 1) / QT;
-    tile = tiles - 1 - (back_slot - (b * group / QT + seq));
+    first = a.batch.offsets[seq];
+    end = a.batch.offsets[seq + 1];
+    const int64_t tiles = (max((int64_t)0, min(end, a.batch.n_rows) - first) * group + QT - 1) / QT;
+    tile = tiles - 1 - (back_slot - (first * group / QT + seq));
   }
-  const int64_t first = a.batch.offsets[seq], end = a.batch.offsets[seq + 1];
   if (first < 0 || end < first) return;
   const int rows = (int)max((int64_t)0, min(end, a.batch.n_rows) - first) * group;
   const int row_tiles = (rows + QT - 1) / QT;

@@ -33,7 +33,7 @@ template <typename T, int DH> struct SplitShape {
 
 // What a wavefront knows of a sequence.
 struct SplitSeq {
-  int64_t first;      // its first query row
+  int first;          // its first query row
   int rows, blocks;   // query rows times G, and units per key head
   int n, back;        // keys; keys that the row before the first one would see
   int tiles;          // of one unit
@@ -46,7 +46,7 @@ template <int KT> __device__ __forceinline__ SplitSeq split_sequence(const KvAtt
   s.first = b;
   if (a.batch.offsets) {
     const int64_t first = a.batch.offsets[b], end = a.batch.offsets[b + 1];
-    s.first = first;
+    s.first = (int)first;
     full = end - first;
     const bool wrong = first < 0 || full < 0 || end > a.batch.n_rows;
     if (wrong && report) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
@@ -58,6 +58,12 @@ template <int KT> __device__ __forceinline__ SplitSeq split_sequence(const KvAtt
   s.blocks = (s.rows + kRows - 1) / kRows;
   s.tiles = s.rows ? max(1, (s.n + KT - 1) / KT) : 0;   // (a unit without keys writes zeros)
   return s;
+}
+
+// Of up to 64 sequences each lane keeps one; of more they are read again.
+__device__ __forceinline__ SplitSeq split_from_lane(const SplitSeq &s, int lane) {
+  return SplitSeq{__builtin_amdgcn_readlane(s.first, lane), __builtin_amdgcn_readlane(s.rows, lane), __builtin_amdgcn_readlane(s.blocks, lane),
+                  __builtin_amdgcn_readlane(s.n, lane), __builtin_amdgcn_readlane(s.back, lane), __builtin_amdgcn_readlane(s.tiles, lane)};
 }
 
 __device__ __forceinline__ int64_t split_scan(int64_t v) {        // inclusive sums over the wavefront
@@ -84,10 +90,11 @@ __device__ __forceinline__ int64_t split_lane(int64_t v, int lane) {
 struct SplitPlace {
   int64_t total, first_tile;
   int seq;
+  SplitSeq mine;      // the lane's sequence, of up to 64
 };
 
 template <int KT, typename F> __device__ __forceinline__ SplitPlace split_find(const KvAttention &a, int lane, F target) {
-  SplitPlace p{0, 0, a.batch.n_seqs};
+  SplitPlace p{0, 0, a.batch.n_seqs, SplitSeq{}};
   int lo = 0, n = a.batch.n_seqs;
   int64_t base = 0, at = 0;
   for (bool top = true;; top = false) {
@@ -98,6 +105,7 @@ template <int KT, typename F> __device__ __forceinline__ SplitPlace split_find(c
       if (k >= n) break;
       const SplitSeq s = split_sequence<KT>(a, lo + k, top && blockIdx.x == 0 && threadIdx.x < 64);
       mine += (int64_t)s.blocks * s.tiles;
+      if (top) p.mine = s;
     }
     mine *= a.n_kv_heads;
     const int64_t sums = split_scan(mine);
@@ -170,7 +178,7 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
   int64_t seq_tile = place.first_tile;
   bool begins = true;                                             // the unit is the worker's first
   while (tile < tile_end && seq < a.batch.n_seqs) {
-    SplitSeq s = split_sequence<KT>(a, seq, false);
+    const SplitSeq s = a.batch.n_seqs <= 64 ? split_from_lane(place.mine, seq) : split_sequence<KT>(a, seq, false);
     int64_t in_seq = tile - seq_tile;
     const int64_t seq_tiles = (int64_t)a.n_kv_heads * s.blocks * s.tiles;
     if (in_seq >= seq_tiles) {                                    // (sequences without rows have none)
@@ -409,24 +417,40 @@ __global__ __launch_bounds__(256) void kv_join_kernel(KvAttention a, const float
   const int group = a.n_q_heads / a.n_kv_heads;
   const int q_row = blockIdx.x / a.n_q_heads;
   const int head = blockIdx.x - q_row * a.n_q_heads, kvh = head / group;
+  // Which sequence, its shape, the tiles of all units and of the sequences before this one.
   int seq = q_row;
-  if (a.batch.offsets) {
-    seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, q_row, lane);
-    if (seq >= a.batch.n_seqs) return;
-  }
-  const SplitSeq s = split_sequence<KT>(a, seq, false);
-  const int row = (int)(q_row - s.first) * group + head - kvh * group;
-  if (q_row < s.first || row >= s.rows) return;
-  // tiles of all units and of the sequences before this one
+  SplitSeq s{};
   int64_t total = 0, before = 0;
-  for (int b = lane; b < a.batch.n_seqs; b += 64) {
-    const SplitSeq x = split_sequence<KT>(a, b, false);
-    const int64_t tiles = (int64_t)x.blocks * x.tiles;
-    total += tiles;
-    before += b < seq ? tiles : 0;
+  if (a.batch.n_seqs <= 64) {
+    SplitSeq mine{};
+    int end = 0;
+    if (lane < a.batch.n_seqs) {
+      mine = split_sequence<KT>(a, lane, false);
+      end = a.batch.offsets ? a.batch.offsets[lane + 1] : 0;
+    }
+    if (a.batch.offsets) seq = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.batch.n_seqs && end <= q_row));
+    if (seq >= a.batch.n_seqs) return;
+    s = split_from_lane(mine, seq);
+    const int64_t tiles = (int64_t)mine.blocks * mine.tiles, sums = split_scan(tiles);
+    total = split_lane(sums, 63);
+    before = split_lane(sums, seq) - split_lane(tiles, seq);
+  } else {
+    if (a.batch.offsets) seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, q_row, lane);
+    if (seq >= a.batch.n_seqs) return;
+    s = split_sequence<KT>(a, seq, false);
+    for (int b = lane; b < a.batch.n_seqs; b += 64) {
+      const SplitSeq x = split_sequence<KT>(a, b, false);
+      const int64_t tiles = (int64_t)x.blocks * x.tiles;
+      total += tiles;
+      before += b < seq ? tiles : 0;
+    }
+    total = split_lane(split_scan(total), 63);
+    before = split_lane(split_scan(before), 63);
   }
-  total = split_lane(split_scan(total), 63) * a.n_kv_heads;
-  before = split_lane(split_scan(before), 63) * a.n_kv_heads;
+  total *= a.n_kv_heads;
+  before *= a.n_kv_heads;
+  const int row = (q_row - s.first) * group + head - kvh * group;
+  if (q_row < s.first || row >= s.rows) return;
   const int64_t per = (total + split_workers(DH) - 1) / split_workers(DH);
   const int64_t first = before + (int64_t)(kvh * s.blocks + row / kRows) * s.tiles, last = first + s.tiles - 1;
   const int w0 = (int)(first / per), w1 = (int)(last / per);
