@@ -54,6 +54,6 @@ hipError_t launch_kv_append(const KvBatch &batch, const KvPages &pages, const Kv
 hipError_t launch_kv_attention(const KvAttention &a, int wavefronts, hipStream_t stream);
 // few query rows: split over the keys (kv_split.hip)
 hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream);
-int64_t kv_split_workspace_bytes(int32_t head_dim);
+int64_t kv_split_workspace_bytes(int32_t head_dim, int64_t rows);   // rows times heads
 
 }  // namespace flame

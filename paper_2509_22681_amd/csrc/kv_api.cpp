@@ -23,6 +23,7 @@ int done(hipError_t e) {
 // A grid dimension may have 2^32 - 1 threads.  Attention of packed rows has two of them per row and head, and 256 per sequence and head; split attention, of one row per
 // sequence or of few in all, 256 per row and head.
 constexpr int64_t kMaxRowHeads = (int64_t)1 << 25, kMaxSequenceHeads = ((int64_t)1 << 23) - 1;
+constexpr int64_t kSmallCache = 1024;                          // tokens that a sequence has room for, up to which its keys are not split over the chip
 constexpr int64_t kMaxKeys = ((int64_t)1 << 31) - 65536;     // of a sequence: room for a tile's end behind them in 32 bits
 
 int64_t element(int32_t dtype) { return dtype == FLAME_KV_F32 ? 4 : 2; }
@@ -91,6 +92,11 @@ void take_heads(const flame_kv_config *c, KvAttention *a) {
   a->scale = c->scale == 0.f ? 1.f / std::sqrt((float)c->head_dim) : c->scale;
 }
 
+// What any cache may need: one of little room may go by another route than a large one.
+int64_t workspace_bytes_for(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool decode) {
+  return std::max(kv_route(c, n_seqs, n_rows, true, decode, kMaxKeys).workspace, kv_route(c, n_seqs, n_rows, true, decode, kSmallCache).workspace);
+}
+
 int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_rows,
                  const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream) {
   KvAttention a{};
@@ -99,7 +105,7 @@ int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const 
   if (int rc = take_pages(cfg, cache, &a.pages)) return rc;
   if (!kv_lens) return bad("kv_lens is NULL");
   const KvRoute route = kv_route(*cfg, n_seqs, n_rows, true, offsets == nullptr, a.pages.capacity);
-  const int64_t need = kv_route(*cfg, n_seqs, n_rows, true, offsets == nullptr, kMaxKeys).workspace;
+  const int64_t need = workspace_bytes_for(*cfg, n_seqs, n_rows, offsets == nullptr);
   if (need > 0 && (!workspace || !aligned(workspace))) return bad("the workspace is NULL or not 16-byte aligned");
   if (workspace_bytes < need) return bad("the workspace is smaller than flame_kv_workspace_bytes", FLAME_GR_CAPACITY_EXCEEDED);
   a.batch = KvBatch{offsets, kv_lens, n_seqs, n_rows, faults};
@@ -123,7 +129,7 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   //   64 (4 x 2 new, 8/2 heads of 64) 4096: 14 | 18, 16384: 19 | 24    256 (8 new, 32/8 of 128) 26 | 28, 34 | 48    1024 (16 x 2 new, 32/8) 59 | 71, 221 | 265
   //   1024 (4 x 8 new, 32/8) 34 | 34, 82 | 64    1024 (16 x 8 new, 8/2) 29 | 21, 58 | 37    4096 (128 new, 32/8) 71 | 46, 209 | 83
   //   fp32: 1024 (32 new, 32/8) 49 | 165, 129 | 187    4096 (4 x 32 new, 32/8) 138 | 172, 499 | 362    room for 512: 1024 (4 x 8 new, 32/8) 21 | 13
-  if (decode || (paged && capacity > 1024 && heads <= (f32 ? 2048 : rows < 16 ? 1024 : 512))) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim)};
+  if (decode || (paged && capacity > kSmallCache && heads <= (f32 ? 2048 : rows < 16 ? 1024 : 512))) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim, heads)};
   const int64_t four = f32 ? 288 : 160, two = f32 ? 640 : c.head_dim == 32 ? 576 : 384;
   const bool wide = f32 && c.head_dim == 128;
   const auto workgroups = [&](int64_t kp) { return (n_rows * group * kp / 128 + n_seqs) * c.n_kv_heads; };
@@ -159,7 +165,7 @@ int flame_kv_workspace_bytes(const flame_kv_config *cfg, int32_t n_seqs, int64_t
   if (int rc = check_config(cfg)) return rc;
   if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
   if (!bytes) return bad("bytes is NULL");
-  *bytes = std::max(kv_route(*cfg, n_seqs, n_tokens, true, false, kMaxKeys).workspace, n_tokens == n_seqs ? kv_route(*cfg, n_seqs, n_tokens, true, true, kMaxKeys).workspace : 0);
+  *bytes = std::max(workspace_bytes_for(*cfg, n_seqs, n_tokens, false), n_tokens == n_seqs ? workspace_bytes_for(*cfg, n_seqs, n_tokens, true) : 0);
   return FLAME_GR_OK;
 }
 

@@ -14,6 +14,8 @@
 //     transposition within its own registers (byte permutes of word pairs), feature D/16 * m + j in product j.
 // A unit that ends within its wavefront is written; the others leave maximum, sum and unnormalised rows in the workspace, for a second kernel that
 // adds up a unit's parts in the order of their keys.  Every part and every join has a fixed order: the same call gives the same bits.
+#include <algorithm>
+
 #include "kv_device.h"
 
 namespace flame {
@@ -98,14 +100,29 @@ template <int KT, typename F> __device__ __forceinline__ SplitPlace split_find(c
   int lo = 0, n = a.batch.n_seqs;
   int64_t base = 0, at = 0;
   for (bool top = true;; top = false) {
-    const int chunk = (n + 63) / 64;
+    // lane i: the tiles of `chunk` sequences from lo + i chunk on, of one sequence in the end
+    const bool report = top && blockIdx.x == 0 && threadIdx.x < 64;
     int64_t mine = 0;
-    for (int i = 0; i < chunk; ++i) {
-      const int k = lane * chunk + i;
-      if (k >= n) break;
-      const SplitSeq s = split_sequence<KT>(a, lo + k, top && blockIdx.x == 0 && threadIdx.x < 64);
-      mine += (int64_t)s.blocks * s.tiles;
-      if (top) p.mine = s;
+    int chunk = 1;
+    if (n <= 64) {
+      if (lane < n) {
+        const SplitSeq s = split_sequence<KT>(a, lo + lane, report);
+        mine = (int64_t)s.blocks * s.tiles;
+        if (top) p.mine = s;
+      }
+    } else {
+      // the wavefront reads 64 neighbours at a time
+      chunk = (n + 4095) / 4096 * 64;
+      for (int i = 0; i * chunk < n; ++i) {
+        int64_t sum = 0;
+        for (int k = lane; k < chunk; k += 64) {
+          if (i * chunk + k >= n) break;
+          const SplitSeq s = split_sequence<KT>(a, lo + i * chunk + k, report);
+          sum += (int64_t)s.blocks * s.tiles;
+        }
+        const int64_t all = split_lane(split_scan(sum), 63);
+        if (lane == i) mine = all;
+      }
     }
     mine *= a.n_kv_heads;
     const int64_t sums = split_scan(mine);
@@ -120,7 +137,7 @@ template <int KT, typename F> __device__ __forceinline__ SplitPlace split_find(c
     base += split_lane(sums, l) - split_lane(mine, l);
     lo += l * chunk;
     n = min(chunk, n - l * chunk);
-    if (n <= 1) {
+    if (chunk == 1) {
       p.seq = lo;
       p.first_tile = base;
       return p;
@@ -129,7 +146,9 @@ template <int KT, typename F> __device__ __forceinline__ SplitPlace split_find(c
 }
 
 // Parts of a worker: the one it begins with, and one that goes on behind its end.
-template <int DH> __host__ __device__ constexpr int split_part_floats() { return kRows * DH + 2 * kRows; }
+constexpr int split_part_floats(int dh) { return kRows * dh + 2 * kRows; }
+// The workspace: the parts [workers][2], and behind them for every output row which workers have its parts (the first one twice, plus 1 if its part there is the second; the last one).
+constexpr int64_t split_parts_floats(int dh) { return (int64_t)split_workers(dh) * 2 * split_part_floats(dh); }
 
 __device__ __forceinline__ float split_max(float v) {             // over the four lanes that share a query row
   const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -377,6 +396,10 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
       }
     }
     l = split_sum(l);
+    if (t0 == 0 && row_there && g == 0) {
+      const int last = t1 == s.tiles ? worker : (int)((tile + s.tiles - 1) / per);
+      ((int2 *)(parts + split_parts_floats(DH)))[(int64_t)(s.first + token) * a.n_q_heads + head] = int2{2 * worker + !begins, last};
+    }
     // accumulator element e of product j: feature VF (4 g + e) + j of my row (fp32 with 128 features: 4 (4 g + e) + j % 4 of half j / 4)
     auto feature = [&](int e, int j) { return VB == 32 ? 64 * (j >> 2) + 4 * (4 * g + e) + (j & 3) : VF * (4 * g + e) + j; };
     if (t0 == 0 && t1 == s.tiles) {
@@ -390,7 +413,7 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
           for (int j = 0; j < VF; ++j) out[feature(e, j)] = kv_round<T>(nothing ? 0.f : o[j][e] * inv);
       }
     } else if (row_there) {
-      float *part = parts + ((int64_t)worker * 2 + (begins ? 0 : 1)) * split_part_floats<DH>();
+      float *part = parts + ((int64_t)worker * 2 + (begins ? 0 : 1)) * split_part_floats(DH);
       if (g == 0) {
         part[l16] = m;
         part[kRows + l16] = l;
@@ -406,102 +429,89 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
   }
 }
 
-// One workgroup per query row and head: adds up the parts of its unit, if it was cut.  Bound by latency: DH / 4 lanes share a part, so that
+// Adds up the parts of the query rows and heads whose units were cut; a workgroup looks at `rows` of them.  Bound by latency: DH / 4 lanes share a part, so that
 // 8 to 32 parts are read at once.
 template <typename T, int DH>
-__global__ __launch_bounds__(256) void kv_join_kernel(KvAttention a, const float *__restrict__ parts) {
-  constexpr int KT = SplitShape<T, DH>::KT;
+__global__ __launch_bounds__(256) void kv_join_kernel(KvAttention a, const float *__restrict__ parts, int rows) {
   constexpr int L = DH / 4, P = 256 / L;                          // lanes of a part, parts at once
   __shared__ float m_s[P], l_s[P], o_s[P][DH + 4];
   const int lane = threadIdx.x & 63;
   const int group = a.n_q_heads / a.n_kv_heads;
-  const int q_row = blockIdx.x / a.n_q_heads;
-  const int head = blockIdx.x - q_row * a.n_q_heads, kvh = head / group;
-  // Which sequence, its shape, the tiles of all units and of the sequences before this one.
-  int seq = q_row;
-  SplitSeq s{};
-  int64_t total = 0, before = 0;
-  if (a.batch.n_seqs <= 64) {
-    SplitSeq mine{};
-    int end = 0;
-    if (lane < a.batch.n_seqs) {
-      mine = split_sequence<KT>(a, lane, false);
-      end = a.batch.offsets ? a.batch.offsets[lane + 1] : 0;
+  const int64_t first_row = (int64_t)blockIdx.x * rows;           // rows here are rows times heads
+  int2 of = {0, 0};
+  const int64_t mine = first_row + lane;
+  bool cut = lane < rows && mine < a.batch.n_rows * a.n_q_heads;
+  if (cut) of = ((const int2 *)(parts + split_parts_floats(DH)))[mine];
+  int start = cut ? (int)(mine / a.n_q_heads) : 0;                // the first row of the row's sequence
+  if (a.batch.offsets) {
+    // Rows that no sequence has were left as they were, and so was what is here about them.
+    for (int i = 0; i < rows; ++i) {
+      const int64_t row = (first_row + i) / a.n_q_heads;
+      const int seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, row, lane);
+      const int64_t first = seq < a.batch.n_seqs ? a.batch.offsets[seq] : -1;
+      if (lane == i) {
+        cut &= first >= 0 && row >= first;
+        start = (int)first;
+      }
     }
-    if (a.batch.offsets) seq = __builtin_popcountll(__builtin_amdgcn_ballot_w64(lane < a.batch.n_seqs && end <= q_row));
-    if (seq >= a.batch.n_seqs) return;
-    s = split_from_lane(mine, seq);
-    const int64_t tiles = (int64_t)mine.blocks * mine.tiles, sums = split_scan(tiles);
-    total = split_lane(sums, 63);
-    before = split_lane(sums, seq) - split_lane(tiles, seq);
-  } else {
-    if (a.batch.offsets) seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, q_row, lane);
-    if (seq >= a.batch.n_seqs) return;
-    s = split_sequence<KT>(a, seq, false);
-    for (int b = lane; b < a.batch.n_seqs; b += 64) {
-      const SplitSeq x = split_sequence<KT>(a, b, false);
-      const int64_t tiles = (int64_t)x.blocks * x.tiles;
-      total += tiles;
-      before += b < seq ? tiles : 0;
-    }
-    total = split_lane(split_scan(total), 63);
-    before = split_lane(split_scan(before), 63);
   }
-  total *= a.n_kv_heads;
-  before *= a.n_kv_heads;
-  const int row = (q_row - s.first) * group + head - kvh * group;
-  if (q_row < s.first || row >= s.rows) return;
-  const int64_t per = (total + split_workers(DH) - 1) / split_workers(DH);
-  const int64_t first = before + (int64_t)(kvh * s.blocks + row / kRows) * s.tiles, last = first + s.tiles - 1;
-  const int w0 = (int)(first / per), w1 = (int)(last / per);
-  if (w0 == w1) return;                                           // it was not cut
-  const int r = row % kRows, p = threadIdx.x / L, f = threadIdx.x % L * 4;
-  const bool later = first > (int64_t)w0 * per;                   // in the first worker it is not the unit that the worker begins with
-  float m = -INFINITY, l = 0.f;
-  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  cut &= of.x >> 1 < of.y && of.x >= 0 && of.y < split_workers(DH);
+  for (uint64_t left = __builtin_amdgcn_ballot_w64(cut); left; left &= left - 1) {
+    const int which = __builtin_ctzll(left);
+    const int code = __builtin_amdgcn_readlane(of.x, which), w0 = code >> 1, w1 = __builtin_amdgcn_readlane(of.y, which);
+    const int64_t q_row = (first_row + which) / a.n_q_heads;
+    const int head = (int)(first_row + which - q_row * a.n_q_heads);
+    const int r = (((int)q_row - __builtin_amdgcn_readlane(start, which)) * group + head % group) % kRows, p = threadIdx.x / L, f = threadIdx.x % L * 4;
+    float m = -INFINITY, l = 0.f;
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int w = w0 + p; w <= w1; w += P) {
-    const float *part = parts + ((int64_t)w * 2 + (w == w0 && later ? 1 : 0)) * split_part_floats<DH>();
-    const float mw = part[r], lw = part[kRows + r];
-    const f32x4 ow = *(const f32x4 *)(part + 2 * kRows + r * DH + f);
-    const float m_new = fmaxf(m, mw), m_at = m_new == -INFINITY ? 0.f : m_new;
-    const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_at), take = mw == m_new ? 1.f : __builtin_amdgcn_exp2f(mw - m_at);
-    l = l * keep + lw * take;
+    for (int w = w0 + p; w <= w1; w += P) {
+      const float *part = parts + ((int64_t)w * 2 + (w == w0 ? code & 1 : 0)) * split_part_floats(DH);
+      const float mw = part[r], lw = part[kRows + r];
+      const f32x4 ow = *(const f32x4 *)(part + 2 * kRows + r * DH + f);
+      const float m_new = fmaxf(m, mw), m_at = m_new == -INFINITY ? 0.f : m_new;
+      const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_at), take = mw == m_new ? 1.f : __builtin_amdgcn_exp2f(mw - m_at);
+      l = l * keep + lw * take;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[i] = o[i] * keep + ow[i] * take;
-    m = m_new;
+      for (int i = 0; i < 4; ++i) o[i] = o[i] * keep + ow[i] * take;
+      m = m_new;
+    }
+    *(f32x4 *)&o_s[p][f] = o;
+    if (f == 0) { m_s[p] = m; l_s[p] = l; }
+    __syncthreads();
+    if (threadIdx.x < DH) {
+      float top = -INFINITY, sum = 0.f, out = 0.f;
+#pragma unroll
+      for (int i = 0; i < P; ++i) top = fmaxf(top, m_s[i]);
+      const float at = top == -INFINITY ? 0.f : top;
+#pragma unroll
+      for (int i = 0; i < P; ++i) {
+        const float take = m_s[i] == top ? 1.f : __builtin_amdgcn_exp2f(m_s[i] - at);
+        sum += l_s[i] * take;
+        out += o_s[i][threadIdx.x] * take;
+      }
+      ((T *)(a.out.p + (int64_t)q_row * a.out.row + head * a.out.head))[threadIdx.x] = kv_round<T>(top == -INFINITY && sum == 0.f ? 0.f : out / sum);
+    }
+    __syncthreads();
   }
-  *(f32x4 *)&o_s[p][f] = o;
-  if (f == 0) { m_s[p] = m; l_s[p] = l; }
-  __syncthreads();
-  if (threadIdx.x >= DH) return;
-  float top = -INFINITY, sum = 0.f, out = 0.f;
-#pragma unroll
-  for (int i = 0; i < P; ++i) top = fmaxf(top, m_s[i]);
-  const float at = top == -INFINITY ? 0.f : top;
-#pragma unroll
-  for (int i = 0; i < P; ++i) {
-    const float take = m_s[i] == top ? 1.f : __builtin_amdgcn_exp2f(m_s[i] - at);
-    sum += l_s[i] * take;
-    out += o_s[i][threadIdx.x] * take;
-  }
-  ((T *)(a.out.p + (int64_t)q_row * a.out.row + head * a.out.head))[threadIdx.x] = kv_round<T>(top == -INFINITY && sum == 0.f ? 0.f : out / sum);
 }
 
 }  // namespace
 
-int64_t kv_split_workspace_bytes(int32_t head_dim) {
-  return (int64_t)split_workers(head_dim) * 2 * 4 * (head_dim == 32 ? split_part_floats<32>() : head_dim == 64 ? split_part_floats<64>() : split_part_floats<128>());
+int64_t kv_split_workspace_bytes(int32_t head_dim, int64_t rows) {
+  return split_parts_floats(head_dim) * 4 + (rows + 1) / 2 * 16;
 }
 
 hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream) {
-  const unsigned joins = (unsigned)(a.batch.n_rows * a.n_q_heads);
+  // A workgroup of the join per row and head up to 16384 (most of more are not cut: there are no more cut units than wavefronts), and no more of them than lanes.
+  const int64_t joins = a.batch.n_rows * a.n_q_heads;
+  const int rows = (int)std::min((joins + 16383) / 16384, (int64_t)64);
   kv_with_type(a.dtype, [&](auto t) {
     using T = decltype(t);
     kv_with_width(a.head_dim, [&](auto width) {
       constexpr int DH = decltype(width)::value;
       kv_split_kernel<T, DH><<<split_workers(DH) / 4, 256, 0, stream>>>(a, (float *)workspace);
-      kv_join_kernel<T, DH><<<joins, 256, 0, stream>>>(a, (const float *)workspace);
+      kv_join_kernel<T, DH><<<(unsigned)((joins + rows - 1) / rows), 256, 0, stream>>>(a, (const float *)workspace, rows);
     });
   });
   return hipGetLastError();

@@ -106,7 +106,7 @@ class Cache:
 
 def spread(n, dtype, hkv):
     """Sequences without tokens behind the others, that make a launch count as a larger one: the forms with four, two and one wavefront per 32 rows (thresholds in
-    kv_attn.hip: 160 and 384 or 576 workgroups, fp32 288 and 640)."""
+    kv_api.cpp: 160 and 384 or 576 workgroups, fp32 288 and 640)."""
     return [0] * (0 if n == 0 else (300 if dtype != "f32" else 450) // hkv if n == 1 else 700 // hkv + 1)
 
 
@@ -308,6 +308,79 @@ def test_decode(B, dtype, hq, hkv, dim, page, head_major):
     assert int(faults[0]) == 0
     for b, n in enumerate(lens):
         check_attention(host(out[b:b + 1]), host(q[b:b + 1]), *c.rows(b, n), dtype, what=(b, n))
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim,n_seqs", [("bf16", 8, 2, 64, 65), ("f16", 4, 1, 128, 200), ("bf16", 8, 2, 32, 4200), ("f32", 4, 4, 32, 5000), ("f16", 32, 2, 64, 700)])
+def test_decode_of_many_sequences(B, dtype, hq, hkv, dim, n_seqs):
+    """More sequences than lanes, and more rows of heads than workgroups of the join; some of them long, so that their keys are cut."""
+    import torch
+    gen, rng = generator(n_seqs), np.random.default_rng(n_seqs)
+    lens = rng.integers(0, 30, n_seqs)
+    long = [0, 1, n_seqs // 2, n_seqs - 1]
+    lens[long] = [3000, 700, 1999, 4001]
+    c = Cache(B, gen, dtype, hq, hkv, dim, lens.tolist(), 16)
+    q = rand(gen, dtype, n_seqs, hq, dim)
+    out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kv_decode(c.cfg, c.packed, q, ints(lens), out, workspace_for(B, c.cfg, n_seqs), faults=faults)
+    assert int(faults[0]) == 0 and not bool((out == 7.0).all(-1).any())
+    pool_k, pool_v, got, want = host(c.k), host(c.v), host(out), host(q)
+    for b in long + rng.integers(0, n_seqs, 60).tolist():
+        page, slot, _ = kv_oracle.page_rows(c.table_host[b], c.page, c.n_pages, int(lens[b]))
+        check_attention(got[b:b + 1], want[b:b + 1], pool_k[page, slot], pool_v[page, slot], dtype, what=(b, int(lens[b])))
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim,n_seqs", [("bf16", 4, 1, 64, 70), ("f16", 2, 2, 128, 300), ("f32", 4, 2, 32, 90), ("bf16", 2, 1, 32, 4500)])
+@pytest.mark.parametrize("paged", [False, True])
+def test_many_ragged_sequences(B, dtype, hq, hkv, dim, n_seqs, paged):
+    """More sequences than lanes, of zero to 300 rows each, on row tiles: packed, and over caches."""
+    import torch
+    gen, rng = generator(n_seqs), np.random.default_rng(n_seqs)
+    new = rng.integers(0, 20, n_seqs)
+    new[rng.integers(0, n_seqs, n_seqs // 4)] = 0
+    new[[0, n_seqs // 3, n_seqs - 1]] = [300, 129, 40]
+    lens = new + (rng.integers(0, 70, n_seqs) if paged else 0)
+    off, n = offsets(new), int(new.sum())
+    q = rand(gen, dtype, n + 5, hq, dim)
+    out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    if paged:
+        c = Cache(B, gen, dtype, hq, hkv, dim, lens.tolist(), 16)
+        B.flame_kv_extend(c.cfg, c.packed, q, ints(off), ints(lens), out, workspace_for(B, c.cfg, n_seqs, n + 5), faults=faults)
+        pool_k, pool_v = host(c.k), host(c.v)
+    else:
+        k, v = rand(gen, dtype, n, hkv, dim), rand(gen, dtype, n, hkv, dim)
+        B.flame_kv_prompt(B.make_kv_config(dtype, hq, hkv, dim), q, k, v, ints(off), out, faults=faults)
+        pool_k, pool_v = host(k), host(v)
+    assert int(faults[0]) == 0 and bool((out[n:] == 7.0).all()) and not bool((out[:n] == 7.0).all(-1).any())
+    got, want = host(out), host(q)
+    for b in [0, n_seqs // 3, n_seqs - 1] + rng.integers(0, n_seqs, 40).tolist():
+        s = slice(off[b], off[b + 1])
+        if paged:
+            page, slot, _ = kv_oracle.page_rows(c.table_host[b], c.page, c.n_pages, int(lens[b]))
+            check_attention(got[s], want[s], pool_k[page, slot], pool_v[page, slot], dtype, what=(int(b), int(lens[b])))
+        else:
+            check_attention(got[s], want[s], pool_k[s], pool_v[s], dtype, what=int(b))
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim,n_seqs", [("bf16", 4, 2, 64, 130), ("f32", 4, 1, 32, 300), ("f16", 2, 2, 128, 5000)])
+def test_extend_of_many_sequences(B, dtype, hq, hkv, dim, n_seqs):
+    """Few new tokens in all, of more sequences than lanes (most of which have none), split over the keys; with rows behind the last sequence."""
+    import torch
+    gen, rng = generator(n_seqs), np.random.default_rng(n_seqs)
+    new, lens = np.zeros(n_seqs, np.int64), rng.integers(0, 30, n_seqs)
+    some = np.unique(rng.integers(0, n_seqs, 60))
+    new[some] = rng.integers(1, 4, some.size)
+    lens[some] += rng.choice([0, 5, 900, 1500], some.size)
+    c = Cache(B, gen, dtype, hq, hkv, dim, lens.tolist(), 16, tokens=2000)
+    off, n = offsets(new), int(new.sum())
+    q = rand(gen, dtype, n + 3, hq, dim)
+    out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kv_extend(c.cfg, c.packed, q, ints(off), ints(lens), out, workspace_for(B, c.cfg, n_seqs, n + 3), faults=faults)
+    assert int(faults[0]) == 0 and bool((out[n:] == 7.0).all())
+    pool_k, pool_v, got, want = host(c.k), host(c.v), host(out), host(q)
+    for b in some:
+        page, slot, _ = kv_oracle.page_rows(c.table_host[b], c.page, c.n_pages, int(lens[b]))
+        s = slice(off[b], off[b + 1])
+        check_attention(got[s], want[s], pool_k[page, slot], pool_v[page, slot], dtype, what=(int(b), int(lens[b])))
 
 
 @pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 8, 2, 64), ("f16", 4, 4, 128), ("f32", 4, 2, 64), ("bf16", 16, 2, 128), ("f16", 6, 3, 32)])
