@@ -20,8 +20,8 @@ int done(hipError_t e) {
   return bad(hipGetErrorString(e), FLAME_GR_HIP_ERROR);
 }
 
-// A grid dimension may have 2^32 - 1 threads.  Attention of packed rows has two of them per row and head, and 256 per sequence and head; split attention, of one row per
-// sequence or of few in all, 256 per row and head.
+// A grid dimension may have 2^32 - 1 threads.  Attention on row tiles has two of them per row and head, and 256 per sequence and head; the join of split attention has up to 2^22,
+// and 256 per 64 rows and heads where those are more than 2^20.
 constexpr int64_t kMaxRowHeads = (int64_t)1 << 25, kMaxSequenceHeads = ((int64_t)1 << 23) - 1;
 constexpr int64_t kSmallCache = 1024;                          // tokens that a sequence has room for, up to which its keys are not split over the chip
 constexpr int64_t kMaxKeys = ((int64_t)1 << 31) - 65536;     // of a sequence: room for a tile's end behind them in 32 bits
@@ -125,11 +125,22 @@ namespace flame {
 KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool paged, bool decode, int64_t capacity) {
   const bool f32 = c.dtype == FLAME_KV_F32;
   const int64_t group = c.n_q_heads / c.n_kv_heads, heads = n_rows * c.n_q_heads, rows = n_rows * group / std::max(n_seqs, 1);   // rows: of a sequence and key head
-  // The split kernel reads the keys again for every 16 rows, and has no masked rows to carry.  us split | flash in parts, at rows times heads and room for the tokens there are (bf16):
-  //   64 (4 x 2 new, 8/2 heads of 64) 4096: 14 | 18, 16384: 19 | 24    256 (8 new, 32/8 of 128) 26 | 28, 34 | 48    1024 (16 x 2 new, 32/8) 59 | 71, 221 | 265
-  //   1024 (4 x 8 new, 32/8) 34 | 34, 82 | 64    1024 (16 x 8 new, 8/2) 29 | 21, 58 | 37    4096 (128 new, 32/8) 71 | 46, 209 | 83
-  //   fp32: 1024 (32 new, 32/8) 49 | 165, 129 | 187    4096 (4 x 32 new, 32/8) 138 | 172, 499 | 362    room for 512: 1024 (4 x 8 new, 32/8) 21 | 13
-  if (decode || (paged && capacity > kSmallCache && heads <= (f32 ? 2048 : rows < 16 ? 1024 : 512))) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim, heads)};
+  // The split kernel reads the keys again for every 16 rows of a sequence and key head; up to there it reads them once, whatever the sequences' lengths, and carries no masked rows.
+  // us split | row tiles, in parts where there are few, by rows of a sequence and key head and by rows times heads; 16-bit:
+  //   up to 16 rows: 1024 (64 sequences x 2 new, 8/2 heads of 64, over 2048) 25 | 29, 2048 (16 x 4, 32/8 of 128, over 2048) 40 | 48, (over 8192) 128 | 126, 4096 (64 x 2, 32/8, over 2048) 128 | 108;
+  //     of more than 64 sequences, which the row tiles do not sort by length: 6400 (200 x 4, 8/2 of 64, over 100..8192) 118 | 230, (over 2048) 62 | 54
+  //   more: 256 (8 new, 32/8, over 4096) 26 | 28, (over 16384) 34 | 48, 1024 (4 x 8, 32/8) 34 | 34, 82 | 64, 4096 (128 new, 32/8) 71 | 46, 209 | 83
+  // fp32: up to 32 rows: 2048 (16 x 4, 32/8, over 2048) 65 | 117, 16384 (64 x 8, 32/8, over 2048) 301 | 401; more: 1024 (32 new, 32/8, over 4096) 49 | 165,
+  //   4096 (4 x 32, 32/8, over 4096) 138 | 172, (over 16384) 499 | 362.  Room for 512 tokens: 1024 (4 x 8, 32/8) 21 | 13
+  const int64_t few = f32 ? (rows <= 32 ? 16384 : 2048) : rows > 16 ? 512 : n_seqs > 64 ? 8192 : 2048;
+  if (decode || (paged && capacity > kSmallCache && heads <= few)) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim, heads)};
+  // Four or two wavefronts share 32 rows where that many workgroups of one wavefront per 32 rows leave the chip's 512 places empty.  us with one | two | four, at that many workgroups
+  // (prompts x tokens); 16-bit, 64 features: 72 (1 x 1024, 8 heads) 23 | 15 | 12, 160 (4 x 512) 14 | 11 | 10, 264 (1 x 4096) 76 | 49 | 49, 288 (4 x 1024) 24 | 19 | 24,
+  //   384 (16 x 256) 11 | 11 | 15, 1152 (16 x 1024) 45 | 55 | 77
+  //   128 features, 32/8 heads: 72 (1 x 256) 12 | 11 | 10, 264 (1 x 1024) 30 | 27 | 45, 520 (1 x 2048) 60 | 64 | 124
+  //   32 features, 16 heads: 272 (1 x 2048) 32 | 20 | 23, 576 (4 x 1024) 23 | 20 | 30, 768 (16 x 256) 10 | 13 | 21
+  // fp32, 64 features: 264 (1 x 4096) 290 | 222 | 198, 288 (4 x 1024) 99 | 76 | 68, 384 (16 x 256) 34 | 25 | 38, 1280 (32 x 512) 128 | 123 | 189
+  //   128 features: 264 146 | 97, 544 132 | 114, 1152 124 | 160;  32 features: 576 72 | 68 | 67, 768 26 | 29 | 33
   const int64_t four = f32 ? 288 : 160, two = f32 ? 640 : c.head_dim == 32 ? 576 : 384;
   const bool wide = f32 && c.head_dim == 128;
   const auto workgroups = [&](int64_t kp) { return (n_rows * group * kp / 128 + n_seqs) * c.n_kv_heads; };

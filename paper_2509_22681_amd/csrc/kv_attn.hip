@@ -6,7 +6,7 @@
 // A workgroup takes 128 query rows of one sequence and key head, row = token * G + head of the
 // group (the G query heads that share a key head are rows of one tile: short sequences fill it, and the mask cuts through fewer key tiles), four wavefronts of 32 rows each.  It
 // walks the keys in tiles of 64, two stages in LDS, brought there by LDS-DMA loads one tile ahead.  In small launches two or four wavefronts share 32 rows and take a part of each
-// tile's keys, with a maximum, sum and accumulator of their own that are joined at the end (launch_flash_for_size).  Products are transposed as in attn_mfma.hip,
+// tile's keys, with a maximum, sum and accumulator of their own that are joined at the end (kv_route in kv_api.cpp).  Products are transposed as in attn_mfma.hip,
 //     S^T[key][row] = K Q^T        A operand = K rows, B operand = Q rows
 //     O^T[feature][row] += V^T P^T A operand = V^T rows, B operand = P^T
 // so that the first product's accumulator, where a lane has one row and 16 of 32 keys, is the second product's B operand as it stands: elements 8 s + i of a lane in half h are keys
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
     end = __builtin_amdgcn_readlane(e, seq);
   } else {
     // Those of sequence b begin at slot offsets[b] * G / QT + b, where there is room for them whatever the lengths; the last sequence goes first.
-  const int64_t back_slot = gridDim.x / a.n_kv_heads / a.splits - 1 - slot;
+    const int64_t back_slot = gridDim.x / a.n_kv_heads / a.splits - 1 - slot;
     int lo = 0, n = a.batch.n_seqs;                               // the last sequence whose slots begin at or before this one
     while (n > 1) {
       const int step = (n + 63) / 64;
