@@ -687,6 +687,81 @@ def test_other_streams_and_a_padded_batch(B):
     check_attention(host(out[3:5]), host(q[3:5]), *c.rows(2, 45), "f16")
 
 
+@pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 8, 2, 64), ("f16", 4, 4, 128), ("f32", 4, 1, 32), ("f32", 3, 3, 128)])
+def test_strided_rows(B, dtype, hq, hkv, dim):
+    """Queries, keys and values as slices of one projection's rows, outputs as a slice of wider rows and head by head: what lies beside them stays."""
+    import torch
+    gen, new, lens = generator(14), [40, 1, 9], [1500, 60, 9]
+    off, n = offsets(new), sum(new)
+    rows = rand(gen, dtype, n, hq + 2 * hkv + 1, dim)
+    q, k, v = rows[:, :hq], rows[:, hq:hq + hkv], rows[:, hq + hkv:hq + 2 * hkv]
+    for head_major in (False, True):
+        for room in (0, 4096):                                          # row tiles whole, in parts or split
+            c = Cache(B, gen, dtype, hq, hkv, dim, lens, 16, head_major, tokens=room)
+            for kind in ("prompt", "extend", "decode"):
+                m = 3 if kind == "decode" else n
+                wide = torch.full((hq + 2, m, dim) if head_major else (m, hq + 2, dim), 7.0, dtype=q.dtype, device=DEV)
+                out = (wide.transpose(0, 1) if head_major else wide)[:, 1:hq + 1]
+                if kind == "prompt":
+                    B.flame_kv_prompt(c.cfg, q, k, v, ints(off), out)
+                elif kind == "extend":
+                    B.flame_kv_extend(c.cfg, c.packed, q, ints(off), ints(lens), out, workspace_for(B, c.cfg, 3, n))
+                else:
+                    B.flame_kv_decode(c.cfg, c.packed, q[:3], ints(lens), out, workspace_for(B, c.cfg, 3))
+                beside = wide.transpose(0, 1) if head_major else wide
+                assert bool((beside[:, 0] == 7.0).all()) and bool((beside[:, -1] == 7.0).all())
+                for b, n_b in enumerate(lens):
+                    rows_b = slice(b, b + 1) if kind == "decode" else slice(off[b], off[b + 1])
+                    keys, values = (host(k[rows_b]), host(v[rows_b])) if kind == "prompt" else c.rows(b, n_b)
+                    check_attention(host(out[rows_b]), host(q[rows_b]), keys, values, dtype, what=(kind, head_major, room, b))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("empty", [0, 100])
+@pytest.mark.parametrize("off", [[0, 40, 20, 60], [-5, 40, 50, 60], [0, 30, 90, 90], [0, 30, 2 ** 31 - 1, 60], [70, 80, 90, 2 ** 31 - 1], [0, -2 ** 31, 2 ** 31 - 1, 60]], ids=str)
+def test_offsets_that_are_none(B, dtype, empty, off):
+    """Offsets that decrease, begin below 0 or end behind the rows are reported, and nothing is written outside the 60 rows (on row tiles, in parts, split; of up to 64
+    sequences and of more).  A first sequence that is one has its rows."""
+    import torch
+    gen, lens = generator(15), [900, 60, 90] + [0] * empty
+    off = off + [off[-1]] * empty
+    fault = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for room, hq in ((0, 4), (4096, 64), (4096, 2)):
+        c = Cache(B, gen, dtype, hq, hq, 64, lens, 16, tokens=room)
+        q, k = rand(gen, dtype, 60, hq, 64), rand(gen, dtype, 60, hq, 64)
+        for kind in ("prompt", "extend"):
+            buffer = torch.full((180, hq, 64), 7.0, dtype=q.dtype, device=DEV)
+            out = buffer[60:120]
+            fault.zero_()
+            if kind == "prompt":
+                B.flame_kv_prompt(c.cfg, q, k, k, ints(off), out, faults=fault)
+            else:
+                B.flame_kv_extend(c.cfg, c.packed, q, ints(off), ints(lens), out, workspace_for(B, c.cfg, len(lens), 60), faults=fault)
+            assert int(fault[0]) == 4, (kind, room)
+            assert bool((buffer[:60] == 7.0).all()) and bool((buffer[120:] == 7.0).all())
+            if off[:2] == [0, 30]:
+                keys, values = (host(k[:30]), host(k[:30])) if kind == "prompt" else c.rows(0, 900)
+                check_attention(host(out[:30, :1]), host(q[:30, :1]), keys[:, :1], values[:, :1], dtype, what=(kind, room, hq))
+
+
+def test_two_calls_at_once(B):
+    """Calls on two streams that share a cache, each with a workspace of its own."""
+    import torch
+    gen, lens = generator(16), [5000, 3000]
+    c = Cache(B, gen, "bf16", 8, 2, 64, lens, 16)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    q = [rand(gen, "bf16", 2, 8, 64) for _ in streams]
+    out, ws, n = [torch.empty_like(x) for x in q], [workspace_for(B, c.cfg, 2) for _ in streams], ints(lens)
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, stream in enumerate(streams):
+            B.flame_kv_decode(c.cfg, c.packed, q[i], n, out[i], ws[i], stream=stream)
+    torch.cuda.synchronize()
+    for i in (0, 1):
+        for b, n_b in enumerate(lens):
+            check_attention(host(out[i][b:b + 1]), host(q[i][b:b + 1]), *c.rows(b, n_b), "bf16", what=(i, b))
+
+
 def test_the_same_call_gives_the_same_bits(B):
     """The same call twice gives the same bits, at sizes where the work is split and joined."""
     import torch
