@@ -141,9 +141,10 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   //   384 (16 x 256) 11 | 11 | 15, 1152 (16 x 1024) 45 | 55 | 77
   //   128 features, 32/8 heads: 72 (1 x 256) 12 | 11 | 10, 264 (1 x 1024) 30 | 27 | 45, 520 (1 x 2048) 60 | 64 | 124
   //   32 features, 16 heads: 272 (1 x 2048) 32 | 20 | 23, 576 (4 x 1024) 23 | 20 | 30, 768 (16 x 256) 10 | 13 | 21
-  // fp32, 64 features: 264 (1 x 4096) 290 | 222 | 198, 288 (4 x 1024) 99 | 76 | 68, 384 (16 x 256) 34 | 25 | 38, 1280 (32 x 512) 128 | 123 | 189
-  //   128 features: 264 146 | 97, 544 132 | 114, 1152 124 | 160;  32 features: 576 72 | 68 | 67, 768 26 | 29 | 33
-  const int64_t four = f32 ? 288 : 160, two = f32 ? 640 : c.head_dim == 32 ? 576 : 384;
+  // fp32, 64 features: 136 (1 x 2048) 148 | 87 | 59, 160 (4 x 512) 42 | 27 | 30, 264 (1 x 4096) 290 | 171 | 200, 288 (4 x 1024) 79 | 52 | 70, 384 (16 x 256) 26 | 22 | 43,
+  //   560 (32 x 257..640) 79 | 76, 596 (16 x 300..2048) 191 | 143, 1280 (32 x 512) 128 | 150
+  //   128 features: 264 (1 x 1024) 145 | 95, 520 (1 x 2048) 287 | 327;  32 features: 144 (1 x 1024) 47 | 27 | 20, 320 (4 x 512) 26 | 20, 576 (4 x 1024) 53 | 60, 768 (16 x 256) 23 | 30
+  const int64_t four = f32 ? 150 : 160, two = f32 ? (c.head_dim == 64 ? 640 : 512) : c.head_dim == 32 ? 576 : 384;
   const bool wide = f32 && c.head_dim == 128;
   const auto workgroups = [&](int64_t kp) { return (n_rows * group * kp / 128 + n_seqs) * c.n_kv_heads; };
   KvRoute r{false, workgroups(1) <= four && !wide ? 4 : workgroups(1) <= two ? 2 : 1, 1, 0};

@@ -125,9 +125,16 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
         kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
       }
     }
-  const int kvh = blockIdx.x % a.n_kv_heads;
-  const int64_t slot = blockIdx.x / a.n_kv_heads / a.splits;
-  const int split = blockIdx.x / a.n_kv_heads % a.splits;
+  // A compute unit holds two workgroups, of which the first 256 and the next are neighbours: the second half goes the other way round, so that a long one has a short one beside it
+  // (4 prompts of 2048, 8/2 heads of 64: 50 -> 40 us, fp32 4 of 1024, 16 heads of 32: 69 -> 60; launches of many more are as before).
+  unsigned block = blockIdx.x;
+  if (flash_workgroups<T, DH, KP>() == 2) {
+    const unsigned placed = min(gridDim.x, 512u);
+    if (block >= 256 && block < placed) block = 256 + placed - 1 - block;
+  }
+  const int kvh = block % a.n_kv_heads;
+  const int64_t slot = block / a.n_kv_heads / a.splits;
+  const int split = block / a.n_kv_heads % a.splits;
   int seq;
   int64_t tile, first, end;                                       // tile: counted from the sequence's end
   if (a.batch.n_seqs <= 64) {
