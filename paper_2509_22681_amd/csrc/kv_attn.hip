@@ -36,8 +36,12 @@ template <typename T, int DH, int KP> constexpr int flash_lds_bytes() {
   constexpr int stages = 4 * KP * key_block<T, DH, KP>() * DH * (int)sizeof(T), parts = KP == 1 ? 0 : 4 * 32 * (DH + 6) * 4;
   return stages > parts ? stages : parts;
 }
-// Workgroups of 4 wavefronts on a compute unit.
-template <typename T, int DH, int KP> constexpr int flash_workgroups() { return flash_lds_bytes<T, DH, KP>() > 72 * 1024 ? 1 : 2; }
+// Workgroups of 4 wavefronts on a compute unit, as LDS and registers allow (three in place of two of heads of 64: 64 prompts of 512..1024, 8 heads, 142 -> 114 us, one of 16384 395 -> 352;
+// four in place of three of 32 features 185 -> 165, fp32 three in place of two 622 -> 561).
+template <typename T, int DH, int KP> constexpr int flash_workgroups() {
+  constexpr int lds = flash_lds_bytes<T, DH, KP>();
+  return lds > 72 * 1024 ? 1 : DH == 32 && sizeof(T) == 2 && lds <= 32 * 1024 ? 4 : DH * sizeof(T) <= 128 && lds <= 40 * 1024 ? 3 : 2;
+}
 
 template <typename T> struct Matrix32;              // (fp32 products are 32x32x2: the third dimension is the lane's half)
 template <> struct Matrix32<bf16_t> {
@@ -125,10 +129,10 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
         kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
       }
     }
-  // A compute unit holds two workgroups, of which the first 256 and the next are neighbours: the second half goes the other way round, so that a long one has a short one beside it
+  // Of a compute unit's workgroups, one is of the first 256 and one of the next: those go the other way round, so that a long one has a short one beside it
   // (4 prompts of 2048, 8/2 heads of 64: 50 -> 40 us, fp32 4 of 1024, 16 heads of 32: 69 -> 60; launches of many more are as before).
   unsigned block = blockIdx.x;
-  if (flash_workgroups<T, DH, KP>() == 2) {
+  if (flash_workgroups<T, DH, KP>() >= 2) {
     const unsigned placed = min(gridDim.x, 512u);
     if (block >= 256 && block < placed) block = 256 + placed - 1 - block;
   }
@@ -207,8 +211,8 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   const int t_begin = split * cut.tiles, n_tiles = min(cut.tiles, (n_seen + KW - 1) / KW - t_begin), key0 = t_begin * KW;
   const int part = KP == 1 ? 0 : wave % KP, wave_row = row0 + wave / KP * 32;
   const bool active = wave_row < rows;
-  const int my_row = active ? min(wave_row + l32, rows - 1) : row0, token = my_row / group, head = kvh * group + my_row - token * group;
-  const int sees = seen_by(my_row), wave_least = active ? seen_by(wave_row) : 0, wave_most = active ? seen_by(min(wave_row + 31, rows - 1)) : 0;
+  auto my_row = [&]() { return active ? min(wave_row + l32, rows - 1) : row0; };
+  const int sees = seen_by(my_row()), wave_least = active ? seen_by(wave_row) : 0, wave_most = active ? seen_by(min(wave_row + 31, rows - 1)) : 0;
 
   typedef __attribute__((address_space(1))) const void gvoid;
   typedef __attribute__((address_space(3))) void lvoid;
@@ -255,6 +259,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   typedef uint32_t word4 __attribute__((ext_vector_type(4)));
   word4 fq[KS];
   {
+    const int row = my_row(), token = row / group, head = kvh * group + row - token * group;
     const char *q = a.q.p + (first + token) * a.q.row + head * a.q.head;
 #pragma unroll
     for (int s = 0; s < KS; ++s) fq[s] = *(const word4 *)(q + s * 32 + lh * 16);
@@ -547,7 +552,8 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   }
   if (cut.parts > 1) {
     if (wave_row + l32 >= rows) return;
-    const int64_t to = flash_part_row(a, split, (first + token) * a.n_q_heads + head);
+    const int row = wave_row + l32, tk = row / group;
+    const int64_t to = flash_part_row(a, split, (first + tk) * a.n_q_heads + kvh * group + row - tk * group);
     float *po = a.parts + to * DH;
     if constexpr (F32) {
 #pragma unroll
