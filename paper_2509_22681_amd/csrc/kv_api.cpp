@@ -136,14 +136,14 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   // Room for 512 tokens, bf16: 1024 (4 x 8, 32/8) 21 | 13
   const int64_t few = f32 ? (rows <= 32 ? 16384 : 1024) : rows > 32 ? 0 : rows > 16 ? 512 : n_seqs > 64 ? 8192 : 2048;
   if (decode || (paged && capacity > kSmallCache && heads <= few)) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim, heads)};
-  // Four or two wavefronts share 32 rows where that many workgroups of one wavefront per 32 rows leave the chip's 512 places empty.  us with one | two | four, at that many workgroups
-  // (prompts x tokens); 16-bit, 64 features: 72 (1 x 1024, 8 heads) 23 | 15 | 12, 160 (4 x 512) 14 | 11 | 10, 264 (1 x 4096) 76 | 49 | 49, 288 (4 x 1024) 24 | 19 | 24,
-  //   384 (16 x 256) 11 | 11 | 15, 1152 (16 x 1024) 45 | 55 | 77
-  //   128 features, 32/8 heads: 72 (1 x 256) 12 | 11 | 10, 264 (1 x 1024) 30 | 27 | 45, 520 (1 x 2048) 60 | 64 | 124
-  //   32 features, 16 heads: 272 (1 x 2048) 32 | 20 | 23, 576 (4 x 1024) 23 | 20 | 30, 768 (16 x 256) 10 | 13 | 21
-  // fp32, 64 features: 136 (1 x 2048) 148 | 87 | 59, 160 (4 x 512) 42 | 27 | 30, 264 (1 x 4096) 290 | 171 | 200, 288 (4 x 1024) 79 | 52 | 70, 384 (16 x 256) 26 | 22 | 43,
-  //   560 (32 x 257..640) 79 | 76, 596 (16 x 300..2048) 191 | 143, 1280 (32 x 512) 128 | 150
-  //   128 features: 264 (1 x 1024) 145 | 95, 520 (1 x 2048) 287 | 327;  32 features: 144 (1 x 1024) 47 | 27 | 20, 320 (4 x 512) 26 | 20, 576 (4 x 1024) 53 | 60, 768 (16 x 256) 23 | 30
+  // Four or two wavefronts share 32 rows where that many workgroups of one wavefront per 32 rows leave places of the chip empty, or all are placed at
+  // once and wait for the longest.  us with one | two | four, at that many workgroups
+  // (prompts x tokens); 16-bit, 64 features: 72 (1 x 1024, 8 heads) 22 | 16 | 12, 160 (4 x 512) 14 | 11 | 10, 264 (1 x 4096) 74 | 48 | 49, 288 (4 x 1024) 23 | 18 | 23,
+  //   384 (16 x 256) 11 | 12 | 17, 528 (2 x 4096) 75 | 66, 544 (4 x 2048) 41 | 45, 1152 (16 x 1024) 45 | 61 | 86
+  //   128 features, 32/8 heads: 72 (1 x 256) 12 | 11 | 10, 264 (1 x 1024) 30 | 26 | 45, 520 (1 x 2048) 57 | 62 | 128;  32 features, 16 heads: 272 (1 x 2048) 32 | 20 | 22, 576 (4 x 1024) 20 | 21 | 32
+  // fp32, 64 features: 136 (1 x 2048) 148 | 87 | 57, 160 (4 x 512) 42 | 27 | 30, 264 (1 x 4096) 290 | 171 | 200, 288 (4 x 1024) 79 | 52 | 70, 384 (16 x 256) 26 | 23 | 43,
+  //   560 (32 x 257..640, 4 heads) 76 | 76, 596 (16 x 300..2048) 190 | 143, 1280 (32 x 512) 129 | 150
+  //   128 features: 264 (1 x 1024) 145 | 95, 520 (1 x 2048) 287 | 327;  32 features: 144 (1 x 1024) 46 | 27 | 20, 320 (4 x 512) 27 | 20 | 27, 576 (4 x 1024) 53 | 60
   const int64_t four = f32 ? 150 : 160, two = f32 ? (c.head_dim == 64 ? 640 : 512) : c.head_dim == 32 ? 576 : 384;
   const bool wide = f32 && c.head_dim == 128;
   const auto workgroups = [&](int64_t kp) { return (n_rows * group * kp / 128 + n_seqs) * c.n_kv_heads; };

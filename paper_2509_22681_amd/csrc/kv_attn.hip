@@ -1,7 +1,7 @@
 // Causal softmax attention of packed query rows with grouped heads, over packed keys or a paged cache.
 //
-// Bound by the matrix pipe and the vector work of the softmax beside it, and in the end by power: one prompt of 32768, 16/2 heads of 128, bf16, runs at 0.97 PFLOP/s and a clock of
-// 2.0 GHz, with the matrix pipe busy 47 % of the cycles (a plain matrix product of 8192 reaches 1.22 PFLOP/s on this chip).  Forms with fewer cycles ran at a lower clock in the same time.
+// Bound by the matrix pipe and the vector work of the softmax beside it, and in the end by power: one prompt of 32768, 16/2 heads of 128, bf16, runs at 1.0 PFLOP/s (4.4 ms) and a clock of
+// 2.0 GHz, with the matrix pipe busy 48 % of the cycles (a plain matrix product of 8192 reaches 1.22 PFLOP/s on this chip).  Forms with fewer cycles ran at a lower clock in the same time.
 //
 // A workgroup takes 128 query rows of one sequence and key head, row = token * G + head of the
 // group (the G query heads that share a key head are rows of one tile: short sequences fill it, and the mask cuts through fewer key tiles), four wavefronts of 32 rows each.  It
