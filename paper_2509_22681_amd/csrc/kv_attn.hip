@@ -141,6 +141,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   const int split = block / a.n_kv_heads % a.splits;
   int seq;
   int64_t tile, first, end;                                       // tile: counted from the sequence's end
+  int kv_len = 0;
   if (a.batch.n_seqs <= 64) {
     // One lane per sequence: the tiles of those that come before it.
     int64_t tiles = 0;
@@ -162,6 +163,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
     tile = slot - __builtin_amdgcn_readlane(before, seq);
     first = __builtin_amdgcn_readlane(b, seq);
     end = __builtin_amdgcn_readlane(e, seq);
+    if (PAGED) kv_len = __builtin_amdgcn_readlane(keys, seq);
   } else {
     // Those of sequence b begin at slot offsets[b] * G / QT + b, where there is room for them whatever the lengths; the last sequence goes first.
     const int64_t back_slot = gridDim.x / a.n_kv_heads / a.splits - 1 - slot;
@@ -177,6 +179,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
     seq = min(lo, a.batch.n_seqs - 1);
     first = a.batch.offsets[seq];
     end = a.batch.offsets[seq + 1];
+    if (PAGED) kv_len = a.batch.kv_lens[seq];
     const int64_t tiles = (max((int64_t)0, min(end, a.batch.n_rows) - first) * group + QT - 1) / QT;
     tile = tiles - 1 - (back_slot - (first * group / QT + seq));
   }
@@ -190,13 +193,16 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   const char *kp, *vp;
   const int32_t *table = nullptr;
   if (PAGED) {
-    n = kv_clip(a.batch.kv_lens[seq], a.pages.capacity);
+    n = kv_clip(kv_len, a.pages.capacity);
     kp = a.pages.k + kvh * a.pages.head;
     vp = a.pages.v + kvh * a.pages.head;
     table = a.pages.table + seq * a.pages.table_stride;
   } else {
-    const int32_t *ko = a.k_offsets ? a.k_offsets : a.batch.offsets;
-    const int64_t k_first = ko[seq], k_end = ko[seq + 1];
+    int64_t k_first = first, k_end = end;
+    if (a.k_offsets) {
+      k_first = a.k_offsets[seq];
+      k_end = a.k_offsets[seq + 1];
+    }
     n = k_first < 0 ? 0 : (int)max((int64_t)0, min(k_end, a.n_keys) - k_first);
     kp = a.k.p + k_first * a.k.row + kvh * a.k.head;
     vp = a.v.p + k_first * a.v.row + kvh * a.v.head;
