@@ -148,13 +148,15 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   const bool wide = f32 && c.head_dim == 128;
   const auto workgroups = [&](int64_t kp) { return (n_rows * group * kp / 128 + n_seqs) * c.n_kv_heads; };
   KvRoute r{false, workgroups(1) <= four && !wide ? 4 : workgroups(1) <= two ? 2 : 1, 1, 0};
-  // Parts of at least 512 tokens' room, as many as make one round of the chip's 512 places or two of them full, by the number of workgroups that sequences of equal rows would have.
+  // Where there is room for 1024 tokens: parts of at least 256, more than 32 of at least 512, as many as make one round of the chip's 512 places or two of them full, by the number of workgroups that sequences of equal rows would have.
   // us whole | in parts and joined (bf16, 32/8 heads of 128): 1 x 128 new over 4096 53 | 36, over 16384 217 | 63; 4 x 128 over 16384 531 | 204; 16 x 32 over 16384 469 | 275;
-  // 8/2 heads of 64: 4 x 512 over 4096 50 | 50.  (25 parts in place of 16, one and a half rounds, cost 1 x 128 over 16384 26 us more.)
-  if (paged && workgroups(1) <= 400) {
+  // 8/2 heads of 64: 4 x 512 over 4096 50 | 50.  (25 parts in place of 16, one and a half rounds, cost 1 x 128 over 16384 26 us more.
+  // Parts of 512 | 256: fp32, 32/8 heads of 128, 3 x 163 over 1277 185 | 142, 6/2 of 128 101 | 54, bf16 44 | 39; 64 parts of 256 | 32 of 512: 1 x 16 over 16384 44 | 36.
+  // With room for 700 and 16 x 40 new, 8/2 of 64, whole | in parts: 13 | 19.)
+  if (paged && workgroups(1) <= 400 && capacity >= kSmallCache) {
     const int32_t kp = rows <= 32 && !wide ? 4 : rows <= 64 ? 2 : 1;
     const int64_t likely = n_seqs * ((rows * kp + 127) / 128) * c.n_kv_heads;
-    const int64_t parts = std::min({(likely > 256 ? 1024 : 512) / std::max(likely, (int64_t)1), capacity / 512, (int64_t)64});
+    const int64_t parts = std::min({(likely > 256 ? 1024 : 512) / std::max(likely, (int64_t)1), std::min(capacity / 256, std::max((int64_t)32, capacity / 512)), (int64_t)64});
     if (parts > 1) r = KvRoute{false, kp, (int32_t)parts, parts * heads * (c.head_dim + 2) * 4};
   }
   return r;
