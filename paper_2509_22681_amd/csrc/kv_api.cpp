@@ -41,7 +41,7 @@ int check_config(const flame_kv_config *c) {
 
 int check_batch(const flame_kv_config *c, int32_t n_seqs, int64_t n_rows) {
   if (n_seqs < 0 || (int64_t)n_seqs * c->n_q_heads > kMaxSequenceHeads) return bad("sequences times heads must be in [0, 2^23)");
-  if (n_rows < 0 || n_rows * c->n_q_heads > kMaxRowHeads) return bad("rows times heads must be in [0, 2^25]");
+  if (n_rows < 0 || n_rows > kMaxRowHeads / c->n_q_heads) return bad("rows times heads must be in [0, 2^25]");
   return FLAME_GR_OK;
 }
 

@@ -192,3 +192,14 @@ def test_oracle_of_attention_against_a_brute_force():
                 a, b = (2 * j, 2 * j + 1) if inter else (j, j + 3)
                 z = (x[t, :, a] + 1j * x[t, :, b]) * np.exp(1j * p[t] * f[j])
                 assert np.allclose(y[t, :, a], z.real) and np.allclose(y[t, :, b], z.imag)
+
+
+@pytest.mark.parametrize("n_tokens", [(1 << 22) + 1, 1 << 61, 1 << 62, (1 << 63) - 1])
+def test_row_counts_whose_products_with_the_heads_wrap(n_tokens):
+    """8 heads times 2^61 rows is 0 in 64 bits: the limit is compared before anything is multiplied."""
+    cfg = B.make_kv_config("bf16", 8, 2, 64)
+    with pytest.raises(B.FlameGRError) as e:
+        B.flame_kv_workspace_bytes(cfg, 3, n_tokens)
+    assert e.value.code == INVALID
+    for op in OPS[:3]:
+        assert call(op, n_tokens=n_tokens) == INVALID, op
