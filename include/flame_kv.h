@@ -111,17 +111,18 @@ int flame_kv_prompt(const flame_kv_config *cfg, const flame_kv_rows *q, const fl
 /* Causal attention of the newest tokens of every sequence over its cache (which holds them already: flame_kv_append first).
  *   q, out       rows [n_tokens][n_q_heads], sequence b at q_offsets[b]..q_offsets[b+1]
  *   kv_lens      device [n_seqs]: tokens in the cache
- *   workspace    device, flame_kv_workspace_bytes(cfg, n_seqs, n_tokens) bytes, 16-byte aligned.  It holds nothing between calls; two calls that
- *                overlap in time need one each. */
+ *   workspace    device, 16-byte aligned, of flame_kv_workspace_bytes bytes for these sequences and rows or for more.  It holds nothing between
+ *                calls; two calls that overlap in time need one each. */
 int flame_kv_extend(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *q_offsets, const int32_t *kv_lens,
                     int32_t n_seqs, int64_t n_tokens, const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream);
 
 /* Attention of one new token of every sequence over its cache: row b of q and out [n_seqs][n_q_heads] belongs to sequence b.
- * A sequence of length 0 has an output of zeros.  Workspace: flame_kv_workspace_bytes(cfg, n_seqs, n_seqs). */
+ * A sequence of length 0 has an output of zeros.  Workspace: as of n_seqs rows. */
 int flame_kv_decode(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *kv_lens, int32_t n_seqs,
                     const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream);
 
-/* HOST arithmetic: workspace of flame_kv_extend and flame_kv_decode for this many sequences and query rows. */
+/* HOST arithmetic: a workspace for every flame_kv_extend and flame_kv_decode of this configuration with up to so many sequences and query rows:
+ * a program asks once, for its largest batch. */
 int flame_kv_workspace_bytes(const flame_kv_config *cfg, int32_t n_seqs, int64_t n_tokens, int64_t *bytes);
 
 /* HOST arithmetic: the geometric frequencies base^(-2j / rot_dim), j = 0..rot_dim/2-1, into out [rot_dim/2]. */

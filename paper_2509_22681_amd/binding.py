@@ -661,7 +661,7 @@ def flame_kv_rotation_frequencies(rot_dim: int, base: float = 10000.0) -> np.nda
 
 
 def flame_kv_workspace_bytes(cfg: flame_kv_config, n_seqs: int, n_tokens: Optional[int] = None) -> int:
-    """Bytes that flame_kv_extend needs for this many sequences and query rows; n_tokens None: flame_kv_decode."""
+    """Bytes of a workspace for every flame_kv_extend and flame_kv_decode of up to this many sequences and query rows (n_tokens None: one row each)."""
     out = C.c_int64(0)
     _kv_check(_lib.flame_kv_workspace_bytes(C.byref(cfg), n_seqs, n_seqs if n_tokens is None else n_tokens, C.byref(out)))
     return out.value
@@ -695,7 +695,7 @@ def flame_kv_prompt(cfg, q, k, v, q_offsets, out, k_offsets=None, faults=None, s
 
 def flame_kv_extend(cfg, cache, q, q_offsets, kv_lens, out, workspace=None, faults=None, stream=None) -> None:
     """q, out: device rows [n_tokens, n_q_heads, head_dim], the newest tokens of every sequence; q_offsets [n_seqs + 1], kv_lens [n_seqs]: device int32;
-    workspace: device tensor of at least flame_kv_workspace_bytes(cfg, n_seqs, n_tokens) bytes."""
+    workspace: device tensor of flame_kv_workspace_bytes bytes for these sequences and rows or for more."""
     n_seqs, n, dev = len(kv_lens), len(q), torch.cuda.current_device()
     if len(out) != n:
         raise ValueError("out must have the rows of q")
@@ -709,7 +709,7 @@ def flame_kv_extend(cfg, cache, q, q_offsets, kv_lens, out, workspace=None, faul
 
 def flame_kv_decode(cfg, cache, q, kv_lens, out, workspace=None, faults=None, stream=None) -> None:
     """q, out: device rows [n_seqs, n_q_heads, head_dim], one new token of every sequence; kv_lens: device int32 [n_seqs];
-    workspace: device tensor of at least flame_kv_workspace_bytes(cfg, n_seqs) bytes."""
+    workspace: device tensor of flame_kv_workspace_bytes bytes for these sequences or for more."""
     n_seqs, dev = len(kv_lens), torch.cuda.current_device()
     if len(q) != n_seqs or len(out) != n_seqs:
         raise ValueError("q and out must have one row per sequence")

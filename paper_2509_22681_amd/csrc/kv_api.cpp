@@ -25,6 +25,8 @@ int done(hipError_t e) {
 constexpr int64_t kMaxRowHeads = (int64_t)1 << 25, kMaxSequenceHeads = ((int64_t)1 << 23) - 1;
 constexpr int64_t kSmallCache = 1024;                          // tokens that a sequence has room for, up to which its keys are not split over the chip
 constexpr int64_t kMaxKeys = ((int64_t)1 << 31) - 65536;     // of a sequence: room for a tile's end behind them in 32 bits
+// Limits of kv_route, for the workspace of every call up to a size: rows times heads of an extend that is split, parts of a row tile's keys, and workgroups of a launch whose keys are cut.
+constexpr int64_t kSplitRowHeads = 16384, kMostParts = 64, kPartWorkgroups = 400;
 
 int64_t element(int32_t dtype) { return dtype == FLAME_KV_F32 ? 4 : 2; }
 bool aligned(const void *p) { return ((uintptr_t)p & 15) == 0; }
@@ -92,9 +94,22 @@ void take_heads(const flame_kv_config *c, KvAttention *a) {
   a->scale = c->scale == 0.f ? 1.f / std::sqrt((float)c->head_dim) : c->scale;
 }
 
-// What any cache may need: one of little room may go by another route than a large one.
+// What a call of this size needs over any cache: one of little room may go by another route than a large one.
 int64_t workspace_bytes_for(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool decode) {
   return std::max(kv_route(c, n_seqs, n_rows, true, decode, kMaxKeys).workspace, kv_route(c, n_seqs, n_rows, true, decode, kSmallCache).workspace);
+}
+
+// What any call of up to this many sequences and rows may need, over any cache: a bound that only grows with either.  Decoding splits the rows of one per sequence, an extend up to
+// kSplitRowHeads.  In parts, kv_route cuts keys into up to kMostParts, and into at most 1024 / likely: with s sequences of r rows (of a key head) and kp wavefronts to 32 of them, likely is
+// s ceil(r kp / 128) key heads, and there are fewer than s (r + 1) key heads rows times heads; r + 1 <= 129 ceil(r kp / 128), so that parts times rows times heads stay below 1024 * 129.
+// (Without rows to a whole sequence, r = 0, they stay below kMostParts kPartWorkgroups, which is less.)
+int64_t workspace_bound(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows) {
+  if (n_seqs == 0 || n_rows == 0) return 0;
+  const int64_t heads = n_rows * c.n_q_heads;
+  static_assert(kMostParts * kPartWorkgroups <= 1024 * 129, "what a sequence of less than a row may need");
+  const int64_t split = kv_split_workspace_bytes(c.head_dim, std::max(std::min((int64_t)n_seqs, n_rows) * c.n_q_heads, std::min(heads, kSplitRowHeads)));
+  const int64_t parts = std::min(kMostParts * heads, (int64_t)1024 * 129) * (c.head_dim + 2) * 4;
+  return std::max(split, parts);
 }
 
 int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_rows,
@@ -107,7 +122,7 @@ int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const 
   const KvRoute route = kv_route(*cfg, n_seqs, n_rows, true, offsets == nullptr, a.pages.capacity);
   const int64_t need = workspace_bytes_for(*cfg, n_seqs, n_rows, offsets == nullptr);
   if (need > 0 && (!workspace || !aligned(workspace))) return bad("the workspace is NULL or not 16-byte aligned");
-  if (workspace_bytes < need) return bad("the workspace is smaller than flame_kv_workspace_bytes", FLAME_GR_CAPACITY_EXCEEDED);
+  if (workspace_bytes < need) return bad("the workspace is smaller than this call needs (flame_kv_workspace_bytes)", FLAME_GR_CAPACITY_EXCEEDED);
   a.batch = KvBatch{offsets, kv_lens, n_seqs, n_rows, faults};
   take_heads(cfg, &a);
   if (route.split) return done(launch_kv_split(a, workspace, (hipStream_t)stream));
@@ -134,7 +149,7 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   // fp32: up to 32 rows: 2048 (16 x 4, 32/8, over 2048) 64 | 113, 16384 (64 x 8, 32/8, over 2048) 301 | 399; more: 512 (16 new, 32/8, over 4096) 36 | 55, 1024 (32 new, 32/8, over 4096) 49 | 91,
   //   (over 16384) 129 | 112, 2048 (64 new, 32/8, over 4096) 75 | 92, (over 16384) 235 | 168, 4096 (4 x 32, 32/8, over 4096) 137 | 100
   // Room for 512 tokens, bf16: 1024 (4 x 8, 32/8) 21 | 13
-  const int64_t few = f32 ? (rows <= 32 ? 16384 : 1024) : rows > 32 ? 0 : rows > 16 ? 512 : n_seqs > 64 ? 8192 : 2048;
+  const int64_t few = f32 ? (rows <= 32 ? kSplitRowHeads : 1024) : rows > 32 ? 0 : rows > 16 ? 512 : n_seqs > 64 ? 8192 : 2048;
   if (decode || (paged && capacity > kSmallCache && heads <= few)) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim, heads)};
   // Four or two wavefronts share 32 rows where that many workgroups of one wavefront per 32 rows leave places of the chip empty, or all are placed at
   // once and wait for the longest.  us with one | two | four, at that many workgroups
@@ -153,10 +168,10 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   // 8/2 heads of 64: 4 x 512 over 4096 50 | 50.  (25 parts in place of 16, one and a half rounds, cost 1 x 128 over 16384 26 us more.
   // Parts of 512 | 256: fp32, 32/8 heads of 128, 3 x 163 over 1277 185 | 142, 6/2 of 128 101 | 54, bf16 44 | 39; 64 parts of 256 | 32 of 512: 1 x 16 over 16384 44 | 36.
   // With room for 700 and 16 x 40 new, 8/2 of 64, whole | in parts: 13 | 19.)
-  if (paged && workgroups(1) <= 400 && capacity >= kSmallCache) {
+  if (paged && workgroups(1) <= kPartWorkgroups && capacity >= kSmallCache) {
     const int32_t kp = rows <= 32 && !wide ? 4 : rows <= 64 ? 2 : 1;
     const int64_t likely = n_seqs * ((rows * kp + 127) / 128) * c.n_kv_heads;
-    const int64_t parts = std::min({(likely > 256 ? 1024 : 512) / std::max(likely, (int64_t)1), std::min(capacity / 256, std::max((int64_t)32, capacity / 512)), (int64_t)64});
+    const int64_t parts = std::min({(likely > 256 ? 1024 : 512) / std::max(likely, (int64_t)1), std::min(capacity / 256, std::max((int64_t)32, capacity / 512)), kMostParts});
     if (parts > 1) r = KvRoute{false, kp, (int32_t)parts, parts * heads * (c.head_dim + 2) * 4};
   }
   return r;
@@ -181,7 +196,7 @@ int flame_kv_workspace_bytes(const flame_kv_config *cfg, int32_t n_seqs, int64_t
   if (int rc = check_config(cfg)) return rc;
   if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
   if (!bytes) return bad("bytes is NULL");
-  *bytes = std::max(workspace_bytes_for(*cfg, n_seqs, n_tokens, false), n_tokens == n_seqs ? workspace_bytes_for(*cfg, n_seqs, n_tokens, true) : 0);
+  *bytes = workspace_bound(*cfg, n_seqs, n_tokens);
   return FLAME_GR_OK;
 }
 

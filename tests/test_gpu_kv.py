@@ -806,3 +806,23 @@ def test_refusals_on_the_device(B):
     out = torch.empty(5, 1, 64, device=DEV, dtype=torch.bfloat16)
     B.flame_kv_prompt(one, x, x, x, ints([0, 5]), out)
     check_attention(host(out), host(x), host(x), host(x), "bf16")
+
+
+def test_one_workspace_for_every_smaller_batch(B):
+    """As a server has it: asked for once, for its largest batch, and used by every call."""
+    import torch
+    gen, lens = generator(17), [1500, 60, 900]
+    c = Cache(B, gen, "bf16", 8, 2, 64, lens, 16, tokens=8192)
+    ws = workspace_for(B, c.cfg, 64, 4096)
+    for new in ([1, 0, 0], [1, 1, 1], [30, 2, 1], [300, 0, 200]):
+        off, n = offsets(new), sum(new)
+        q = rand(gen, "bf16", n, 8, 64)
+        out = torch.full_like(q, 7.0)
+        B.flame_kv_extend(c.cfg, c.packed, q, ints(off), ints(lens), out, ws)
+        for b, n_b in enumerate(lens):
+            check_attention(host(out[off[b]:off[b + 1]]), host(q[off[b]:off[b + 1]]), *c.rows(b, n_b), "bf16", what=(new, b))
+    q = rand(gen, "bf16", 3, 8, 64)
+    out = torch.full_like(q, 7.0)
+    B.flame_kv_decode(c.cfg, c.packed, q, ints(lens), out, ws)
+    for b, n_b in enumerate(lens):
+        check_attention(host(out[b:b + 1]), host(q[b:b + 1]), *c.rows(b, n_b), "bf16", what=("decode", b))

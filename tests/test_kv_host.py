@@ -203,3 +203,43 @@ def test_row_counts_whose_products_with_the_heads_wrap(n_tokens):
     assert e.value.code == INVALID
     for op in OPS[:3]:
         assert call(op, n_tokens=n_tokens) == INVALID, op
+
+
+class Route(C.Structure):
+    _fields_ = [("split", C.c_bool), ("wavefronts", C.c_int32), ("splits", C.c_int32), ("workspace", C.c_int64)]
+
+
+# KvRoute kv_route(const flame_kv_config &, int32_t n_seqs, int64_t n_rows, bool paged, bool decode, int64_t capacity) of csrc/kv.h
+kv_route = B._lib["_ZN5flame8kv_routeERK15flame_kv_configilbbl"]
+kv_route.restype, kv_route.argtypes = Route, [C.POINTER(B.flame_kv_config), C.c_int32, C.c_int64, C.c_bool, C.c_bool, C.c_int64]
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 32, 8, 128), ("f16", 8, 2, 64), ("f32", 32, 8, 128), ("bf16", 1, 1, 32), ("f32", 6, 2, 64), ("f16", 40, 1, 32), ("bf16", 400, 400, 64), ("f32", 4096, 1, 128)])
+def test_a_workspace_of_a_large_batch_serves_every_smaller_one(dtype, hq, hkv, dim):
+    cfg, rng = B.make_kv_config(dtype, hq, hkv, dim), np.random.default_rng(hq)
+    room = [1, 1023, 1024, 1025, 2048, 5000, 8192, 16384, 20000, 32768, 1 << 20, (1 << 31) - 65536]
+    most = [min(1 << 22, ((1 << 23) - 1) // hq), (1 << 25) // hq]           # sequences, rows
+    counts = [sorted({min(n, m) for n in [1, 2, 3, 5, 8, 15, 16, 33, 64, 65, 127, 128, 129, 200, 341, 400, 401, 1000, 1360, 4096, 51199, 1 << 17, m] + rng.integers(1, 3000, 12).tolist()})
+              for m in most]
+    needed = {}
+    for s in counts[0]:
+        for t in counts[1]:
+            needed[s, t] = max(kv_route(cfg, s, t, True, False, c).workspace for c in room)
+        if s <= most[1]:
+            needed[s, s] = max([needed.get((s, s), 0)] + [kv_route(cfg, s, s, True, True, c).workspace for c in room])
+    held = {at: B.flame_kv_workspace_bytes(cfg, *at) for at in needed}
+    for at, bytes_ in held.items():
+        assert bytes_ >= needed[at], at
+    # the largest that any call of up to so many sequences and rows needs: over columns, then over rows
+    for s_most in counts[0]:
+        for t_most in counts[1]:
+            assert held[s_most, t_most] >= max(needed[s, t] for s, t in needed if s <= s_most and t <= t_most), (s_most, t_most)
+    assert held[counts[0][-1], counts[1][-1]] <= 512 << 20
+
+
+def test_what_one_workspace_serves():
+    cfg = B.make_kv_config("bf16", 32, 8, 128)
+    large = B.flame_kv_workspace_bytes(cfg, 64, 4096)
+    for s, t in ((64, 64), (1, 1), (8, 512), (1, 128), (1, 16), (3, 5)):
+        assert B.flame_kv_workspace_bytes(cfg, s, t) <= large, (s, t)
+    assert B.flame_kv_workspace_bytes(cfg, 64) <= large
