@@ -35,7 +35,8 @@
  *     kernels, which check what they address by: an entry out of range makes no access, and is reported in *faults (device int32,
  *     may be NULL), into which the kernels OR the FLAME_KV_FAULT_* bits they meet.  The caller clears it.
  *   - Device buffers stay alive and unmodified until the stream has passed the call.  Outputs must not overlap inputs (q_out may be q).
- *   - Rows behind the last sequence (offsets[n_seqs] <= row < n_tokens) are neither read nor written: a batch may be padded.
+ *   - Rows ahead of the first sequence and behind the last one (row < offsets[0], offsets[n_seqs] <= row < n_tokens) are neither read nor written: a batch
+ *     may be padded.
  */
 #ifndef FLAME_KV_H
 #define FLAME_KV_H
@@ -55,7 +56,8 @@ typedef enum {
   FLAME_KV_FAULT_PAGE = 1,   /* a page-table entry outside [0, n_pages): its tokens are not written, its keys not seen */
   FLAME_KV_FAULT_LENGTH = 2, /* a length below 0 or beyond the table's row (taken as the nearest that fits), or an appended token at a position below 0 or
                                 beyond it (not written to the cache; below 0 its query is not written either) */
-  FLAME_KV_FAULT_OFFSET = 4  /* offsets that decrease, start below 0 or end behind the rows: rows that they leave without a sequence are not written */
+  FLAME_KV_FAULT_OFFSET = 4  /* offsets that decrease, are below 0 or end behind the rows.  Of up to 64 sequences, those before the first offset that decreases or is below 0 have
+                                their results, as far as there are rows, and no other row is written.  Of more, which rows of the batch are written is not defined. */
 } flame_kv_fault;
 
 typedef struct {
@@ -95,8 +97,8 @@ typedef struct {
  *   rotation     NULL: none
  *   offsets      device [n_seqs+1]
  *   kv_lens      device [n_seqs]: tokens of each sequence WITH the new ones; row j of its m new rows has position kv_lens[b] - m + j
- * Every value written is the rounding of one expression: the same call gives the same bits.  Two new tokens in one slot (a page
- * that two sequences share) leave either's values there. */
+ * Every value written is the rounding of one expression: the same call gives the same bits.  Of two new tokens in one slot (a page
+ * that two sequences share) every value there is one or the other's. */
 int flame_kv_append(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *k, const flame_kv_rows *v, const flame_kv_rows *q,
                     const flame_kv_rows *q_out, const flame_kv_rotation *rotation, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs,
                     int64_t n_tokens, int32_t *faults, void *stream);

@@ -41,15 +41,14 @@ __global__ __launch_bounds__(64 * kTokensPerBlock) void kv_append_kernel(KvBatch
   constexpr int E = 16 / sizeof(T);
   __shared__ float2 turn_s[kTokensPerBlock][kMaxRotationPairs];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (blockIdx.x == 0 && batch.faults)
+    for (int b = threadIdx.x; b < batch.n_seqs; b += 64 * kTokensPerBlock) kv_report_offsets(batch.offsets[b], batch.offsets[b + 1], batch.n_rows, batch.faults);
   const int64_t token = (int64_t)blockIdx.x * kTokensPerBlock + wave;
   if (token >= batch.n_rows) return;
   const int seq = kv_find_sequence(batch.offsets, batch.n_seqs, token, lane);
   if (seq >= batch.n_seqs) return;                                        // behind the last sequence
   const int64_t first = batch.offsets[seq], end = batch.offsets[seq + 1];
-  if (token < first || first < 0 || end > batch.n_rows) {
-    if (lane == 0) kv_fault(batch.faults, FLAME_KV_FAULT_OFFSET);
-    if (token < first || first < 0) return;
-  }
+  if (first < 0 || token < first || token >= end) return;                 // ahead of the first one, or offsets that are none
   const int64_t position = (int64_t)batch.kv_lens[seq] - end + token;
   const bool placed = position >= 0 && position < pages.capacity;
   int64_t to = -1;

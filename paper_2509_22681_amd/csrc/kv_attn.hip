@@ -119,14 +119,13 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   if (blockIdx.x == 0 && a.batch.faults)
     for (int b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
       const int64_t first = a.batch.offsets[b], end = a.batch.offsets[b + 1];
-      if (first < 0 || end < first || end > a.batch.n_rows) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
+      kv_report_offsets(first, end, a.batch.n_rows, a.batch.faults);
       if (PAGED) {
         kv_clip_length(a.batch.kv_lens[b], a.pages.capacity, a.batch.faults, true);
       } else if (a.k_offsets) {
-        const int64_t k_first = a.k_offsets[b], k_end = a.k_offsets[b + 1];
-        if (k_first < 0 || k_end < k_first || k_end > a.n_keys) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
-      } else if (first < 0 || end > a.n_keys) {
-        kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
+        kv_report_offsets(a.k_offsets[b], a.k_offsets[b + 1], a.n_keys, a.batch.faults);
+      } else {
+        kv_report_offsets(first, end, a.n_keys, a.batch.faults);
       }
     }
   // Of a compute unit's workgroups, one is of the first 256 and one of the next: those go the other way round, so that a long one has a short one beside it
@@ -149,8 +148,11 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
     if (lane < a.batch.n_seqs) {
       b = a.batch.offsets[lane];
       e = a.batch.offsets[lane + 1];
-      tiles = b < 0 ? 0 : ((int64_t)max(0, (int)min((int64_t)e, a.batch.n_rows) - b) * group + QT - 1) / QT;
-      keys = PAGED ? a.batch.kv_lens[lane] : (int)((int64_t)e - b);
+    }
+    const uint64_t wrong = __builtin_amdgcn_ballot_w64(kv_wrong_offsets(b, e));
+    if (lane < a.batch.n_seqs && !(wrong << (63 - lane))) {       // (none up to this one)
+      tiles = (max((int64_t)0, min((int64_t)e, a.batch.n_rows) - b) * group + QT - 1) / QT;
+      keys = PAGED ? a.batch.kv_lens[lane] : e - b;
     }
     int before = 0;
     for (int j = 0; j < a.batch.n_seqs; ++j) {

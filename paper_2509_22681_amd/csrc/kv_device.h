@@ -11,21 +11,34 @@ __device__ __forceinline__ void kv_fault(int32_t *faults, int32_t bits) {
   if (faults) atomicOr(faults, bits);
 }
 
-// The sequence whose rows hold row t, for the wavefront: the number of b with offsets[b + 1] <= t.  64 probes at a time, so one
-// load's latency for up to 64 sequences and two up to 4096.  n_seqs where the row is behind the last sequence.  Whatever the
-// offsets hold, the probes stay within offsets[1..n_seqs].
+// A sequence whose offsets are none: it has no rows, and of up to 64 sequences neither do those behind it, whose offsets may claim the rows of others.
+__device__ __forceinline__ bool kv_wrong_offsets(int64_t first, int64_t end) { return first < 0 || end < first; }
+__device__ __forceinline__ void kv_report_offsets(int64_t first, int64_t end, int64_t n_rows, int32_t *faults) {
+  if (kv_wrong_offsets(first, end) || end > n_rows) kv_fault(faults, FLAME_KV_FAULT_OFFSET);
+}
+
+// The sequence whose rows hold row t, for the wavefront: the first b with offsets[b + 1] > t.  64 probes at a time, so one
+// load's latency for up to 64 sequences and two up to 4096.  n_seqs where the row is behind the last sequence, or behind offsets that are none.  Whatever the
+// offsets hold, the probes stay within offsets[0..n_seqs].  (A row may still be ahead of its sequence, and of more than 64 behind it: callers look.)
 __device__ __forceinline__ int kv_find_sequence(const int32_t *offsets, int n_seqs, int64_t t, int lane) {
   int lo = 0, n = n_seqs;
   while (n > 64) {
     const int step = (n + 63) / 64;
     const int at = lo + min((lane + 1) * step, n);
-    const int c = __builtin_popcountll(__builtin_amdgcn_ballot_w64(offsets[at] <= t));
+    const uint64_t beyond = __builtin_amdgcn_ballot_w64(offsets[at] > t);
+    const int c = beyond ? __builtin_ctzll(beyond) : 64;
     if (c * step >= n) return lo + n;
     lo += c * step;
     n = min(step, n - c * step);
   }
-  const bool below = lane < n && offsets[lo + lane + 1] <= t;
-  return lo + __builtin_popcountll(__builtin_amdgcn_ballot_w64(below));
+  int first = 0, end = 0;
+  if (lane < n) {
+    first = offsets[lo + lane];
+    end = offsets[lo + lane + 1];
+  }
+  const uint64_t beyond = __builtin_amdgcn_ballot_w64(lane < n && end > t), wrong = __builtin_amdgcn_ballot_w64(lane < n && kv_wrong_offsets(first, end));
+  const int found = beyond ? __builtin_ctzll(beyond) : n;
+  return wrong && __builtin_ctzll(wrong) <= found ? n_seqs : lo + found;
 }
 
 // Tokens of a sequence, within what its row of the table has room for.

@@ -40,6 +40,7 @@ struct SplitSeq {
   int rows, blocks;   // query rows times G, and units per key head
   int n, back;        // keys; keys that the row before the first one would see
   int tiles;          // of one unit
+  bool wrong;         // offsets that are none
 };
 
 template <int KT> __device__ __forceinline__ SplitSeq split_sequence(const KvAttention &a, int b, bool report) {
@@ -47,13 +48,14 @@ template <int KT> __device__ __forceinline__ SplitSeq split_sequence(const KvAtt
   s.n = kv_clip_length(a.batch.kv_lens[b], a.pages.capacity, a.batch.faults, report);
   int64_t m = 1, full = 1;
   s.first = b;
+  s.wrong = false;
   if (a.batch.offsets) {
     const int64_t first = a.batch.offsets[b], end = a.batch.offsets[b + 1];
     s.first = (int)first;
     full = end - first;
-    const bool wrong = first < 0 || full < 0 || end > a.batch.n_rows;
-    if (wrong && report) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
-    m = first < 0 || full < 0 ? 0 : max((int64_t)0, min(full, a.batch.n_rows - first));
+    s.wrong = kv_wrong_offsets(first, end);
+    if (report) kv_report_offsets(first, end, a.batch.n_rows, a.batch.faults);
+    m = s.wrong ? 0 : max((int64_t)0, min(full, a.batch.n_rows - first));
   }
   const int group = a.n_q_heads / a.n_kv_heads;
   s.back = (int)max(s.n - full, -((int64_t)1 << 30));
@@ -66,7 +68,7 @@ template <int KT> __device__ __forceinline__ SplitSeq split_sequence(const KvAtt
 // Of up to 64 sequences each lane keeps one; of more they are read again.
 __device__ __forceinline__ SplitSeq split_from_lane(const SplitSeq &s, int lane) {
   return SplitSeq{__builtin_amdgcn_readlane(s.first, lane), __builtin_amdgcn_readlane(s.rows, lane), __builtin_amdgcn_readlane(s.blocks, lane),
-                  __builtin_amdgcn_readlane(s.n, lane), __builtin_amdgcn_readlane(s.back, lane), __builtin_amdgcn_readlane(s.tiles, lane)};
+                  __builtin_amdgcn_readlane(s.n, lane), __builtin_amdgcn_readlane(s.back, lane), __builtin_amdgcn_readlane(s.tiles, lane), false};
 }
 
 __device__ __forceinline__ int64_t split_scan(int64_t v) {        // inclusive sums over the wavefront
@@ -106,11 +108,13 @@ template <int KT, typename F> __device__ __forceinline__ SplitPlace split_find(c
     int64_t mine = 0;
     int chunk = 1;
     if (n <= 64) {
-      if (lane < n) {
-        const SplitSeq s = split_sequence<KT>(a, lo + lane, report);
-        mine = (int64_t)s.blocks * s.tiles;
-        if (top) p.mine = s;
+      SplitSeq s{};
+      if (lane < n) s = split_sequence<KT>(a, lo + lane, report);
+      if (top) {
+        if (__builtin_amdgcn_ballot_w64(s.wrong) << (63 - lane)) s.rows = s.blocks = s.tiles = 0;   // (one up to this one)
+        p.mine = s;
       }
+      mine = (int64_t)s.blocks * s.tiles;
     } else {
       // the wavefront reads 64 neighbours at a time
       chunk = (n + 4095) / 4096 * 64;

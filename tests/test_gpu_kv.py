@@ -826,3 +826,90 @@ def test_one_workspace_for_every_smaller_batch(B):
     B.flame_kv_decode(c.cfg, c.packed, q, ints(lens), out, ws)
     for b, n_b in enumerate(lens):
         check_attention(host(out[b:b + 1]), host(q[b:b + 1]), *c.rows(b, n_b), "bf16", what=("decode", b))
+
+
+WRONG_OFFSETS = [[0, 30, -2 ** 31, 60], [0, 30, -2 ** 31, 2 ** 31 - 1], [0, 30, 5, 60], [0, 30, 29, 29], [0, 30, 0, 60], [0, 20, 30, 10, 60, 0, 60], [0, 30, -1, 60, 0, 60, 0, 60], [-5, 40, 50, 60]]
+
+
+def before_the_wrong(off):
+    """Sequences before the first offset that decreases or is below 0."""
+    n = 0
+    while n < len(off) - 1 and 0 <= off[n] <= off[n + 1]:
+        n += 1
+    return n
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("off", WRONG_OFFSETS, ids=str)
+def test_sequences_before_offsets_that_are_none(B, dtype, off):
+    """Of up to 64 sequences those before the first offset that decreases or is below 0 have their results, whatever the others claim (their rows, most of the keys, millions of rows);
+    rows of no such sequence stay as they were.  Row tiles, in parts, split."""
+    import torch
+    gen, n_seqs, good = generator(18), len(off) - 1, before_the_wrong(off)
+    lens = [900] + [1200, 90, 1500, 64, 1300, 1400][:n_seqs - 1]
+    rows = off[good] if good else 0
+    fault = torch.zeros(1, dtype=torch.int32, device=DEV)
+    for room, hq in ((0, 4), (4096, 64), (4096, 2)):
+        c = Cache(B, gen, dtype, hq, hq, 64, lens, 16, tokens=room)
+        q, k = rand(gen, dtype, 60, hq, 64), rand(gen, dtype, 60, hq, 64)
+        for kind in ("prompt", "extend"):
+            buffer = torch.full((180, hq, 64), 7.0, dtype=q.dtype, device=DEV)
+            out = buffer[60:120]
+            fault.zero_()
+            if kind == "prompt":
+                B.flame_kv_prompt(c.cfg, q, k, k, ints(off), out, faults=fault)
+            else:
+                ws = torch.zeros(B.flame_kv_workspace_bytes(c.cfg, n_seqs, 60), dtype=torch.uint8, device=DEV)
+                B.flame_kv_extend(c.cfg, c.packed, q, ints(off), ints(lens), out, ws, faults=fault)
+            assert int(fault[0]) == 4, (kind, room)
+            assert bool((buffer[:60] == 7.0).all()) and bool((buffer[60 + rows:] == 7.0).all()), (kind, room)
+            for b in range(good):
+                s = slice(off[b], off[b + 1])
+                keys, values = (host(k[s]), host(k[s])) if kind == "prompt" else c.rows(b, lens[b])
+                check_attention(host(out[s, :1]), host(q[s, :1]), keys[:, :1], values[:, :1], dtype, what=(kind, room, hq, b))
+
+
+@pytest.mark.parametrize("off", WRONG_OFFSETS, ids=str)
+def test_append_before_offsets_that_are_none(B, off):
+    """The same of append: reported, and exactly the tokens of the sequences before are written."""
+    import torch
+    gen, n_seqs, good = generator(19), len(off) - 1, before_the_wrong(off)
+    cfg = B.make_kv_config("bf16", 2, 1, 32)
+    table = np.arange(n_seqs * 8, dtype=np.int32).reshape(n_seqs, 8)
+    k_pool, v_pool = (torch.zeros(n_seqs * 8, 16, 1, 32, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    k, q = rand(gen, "bf16", 60, 1, 32), rand(gen, "bf16", 60, 2, 32)
+    q_out, fault = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    lens = [100 + b for b in range(n_seqs)]
+    B.flame_kv_append(cfg, B.pack_kv_cache(cfg, k_pool, v_pool, ints(table)), k, k, ints(off), ints(lens), q=q, q_out=q_out, faults=fault)
+    assert int(fault[0]) == 4
+    rows = off[good] if good else 0
+    assert torch.equal(q_out[:rows], q[:rows]) and bool((q_out[rows:] == 7.0).all())
+    want = torch.zeros_like(k_pool)
+    for b in range(good):
+        for i in range(off[b], off[b + 1]):
+            t = lens[b] - off[b + 1] + i
+            want[int(table[b, t // 16]), t % 16] = k[i]
+    assert torch.equal(k_pool, want) and torch.equal(v_pool, want)
+
+
+def test_append_reports_offsets_and_writes_the_rest(B):
+    """Offsets that decrease, begin below 0 or end behind the rows: the bit, and the slots that are written.  Rows ahead of the first sequence are like those behind the last one."""
+    import torch
+    gen = generator(20)
+    cfg = B.make_kv_config("bf16", 2, 1, 32)
+    k_pool, v_pool = torch.zeros(4, 4, 1, 32, device=DEV, dtype=torch.bfloat16), torch.zeros(4, 4, 1, 32, device=DEV, dtype=torch.bfloat16)
+    cache = B.pack_kv_cache(cfg, k_pool, v_pool, ints([[0, 1], [2, 3]]))
+    k = rand(gen, "bf16", 12, 1, 32)
+    first, second = [(0, i) for i in range(4)] + [(1, i) for i in range(4)], [(2, i) for i in range(4)]
+    for off, lens, fault, slots in (([0, 4, 2], [4, 2], 4, first[:4]), ([-3, 4, 5], [4, 2], 4, []), ([0, 8, 20], [8, 12], 4, first + second), ([2, 4, 6], [2, 3], 0, first[:2] + second[1:3])):
+        k_pool.zero_(), v_pool.zero_()
+        faults = torch.zeros(1, dtype=torch.int32, device=DEV)
+        B.flame_kv_append(cfg, cache, k, k, ints(off), ints(lens), faults=faults)
+        there = [tuple(x) for x in (k_pool.abs().sum((2, 3)) > 0).nonzero().tolist()]
+        assert (int(faults[0]), there) == (fault, slots), off
+        assert torch.equal(k_pool, v_pool)
+    # attention has the same view of rows ahead of the first sequence
+    q, fault = rand(gen, "bf16", 12, 2, 32), torch.zeros(1, dtype=torch.int32, device=DEV)
+    out = torch.full_like(q, 7.0)
+    B.flame_kv_prompt(cfg, q, k, k, ints([2, 4, 9]), out, faults=fault)
+    assert int(fault[0]) == 0 and bool((out[:2] == 7.0).all()) and bool((out[9:] == 7.0).all()) and not bool((out[2:9] == 7.0).all(-1).any())
