@@ -108,13 +108,15 @@ template <int KT, typename F> __device__ __forceinline__ SplitPlace split_find(c
     int64_t mine = 0;
     int chunk = 1;
     if (n <= 64) {
-      SplitSeq s{};
-      if (lane < n) s = split_sequence<KT>(a, lo + lane, report);
-      if (top) {
-        if (__builtin_amdgcn_ballot_w64(s.wrong) << (63 - lane)) s.rows = s.blocks = s.tiles = 0;   // (one up to this one)
-        p.mine = s;
+      if (lane < n) {
+        const SplitSeq s = split_sequence<KT>(a, lo + lane, report);
+        mine = (int64_t)s.blocks * s.tiles;
+        if (top) p.mine = s;
       }
-      mine = (int64_t)s.blocks * s.tiles;
+      if (top && a.batch.offsets) {
+        const uint64_t wrong = __builtin_amdgcn_ballot_w64(p.mine.wrong);
+        if (wrong && lane >= __builtin_ctzll(wrong)) mine = p.mine.rows = p.mine.blocks = p.mine.tiles = 0;
+      }
     } else {
       // the wavefront reads 64 neighbours at a time
       chunk = (n + 4095) / 4096 * 64;
