@@ -22,9 +22,10 @@
  * The angle is reduced in 64-bit fixed point, so it is as exact at position 2^30 as at 0.
  *
  * Arithmetic.  Products of 16-bit operands are exact and added up in fp32; softmax maxima and sums are fp32; its weights are rounded to the
- * element type for the product with the values (bf16, f16: matrix operands; f32: not rounded); outputs are rounded once.  The sums over the
- * keys are divided by the sum of the weights at the end, and until then a weight may be up to 2^8: of n keys, values beyond 2^120 / n may give
- * infinities (fp32 and bf16; no fp16 value gets there).  An infinite value with a weight below 2^-126 may give a NaN.
+ * element type for the product with the values (bf16, f16: matrix operands; f32: not rounded; an f16 weight is off by half a step or by 2^-32 of the row's
+ * largest); outputs are rounded once.  The sums over the keys are divided by the sum of the weights at the end, and until then a weight may be up to 2^8: of n
+ * keys, values beyond 2^120 / n may give infinities (fp32 and bf16; no fp16 value gets there).  An infinite value may give a NaN where its weight is below 2^-126
+ * (f16: 2^-32) of the row's largest.
  *
  * Conventions
  *   - Every function returns 0 or a negative flame_gr_status; flame_kv_last_error has the message.  On error

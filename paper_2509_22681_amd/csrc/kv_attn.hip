@@ -330,17 +330,18 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
       tops[j] = max3(max3(x[0], x[1], x[2]), max3(x[3], x[4], z[j][15]), j ? tops[0] : -INFINITY);
     }
     const float top = pair_max(tops[NJ - 1]) * scale;
-    // The exponent's reference of a row moves only when its largest logit has left it 2^8 behind: weights stay below 2^8, and rescaling is rare.  Each row goes by its own logits,
-    // and one that does not move is multiplied by exactly 1: no row's bits depend on the others.
-    const bool moves = top > (m == -INFINITY ? m : m + 8.f);
+    // The exponent's reference of a row moves only when its largest logit has left it 2^8 behind: weights stay below 2^8 (fp16, whose reference is lower: 2^15), and rescaling is rare.
+    // Each row goes by its own logits, and one that does not move is multiplied by exactly 1: no row's bits depend on the others.
+    constexpr float lowered = kv_lowered<T>(8);
+    const bool moves = top > (m == -INFINITY ? m : m + (8.f + lowered));
     if (__builtin_amdgcn_ballot_w64(moves)) {
-      const float keep = moves ? __builtin_amdgcn_exp2f(m - top) : 1.f;
+      const float reference = top - lowered, keep = moves ? __builtin_amdgcn_exp2f(m - reference) : 1.f;
       l *= keep;
 #pragma unroll
       for (int b = 0; b < DB; ++b)
 #pragma unroll
         for (int e = 0; e < 16; ++e) o[b][e] *= keep;
-      m = moves ? top : m;
+      m = moves ? reference : m;
     }
     const float nm = m == -INFINITY ? 0.f : -m;                   // (nothing seen yet: all weights are 2^-inf)
     float sum[4] = {0.f, 0.f, 0.f, 0.f};

@@ -73,6 +73,10 @@ template <typename T> __device__ __forceinline__ uint32_t only_finite(uint32_t w
   return ((w & E) == E ? 0u : w & 0xffffu) | ((w >> 16 & E) == E ? 0u : w & 0xffff0000u);
 }
 
+// Softmax weights are 2^(logit - reference), and `above` is what log2 of a weight may come to.  fp16 weights would be zeros from 2^-25 on, thousands of which can make up a row's result
+// beside one of 1; they are held as high as its range has room (up to 2^15), by a reference that is as much lower, in numerator and denominator alike.  Others need no such place.
+template <typename T> constexpr float kv_lowered(int above) { return std::is_same<T, half_t>::value ? (float)(15 - above) : 0.f; }
+
 // One rounding of an fp32 result, to nearest; an fp16 one past the largest finite value becomes infinite, as in IEEE arithmetic.
 template <typename T> __device__ __forceinline__ T kv_round(float v) { return (T)v; }
 

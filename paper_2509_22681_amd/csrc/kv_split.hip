@@ -303,7 +303,7 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
       float top = w[0];
 #pragma unroll
       for (int i = 1; i < VK; ++i) top = fmaxf(top, w[i]);
-      const float m_new = fmaxf(m, split_max(top));
+      const float m_new = fmaxf(m, split_max(top) - kv_lowered<T>(0));   // the reference of the exponents
       const float m_at = m_new == -INFINITY ? 0.f : m_new;       // (nothing seen yet: all weights are 2^-inf)
       if (__builtin_amdgcn_ballot_w64(m_new != m)) {
         const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_at);

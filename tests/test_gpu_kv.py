@@ -913,3 +913,66 @@ def test_append_reports_offsets_and_writes_the_rest(B):
     out = torch.full_like(q, 7.0)
     B.flame_kv_prompt(cfg, q, k, k, ints([2, 4, 9]), out, faults=fault)
     assert int(fault[0]) == 0 and bool((out[:2] == 7.0).all()) and bool((out[9:] == 7.0).all()) and not bool((out[2:9] == 7.0).all(-1).any())
+
+
+def test_fp16_weights_far_below_the_largest(B):
+    """One key with a logit of 17.47 and a value of 0, thousands with logits of 0 and values of 1: weights of 2^-25.2, which fp16 does not have, make up the result together.
+    An fp16 weight is off by half a step or by 2^-32 of the row's largest (2^-40 where the keys are split), which is what attention_bound's last term has 2^-25 for."""
+    import torch
+    c = float(np.float16(17.47))
+    w, n = math.exp(-c), 4096
+
+    def inputs(dim, tokens, hq):
+        q, k = torch.zeros(tokens, hq, dim, device=DEV, dtype=torch.float16), torch.zeros(n, 2, dim, device=DEV, dtype=torch.float16)
+        v = torch.ones_like(k)
+        q[..., 0], k[0, :, 0], v[0] = c, 1.0, 0.0
+        return q, k, v
+
+    def check(got, last, dim, lost, what):
+        others = np.asarray(last, np.float64)[:, None, None]               # keys but the first that a row sees
+        want = others * w / (1 + others * w)
+        bound = want * (2 * 2.0 ** -11 + 2 * ((dim + 7) * 2.0 ** -24 * c + 2.0 ** -22) + 4 * n * 2.0 ** -24) + n * lost + 2.0 ** -24
+        off = np.abs(host(got) - want)
+        assert (off <= bound).all(), (what, float((off / bound).max()))
+
+    for dim in (32, 64, 128):
+        cfg = B.make_kv_config("f16", 8, 2, dim, scale=1.0)
+        for size in (0, 1, 2):
+            q, k, v = inputs(dim, n, 8)
+            out = torch.full_like(q, 7.0)
+            B.flame_kv_prompt(cfg, q, k, v, ints(offsets([n] + spread(size, "f16", 2))), out)
+            check(out, np.arange(n), dim, 2.0 ** -32, ("prompt", dim, size))
+        pools = [x.reshape(256, 16, 2, dim) for x in inputs(dim, 1, 8)[1:]]
+        for seqs, new in ((1, 100), (8, 300), (256, 1)):                  # in parts, whole, split: all sequences have the same pages
+            cache = B.pack_kv_cache(cfg, *pools, ints(np.tile(np.arange(256), (seqs, 1))))
+            q = inputs(dim, seqs * new, 8)[0]
+            out, lens = torch.full_like(q, 7.0), ints([n] * seqs)
+            if new == 1:
+                B.flame_kv_decode(cfg, cache, q, lens, out, workspace_for(B, cfg, seqs))
+            else:
+                B.flame_kv_extend(cfg, cache, q, ints(offsets([new] * seqs)), lens, out, workspace_for(B, cfg, seqs, seqs * new))
+            check(out, np.tile(np.arange(n - new, n), seqs), dim, 2.0 ** -40 if new == 1 else 2.0 ** -32, (dim, seqs, new))
+
+
+@pytest.mark.parametrize("dtype,power", [("f16", 30), ("bf16", 100), ("f32", 100)])
+def test_infinite_values_of_small_weights(B, dtype, power):
+    """A weight of 2^-30 (fp16) or 2^-100 of the largest is a weight: an infinite value that it has makes the row infinite, on every route."""
+    import torch
+    n, dim, room = 3000, 64, 4096
+    gen = generator(21)
+    cfg = B.make_kv_config(dtype, 8, 2, dim, scale=1.0)
+    k, v = torch.zeros(room, 2, dim, device=DEV, dtype=torch_type(dtype)), rand(gen, dtype, room, 2, dim)
+    k[..., 0] = -math.log(2.0) * power / 8                             # logits of -power ln 2,
+    k[5, :, 0] = 0.0                                                   # and one of 0
+    v[40, :, 3], v[41, :, 4] = math.inf, -math.inf
+    cache = B.pack_kv_cache(cfg, k.reshape(256, 16, 2, dim), v.reshape(256, 16, 2, dim), ints(np.tile(np.arange(256), (64, 1))))
+    for seqs, new in ((1, 100), (8, 300), (64, 1)):
+        q = torch.zeros(seqs * new, 8, dim, device=DEV, dtype=torch_type(dtype))
+        q[..., 0] = 8.0
+        out, lens = torch.full_like(q, 7.0), ints([n] * seqs)
+        if new == 1:
+            B.flame_kv_decode(cfg, cache, q, lens, out, workspace_for(B, cfg, seqs))
+        else:
+            B.flame_kv_extend(cfg, cache, q, ints(offsets([new] * seqs)), lens, out, workspace_for(B, cfg, seqs, seqs * new))
+        assert bool((out[..., 3] == math.inf).all()) and bool((out[..., 4] == -math.inf).all()), (seqs, new)
+        assert bool(out[..., 5:].isfinite().all()) and bool(out[..., :3].isfinite().all()), (seqs, new)
