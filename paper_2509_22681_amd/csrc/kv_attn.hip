@@ -148,12 +148,11 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
     if (lane < a.batch.n_seqs) {
       b = a.batch.offsets[lane];
       e = a.batch.offsets[lane + 1];
+      tiles = (max((int64_t)0, min((int64_t)e, a.batch.n_rows) - b) * group + QT - 1) / QT;
+      keys = PAGED ? a.batch.kv_lens[lane] : (int)((int64_t)e - b);
     }
     const uint64_t wrong = __builtin_amdgcn_ballot_w64(kv_wrong_offsets(b, e));
-    if (lane < a.batch.n_seqs && !(wrong << (63 - lane))) {       // (none up to this one)
-      tiles = (max((int64_t)0, min((int64_t)e, a.batch.n_rows) - b) * group + QT - 1) / QT;
-      keys = PAGED ? a.batch.kv_lens[lane] : e - b;
-    }
+    if (wrong && lane >= __builtin_ctzll(wrong)) tiles = 0;
     int before = 0;
     for (int j = 0; j < a.batch.n_seqs; ++j) {
       const int other = __builtin_amdgcn_readlane(keys, j);
