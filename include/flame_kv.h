@@ -13,8 +13,8 @@
  * Attention.  Query head h (0..n_q_heads-1) reads key/value head h / (n_q_heads / n_kv_heads).  With n keys and m queries of a
  * sequence, query row i is the token at position n - m + i and sees the keys at positions 0..n-m+i:
  *     O_i = sum over c <= n-m+i of w_c V_c,    w = softmax over those c of scale <Q_i, K_c>.
- * A query row that sees no key (more queries than keys), or none with a logit above -infinity, has an output of zeros.  Keys and values that a row does not see have no
- * influence on it, whatever they hold (infinities and NaN too); a NaN that it sees makes it NaN.
+ * A query row that sees no key (more queries than keys), or whose logits are all -infinity, has an output of zeros, whatever the values.  Keys and values that a
+ * row does not see have no influence on it, whatever they hold (infinities and NaN too); a NaN that another row sees makes it NaN.
  *
  * Rotation.  The first rot_dim features of a key or query at position p are taken in pairs (a, b) - feature j with feature
  * j + rot_dim/2, or neighbours 2j and 2j + 1 - and pair j turns by the angle p * frequencies[j]:

@@ -497,6 +497,12 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
     if (__syncthreads_or(odd)) {
       run(std::true_type{});
       __syncthreads();
+      // A row whose logits are all -infinity has zeros, though its weights of zero have met infinite values or NaN.  (NaN logits leave l NaN.)
+      const bool nothing = m == -INFINITY && pair_sum(l) == 0.f;
+#pragma unroll
+      for (int b = 0; b < DB; ++b)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[b][e] = nothing ? 0.f : o[b][e];
     }
   } else {
 #pragma unroll

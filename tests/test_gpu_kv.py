@@ -976,3 +976,36 @@ def test_infinite_values_of_small_weights(B, dtype, power):
             B.flame_kv_extend(cfg, cache, q, ints(offsets([new] * seqs)), lens, out, workspace_for(B, cfg, seqs, seqs * new))
         assert bool((out[..., 3] == math.inf).all()) and bool((out[..., 4] == -math.inf).all()), (seqs, new)
         assert bool(out[..., 5:].isfinite().all()) and bool(out[..., :3].isfinite().all()), (seqs, new)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+def test_rows_without_a_logit_above_minus_infinity(B, dtype, dim):
+    """Every logit is -infinity: zeros on every route, whatever the values hold."""
+    import torch
+    gen, n = generator(22), 1500
+    cfg = B.make_kv_config(dtype, 8, 2, dim)
+    k, v = rand(gen, dtype, 4096, 2, dim), rand(gen, dtype, 4096, 2, dim)
+    k[..., 0] = -math.inf
+    v[100, :, 3], v[200, :, 4], v[1400, :, 5] = math.inf, math.nan, -math.inf
+
+    def queries(tokens):
+        q = torch.zeros(tokens, 8, dim, device=DEV, dtype=torch_type(dtype))
+        q[..., 0] = 1.0
+        return q
+
+    for size in (0, 1, 2):
+        q = queries(n)
+        out = torch.full_like(q, 7.0)
+        B.flame_kv_prompt(cfg, q, k[:n], v[:n], ints(offsets([n] + spread(size, dtype, 2))), out)
+        assert not bool(out.any()), ("prompt", size)
+    for seqs, new, pages in ((1, 100, 256), (8, 300, 256), (8, 3, 256), (8, 1, 256), (2, 40, 10)):
+        cache = B.pack_kv_cache(cfg, k.reshape(256, 16, 2, dim), v.reshape(256, 16, 2, dim), ints(np.tile(np.arange(pages), (seqs, 1))))
+        q, lens = queries(seqs * new), ints([min(n, pages * 16)] * seqs)
+        out = torch.full_like(q, 7.0)
+        B.flame_kv_extend(cfg, cache, q, ints(offsets([new] * seqs)), lens, out, workspace_for(B, cfg, seqs, seqs * new))
+        assert not bool(out.any()), ("extend", seqs, new)
+        if new == 1:
+            out.fill_(7.0)
+            B.flame_kv_decode(cfg, cache, q, lens, out, workspace_for(B, cfg, seqs))
+            assert not bool(out.any()), "decode"
