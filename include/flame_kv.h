@@ -19,7 +19,8 @@
  * Rotation.  The first rot_dim features of a key or query at position p are taken in pairs (a, b) - feature j with feature
  * j + rot_dim/2, or neighbours 2j and 2j + 1 - and pair j turns by the angle p * frequencies[j]:
  *     a' = a cos - b sin,   b' = a sin + b cos.
- * The angle is reduced in 64-bit fixed point, so it is as exact at position 2^30 as at 0.
+ * The angle is reduced in 64-bit fixed point: to the error of a small angle, position p adds at most p 2^-61 of a revolution (times the revolutions per position,
+ * where the frequency is more than one), 2^-30 at position 2^31.
  *
  * Arithmetic.  Products of 16-bit operands are exact and added up in fp32; softmax maxima and sums are fp32; its weights are rounded to the
  * element type for the product with the values (bf16, f16: matrix operands; f32: not rounded; an f16 weight is off by half a step or by 2^-32 of the row's

@@ -146,6 +146,7 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   //     of more than 64 sequences, which the row tiles do not sort by length: 6400 (200 x 4, 8/2 of 64, over 100..8192) 118 | 230, (over 2048) 62 | 54
   //   up to 32: 64 (8 new, 8/2 of 64, over 32768) 23 | 35, 256 (8 new, 32/8, over 4096) 25 | 20, (over 16384) 34 | 34, 384 (24 new, 16/16 of 128, over 16384) 45 | 50,
   //     1024 (4 x 8, 32/8, over 4096) 33 | 27, (over 16384) 81 | 70;  more: 384 (12 new, 32/8, over 16384) 51 | 36, 4096 (128 new, 32/8, over 4096) 71 | 36, (over 16384) 209 | 63
+  // The lines between lose where it says so (8 new over 4096, by a fifth): the host knows what room there is, not how long the sequences are, and takes the side that loses less.
   // fp32: up to 32 rows: 2048 (16 x 4, 32/8, over 2048) 64 | 113, 16384 (64 x 8, 32/8, over 2048) 301 | 399; more: 512 (16 new, 32/8, over 4096) 36 | 55, 1024 (32 new, 32/8, over 4096) 49 | 91,
   //   (over 16384) 129 | 112, 2048 (64 new, 32/8, over 4096) 75 | 92, (over 16384) 235 | 168, 4096 (4 x 32, 32/8, over 4096) 137 | 100
   // Room for 512 tokens, bf16: 1024 (4 x 8, 32/8) 21 | 13
@@ -168,6 +169,11 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   // 8/2 heads of 64: 4 x 512 over 4096 50 | 50.  (25 parts in place of 16, one and a half rounds, cost 1 x 128 over 16384 26 us more.
   // Parts of 512 | 256: fp32, 32/8 heads of 128, 3 x 163 over 1277 185 | 142, 6/2 of 128 101 | 54, bf16 44 | 39; 64 parts of 256 | 32 of 512: 1 x 16 over 16384 44 | 36.
   // With room for 700 and 16 x 40 new, 8/2 of 64, whole | in parts: 13 | 19.)
+  // Up to 400 workgroups: whole | in two or three parts, by workgroups(1); bf16, 32/8 heads of 128: 200 (1 x 768 over 4096) 94 | 88,
+  // (over 16384) 356 | 274, 264 (1 x 1024 over 16384) 372 | 305, 352 (4 x 320 over 4096) 180 | 124, (over 16384) 769 | 438, 376 (1 x 1500 over 16384) 673 | 484, 384 (8 x 160 over 16384) 880 | 450,
+  // 392 (4 x 360 over 4096) 137 | 153, (over 16384) 590 | 606, 448 (8 x 192 over 4096) 141 | 151, (over 16384) 606 | 605; 8/2 heads of 64: 188 (1 x 3000 over 4096) 49 | 56, 258 (1 x 4096 over 16384) 194 | 182,
+  // 322 (1 x 5120 over 16384) 313 | 230, 382 (4 x 1500 over 16384) 372 | 273.  fp32: 200 (1 x 768 over 4096, 32/8 of 128) 576 | 481, 392 (4 x 360) 920 | 929, 448 (8 x 192) 1053 | 841 (not taken);
+  // 8/2 of 64 over 16384: 322 (1 x 5120) 1536 | 1220, 382 (4 x 1500) 1779 | 1621.
   if (paged && workgroups(1) <= kPartWorkgroups && capacity >= kSmallCache) {
     const int32_t kp = rows <= 32 && !wide ? 4 : rows <= 64 ? 2 : 1;
     const int64_t likely = n_seqs * ((rows * kp + 127) / 128) * c.n_kv_heads;

@@ -8,8 +8,8 @@
 // D features is D * size / 32 lanes with two 16-byte pieces each: with pairs (j, j + r/2) the pieces hold the two features of every pair, with
 // neighbours as pairs each piece has its own.
 //
-// Angle: revolutions per position are a 64-bit fraction, so position * turns modulo 2^64 is the exact fraction of a
-// revolution up to the rounding of the frequency (2^-54 per position, 2^-23 of a revolution at position 2^31).
+// Angle: revolutions per position are a 64-bit fraction, so position * turns modulo 2^64 is the fraction of a revolution up to that fraction's own error times the position.  It is
+// three roundings of 64-bit mantissas and the cut to 64 bits, below 2^-61 of a revolution (times the revolutions per position, where there are more than one): 2^-30 at position 2^31.
 // The top two bits after adding an eighth give the quadrant, the rest is an angle within +-1/8 revolution, for which fp32 has 2^-28.
 #include "kv_device.h"
 

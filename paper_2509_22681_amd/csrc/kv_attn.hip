@@ -5,8 +5,8 @@
 //
 // A workgroup takes 128 query rows of one sequence and key head, row = token * G + head of the
 // group (the G query heads that share a key head are rows of one tile: short sequences fill it, and the mask cuts through fewer key tiles), four wavefronts of 32 rows each.  It
-// walks the keys in tiles of 64, two stages in LDS, brought there by LDS-DMA loads one tile ahead.  In small launches two or four wavefronts share 32 rows and take a part of each
-// tile's keys, with a maximum, sum and accumulator of their own that are joined at the end (kv_route in kv_api.cpp).  Products are transposed as in attn_mfma.hip,
+// walks the keys in tiles of 32 or 64 (key_block), two stages in LDS, brought there by LDS-DMA loads one tile ahead.  In small launches two or four wavefronts share 32 rows and take 32
+// or 64 keys each of tiles that are two or four times as long, with a maximum, sum and accumulator of their own that are joined at the end (kv_route in kv_api.cpp).  Products are transposed as in attn_mfma.hip,
 //     S^T[key][row] = K Q^T        A operand = K rows, B operand = Q rows
 //     O^T[feature][row] += V^T P^T A operand = V^T rows, B operand = P^T
 // so that the first product's accumulator, where a lane has one row and 16 of 32 keys, is the second product's B operand as it stands: elements 8 s + i of a lane in half h are keys
@@ -37,7 +37,7 @@ template <typename T, int DH, int KP> constexpr int flash_lds_bytes() {
   return stages > parts ? stages : parts;
 }
 // Workgroups of 4 wavefronts on a compute unit, as LDS and registers allow (three in place of two of heads of 64: 64 prompts of 512..1024, 8 heads, 142 -> 114 us, one of 16384 395 -> 352;
-// four in place of three of 32 features 185 -> 165, fp32 three in place of two 622 -> 561).
+// four in place of three of 32 features 185 -> 165, fp32 three in place of two 622 -> 561).  Heads of 32 spill 1 to 4 registers at these bounds, none of it between the products.
 template <typename T, int DH, int KP> constexpr int flash_workgroups() {
   constexpr int lds = flash_lds_bytes<T, DH, KP>();
   return lds > 72 * 1024 ? 1 : DH == 32 && sizeof(T) == 2 && lds <= 32 * 1024 ? 4 : DH * sizeof(T) <= 128 && lds <= 40 * 1024 ? 3 : 2;

@@ -23,7 +23,9 @@ namespace flame {
 
 namespace {
 
-// Wavefronts per SIMD, as their registers allow, and in all.
+// Wavefronts per SIMD, as their registers allow, and in all.  Two tiles in flight fill the registers: 128 features spill 11 to 13 of 256 (48 to 56 bytes a lane), and scalars go to lanes of
+// others (some 350 of 128 features in 16 bits, fewer in the rest).  Decoding of many keys runs at
+// memory speed all the same.
 constexpr int split_occupancy(int dh) { return dh == 128 ? 2 : dh == 64 ? 3 : 4; }
 constexpr int split_workers(int dh) { return 1024 * split_occupancy(dh); }
 constexpr int kRows = 16;           // query rows of a unit

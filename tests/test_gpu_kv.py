@@ -917,7 +917,7 @@ def test_append_reports_offsets_and_writes_the_rest(B):
 
 def test_fp16_weights_far_below_the_largest(B):
     """One key with a logit of 17.47 and a value of 0, thousands with logits of 0 and values of 1: weights of 2^-25.2, which fp16 does not have, make up the result together.
-    An fp16 weight is off by half a step or by 2^-32 of the row's largest (2^-40 where the keys are split), which is what attention_bound's last term has 2^-25 for."""
+    An fp16 weight is off by half a step or by 2^-32 of the row's largest (2^-40 where the keys are split)."""
     import torch
     c = float(np.float16(17.47))
     w, n = math.exp(-c), 4096
