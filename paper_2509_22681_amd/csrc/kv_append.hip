@@ -41,8 +41,9 @@ __global__ __launch_bounds__(64 * kTokensPerBlock) void kv_append_kernel(KvBatch
   constexpr int E = 16 / sizeof(T);
   __shared__ float2 turn_s[kTokensPerBlock][kMaxRotationPairs];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  if (blockIdx.x == 0 && batch.faults)
-    for (int b = threadIdx.x; b < batch.n_seqs; b += 64 * kTokensPerBlock) kv_report_offsets(batch.offsets[b], batch.offsets[b + 1], batch.n_rows, batch.faults);
+  if (batch.faults)
+    for (int64_t b = (int64_t)blockIdx.x * (64 * kTokensPerBlock) + threadIdx.x; b < batch.n_seqs; b += (int64_t)gridDim.x * (64 * kTokensPerBlock))
+      kv_report_offsets(batch.offsets[b], batch.offsets[b + 1], batch.n_rows, batch.faults);
   const int64_t token = (int64_t)blockIdx.x * kTokensPerBlock + wave;
   if (token >= batch.n_rows) return;
   const int seq = kv_find_sequence(batch.offsets, batch.n_seqs, token, lane);

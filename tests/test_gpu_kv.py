@@ -1009,3 +1009,72 @@ def test_rows_without_a_logit_above_minus_infinity(B, dtype, dim):
             out.fill_(7.0)
             B.flame_kv_decode(cfg, cache, q, lens, out, workspace_for(B, cfg, seqs))
             assert not bool(out.any()), "decode"
+
+
+@pytest.mark.parametrize("n_seqs", [1, 63, 64, 65, 129, 700, 4096, 4200])
+@pytest.mark.parametrize("ahead", [0, 5])
+def test_append_of_many_sequences(B, n_seqs, ahead):
+    """More sequences than lanes, most of them with a token or none, with rows ahead of the first and behind the last one: every token in its slot, and nothing else written."""
+    import torch
+    gen, rng = generator(n_seqs), np.random.default_rng(n_seqs)
+    new = rng.integers(0, 3, n_seqs)
+    new[[0, n_seqs // 2, n_seqs - 1]] = [7, 70, 3]
+    lens = new + rng.integers(0, 20, n_seqs)
+    off, n = offsets(new) + ahead, int(new.sum())
+    used = -(-lens // 16)
+    table = np.full((n_seqs, int(used.max())), -7, np.int32)
+    order = rng.permutation(int(used.sum()))
+    for b, first in enumerate(np.cumsum(used) - used):
+        table[b, :used[b]] = order[first:first + used[b]]
+    cfg = B.make_kv_config("f16", 2, 1, 32)
+    k_pool, v_pool = (torch.zeros(len(order), 16, 1, 32, device=DEV, dtype=torch.float16) for _ in range(2))
+    k, v, q = rand(gen, "f16", n + ahead + 6, 1, 32), rand(gen, "f16", n + ahead + 6, 1, 32), rand(gen, "f16", n + ahead + 6, 2, 32)
+    q_out, fault = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    cache = B.pack_kv_cache(cfg, k_pool, v_pool, ints(table))
+    B.flame_kv_append(cfg, cache, k, v, ints(off), ints(lens), q=q, q_out=q_out, faults=fault)
+    seq = np.repeat(np.arange(n_seqs), new)
+    position = np.arange(n) - (off - ahead)[seq + 1] + lens[seq]
+    page, slot = (torch.tensor(x, device=DEV).long() for x in (table[seq, position // 16], position % 16))
+    for pool, x in ((k_pool, k), (v_pool, v)):
+        want = torch.zeros_like(pool)
+        want[page, slot] = x[ahead:ahead + n]
+        assert torch.equal(pool, want)
+    assert int(fault[0]) == 0
+    assert torch.equal(q_out[ahead:ahead + n], q[ahead:ahead + n]) and bool((q_out[:ahead] == 7.0).all()) and bool((q_out[ahead + n:] == 7.0).all())
+    # the last sequence's end behind the rows is seen, whichever workgroup looks at it
+    off[-1] += 100
+    B.flame_kv_append(cfg, cache, k, v, ints(off), ints(lens + 100 * (np.arange(n_seqs) == n_seqs - 1)), faults=fault)
+    assert int(fault[0]) & 4
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("n_seqs", [3, 64, 65, 300])
+def test_attention_with_rows_ahead_of_the_first_sequence(B, dtype, n_seqs):
+    """offsets that do not begin at 0, as those of a part of a larger batch: row tiles, in parts, split."""
+    import torch
+    gen, rng, ahead = generator(23), np.random.default_rng(n_seqs), 40
+    new = rng.integers(0, 4, n_seqs)
+    new[[0, n_seqs - 1]] = [50, 33]
+    off, n = offsets(new) + ahead, int(new.sum()) + ahead
+    lens = new + rng.integers(0, 30, n_seqs)
+    lens[0] = 900
+    for room, hq in ((0, 4), (4096, 16), (4096, 2)):
+        c = Cache(B, gen, dtype, hq, 2, 64, lens.tolist(), 16, tokens=room)
+        q, k = rand(gen, dtype, n + 7, hq, 64), rand(gen, dtype, n + 7, 2, 64)
+        pool_k, pool_v = host(c.k), host(c.v)
+        for kind in ("prompt", "extend"):
+            out, fault = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+            if kind == "prompt":
+                B.flame_kv_prompt(c.cfg, q, k, k, ints(off), out, faults=fault)
+            else:
+                B.flame_kv_extend(c.cfg, c.packed, q, ints(off), ints(lens), out, workspace_for(B, c.cfg, n_seqs, n + 7), faults=fault)
+            assert int(fault[0]) == 0
+            assert bool((out[:ahead] == 7.0).all()) and bool((out[n:] == 7.0).all())
+            for b in [0, n_seqs // 2, n_seqs - 1]:
+                s = slice(off[b], off[b + 1])
+                if kind == "prompt":
+                    keys = values = host(k[s])
+                else:
+                    page, slot, _ = kv_oracle.page_rows(c.table_host[b], 16, c.n_pages, int(lens[b]))
+                    keys, values = pool_k[page, slot], pool_v[page, slot]
+                check_attention(host(out[s]), host(q[s]), keys, values, dtype, what=(kind, room, hq, b))
