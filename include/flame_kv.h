@@ -125,6 +125,28 @@ int flame_kv_extend(const flame_kv_config *cfg, const flame_kv_cache *cache, con
 int flame_kv_decode(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *kv_lens, int32_t n_seqs,
                     const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream);
 
+/* Groups of sequences that begin with the same tokens: sequences group_offsets[g]..group_offsets[g+1] share the first tokens of the first of them. */
+typedef struct {
+  const int32_t *group_offsets; /* device [n_groups+1], from 0 to n_seqs */
+  const int32_t *prefix_lens;   /* device [n_seqs]: so many first tokens of a sequence are those of its group's first sequence, whose own entry is the largest of the group */
+  int32_t n_groups;
+} flame_kv_groups;
+
+/* Attention of the newest tokens of every sequence over its cache, as flame_kv_extend (q_offsets NULL: one new token each, row b of sequence b, as flame_kv_decode), for sequences that
+ * share long beginnings: what a group shares is read once for all rows of the group, where the table row of its first sequence says (which names the group's prefix_lens tokens, whatever
+ * that sequence's own length).  Keys from prefix_lens[b] on are sequence b's own, where its own row of the table says; entries of that row for pages of shared tokens alone are not read.
+ * kv_lens count both.  A shared history may end within a page, a sequence within the shared history (its rows see their own positions, as ever), and a sequence may leave the history
+ * earlier than others do (its prefix_lens is less).  The outputs are those of flame_kv_extend on tables that say the same; sums are cut differently, so the last bits may differ.
+ *   faults       FLAME_KV_FAULT_LENGTH also for a prefix_lens below 0, beyond the table's row, or beyond that of the group's first sequence (tokens from there on are not seen);
+ *                FLAME_KV_FAULT_OFFSET also for group_offsets that decrease, are below 0, or do not go from 0 to n_seqs: a sequence that is in no group, or of up to 64 groups in one
+ *                behind offsets that are none, sees its own tokens alone.  (Of more groups, which rows see what is not defined.)
+ *   workspace    of flame_kv_shared_workspace_bytes bytes for these numbers or larger ones; as in flame_kv_extend */
+int flame_kv_shared(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *q_offsets, const int32_t *kv_lens, const flame_kv_groups *groups,
+                    int32_t n_seqs, int64_t n_tokens, const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream);
+
+/* HOST arithmetic: a workspace for every flame_kv_shared (and flame_kvq_shared) of this configuration with up to so many groups, sequences and query rows. */
+int flame_kv_shared_workspace_bytes(const flame_kv_config *cfg, int32_t n_groups, int32_t n_seqs, int64_t n_tokens, int64_t *bytes);
+
 /* HOST arithmetic: a workspace for every flame_kv_extend and flame_kv_decode of this configuration with up to so many sequences and query rows:
  * a program asks once, for its largest batch. */
 int flame_kv_workspace_bytes(const flame_kv_config *cfg, int32_t n_seqs, int64_t n_tokens, int64_t *bytes);

@@ -178,8 +178,35 @@ _lib.flame_kv_rotation_frequencies.restype = C.c_int
 _lib.flame_kv_last_error.argtypes = []
 _lib.flame_kv_last_error.restype = C.c_char_p
 
-KV_EXPORTS = ("flame_kv_append", "flame_kv_prompt", "flame_kv_extend", "flame_kv_decode", "flame_kv_workspace_bytes", "flame_kv_rotation_frequencies",
-              "flame_kv_last_error")
+
+class flame_kv_groups(C.Structure):
+    _fields_ = [("group_offsets", C.c_void_p), ("prefix_lens", C.c_void_p), ("n_groups", C.c_int32)]
+
+
+class flame_kvq_cache(C.Structure):
+    _fields_ = [("form", C.c_int32), ("k", C.c_void_p), ("v", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p), ("page_stride", C.c_int64), ("slot_stride", C.c_int64),
+                ("head_stride", C.c_int64), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("page_table", C.c_void_p), ("table_stride", C.c_int64), ("pages_per_seq", C.c_int32)]
+
+
+_kvq_cache_p, _kv_groups_p = C.POINTER(flame_kvq_cache), C.POINTER(flame_kv_groups)
+for _name, _cache in (("flame_kv_shared", _kv_cache_p), ("flame_kvq_shared", _kvq_cache_p)):
+    getattr(_lib, _name).argtypes = [_kv_cfg, _cache, _kv_rows_p, C.c_void_p, C.c_void_p, _kv_groups_p, C.c_int32, C.c_int64, _kv_rows_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+    getattr(_lib, _name).restype = C.c_int
+_lib.flame_kv_shared_workspace_bytes.argtypes = [_kv_cfg, C.c_int32, C.c_int32, C.c_int64, C.POINTER(C.c_int64)]
+_lib.flame_kv_shared_workspace_bytes.restype = C.c_int
+_lib.flame_kvq_append.argtypes = [_kv_cfg, _kvq_cache_p, _kv_rows_p, _kv_rows_p, _kv_rows_p, _kv_rows_p, C.POINTER(flame_kv_rotation), C.c_void_p, C.c_void_p,
+                                  C.c_int32, C.c_int64, C.c_void_p, C.c_void_p]
+_lib.flame_kvq_append.restype = C.c_int
+_lib.flame_kvq_read.argtypes = [_kv_cfg, _kvq_cache_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, _kv_rows_p, _kv_rows_p, C.c_void_p, C.c_void_p]
+_lib.flame_kvq_read.restype = C.c_int
+_lib.flame_kvq_extend.argtypes = [_kv_cfg, _kvq_cache_p, _kv_rows_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, _kv_rows_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+_lib.flame_kvq_extend.restype = C.c_int
+_lib.flame_kvq_decode.argtypes = [_kv_cfg, _kvq_cache_p, _kv_rows_p, C.c_void_p, C.c_int32, _kv_rows_p, C.c_void_p, C.c_int64, C.c_void_p, C.c_void_p]
+_lib.flame_kvq_decode.restype = C.c_int
+
+KV_EXPORTS = ("flame_kv_append", "flame_kv_prompt", "flame_kv_extend", "flame_kv_decode", "flame_kv_shared", "flame_kv_workspace_bytes", "flame_kv_shared_workspace_bytes",
+              "flame_kv_rotation_frequencies", "flame_kv_last_error")
+KVQ_EXPORTS = ("flame_kvq_append", "flame_kvq_read", "flame_kvq_extend", "flame_kvq_decode", "flame_kvq_shared")
 
 CLIMBER_EXPORTS = ("flame_climber_head", "flame_climber_block_range", "flame_climber_last_error")
 
@@ -718,6 +745,136 @@ def flame_kv_decode(cfg, cache, q, kv_lens, out, workspace=None, faults=None, st
                               _kv_rows(cfg, out, cfg.n_q_heads, dev, "out", True), wp, wb, None if faults is None else _kv_ints(faults, 1, dev, "faults"), _kv_stream(stream, dev))
     if rc:
         _kv_check(rc)
+
+
+def flame_kv_shared_workspace_bytes(cfg: flame_kv_config, n_groups: int, n_seqs: int, n_tokens: Optional[int] = None) -> int:
+    """Bytes of a workspace for every flame_kv_shared and flame_kvq_shared of up to this many groups, sequences and query rows (n_tokens None: one row each)."""
+    out = C.c_int64(0)
+    _kv_check(_lib.flame_kv_shared_workspace_bytes(C.byref(cfg), n_groups, n_seqs, n_seqs if n_tokens is None else n_tokens, C.byref(out)))
+    return out.value
+
+
+def _kv_shared(call, cfg, cache, q, q_offsets, kv_lens, group_offsets, prefix_lens, out, workspace, faults, stream) -> None:
+    n_seqs, n_groups, n, dev = len(kv_lens), len(group_offsets) - 1, len(q), torch.cuda.current_device()
+    if len(out) != n or (q_offsets is None and n != n_seqs):
+        raise ValueError("out must have the rows of q, and without q_offsets those are one per sequence")
+    wp, wb = _kv_workspace(workspace, dev)
+    groups = flame_kv_groups(_kv_ints(group_offsets, n_groups + 1, dev, "group_offsets"), _kv_ints(prefix_lens, n_seqs, dev, "prefix_lens"), n_groups)
+    rc = call(cfg, cache, _kv_rows(cfg, q, cfg.n_q_heads, dev, "q"), None if q_offsets is None else _kv_ints(q_offsets, n_seqs + 1, dev, "q_offsets"), _kv_ints(kv_lens, n_seqs, dev, "kv_lens"),
+              C.byref(groups), n_seqs, n, _kv_rows(cfg, out, cfg.n_q_heads, dev, "out", True), wp, wb, None if faults is None else _kv_ints(faults, 1, dev, "faults"), _kv_stream(stream, dev))
+    if rc:
+        _kv_check(rc)
+
+
+def flame_kv_shared(cfg, cache, q, q_offsets, kv_lens, group_offsets, prefix_lens, out, workspace=None, faults=None, stream=None) -> None:
+    """flame_kv_extend (q_offsets None: flame_kv_decode) for groups of sequences that begin with the same tokens: sequences group_offsets[g]..group_offsets[g + 1] share their first
+    prefix_lens[b] tokens with the first of them.  group_offsets [n_groups + 1], prefix_lens [n_seqs]: device int32; workspace: of flame_kv_shared_workspace_bytes bytes."""
+    _kv_shared(_lib.flame_kv_shared, cfg, _kv_cache_for(cfg, cache, len(kv_lens), torch.cuda.current_device()), q, q_offsets, kv_lens, group_offsets, prefix_lens, out, workspace, faults, stream)
+
+
+# ---------------------------------------------------------------------------------------------
+# the cache in 8 or 4 bits (include/flame_kvq.h)
+# ---------------------------------------------------------------------------------------------
+FLAME_KVQ_F8, FLAME_KVQ_F4 = 1, 2
+_KVQ_FORMS = {"f8": FLAME_KVQ_F8, "f4": FLAME_KVQ_F4}
+
+
+def make_kvq_pool(cfg: flame_kv_config, form, n_pages: int, page_size: int, device="cuda:0"):
+    """k_pool, v_pool, k_scales, v_scales of zeros for pack_kvq_cache: uint8 [n_pages, page_size, n_kv_heads, head_dim (f8) or head_dim / 2 (f4)] and [..., head_dim / 32]."""
+    row = cfg.head_dim // {FLAME_KVQ_F8: 1, FLAME_KVQ_F4: 2}[_KVQ_FORMS.get(form, form)]
+    shapes = [(n_pages, page_size, cfg.n_kv_heads, row)] * 2 + [(n_pages, page_size, cfg.n_kv_heads, cfg.head_dim // 32)] * 2
+    return tuple(torch.zeros(s, dtype=torch.uint8, device=device) for s in shapes)
+
+
+def pack_kvq_cache(cfg: flame_kv_config, form, k_pool, v_pool, k_scales, v_scales, page_table) -> flame_kvq_cache:
+    """form: "f8" or "f4"; pools: device uint8 [n_pages, page_size, n_kv_heads, head_dim (f8) or head_dim / 2 (f4)] (any strides, the same for both, a head's bytes side by side and the other
+    strides multiples of them); scales: uint8 [n_pages, page_size, n_kv_heads, head_dim / 32], with strides that are the pools' by 32 (f8) or 16 (f4); page_table: device int32
+    [n_seqs, pages_per_seq].  The struct keeps the tensors alive; their contents may change."""
+    form = _KVQ_FORMS.get(form, form)
+    if form not in (FLAME_KVQ_F8, FLAME_KVQ_F4) or cfg.torch_dtype is None:
+        raise ValueError('form must be "f8" or "f4", and the configuration one of make_kv_config')
+    bits = 8 if form == FLAME_KVQ_F8 else 4
+    n_pages, page_size, heads, row = k_pool.shape
+    if heads != cfg.n_kv_heads or row * 8 != cfg.head_dim * bits or k_pool.dtype is not torch.uint8:
+        raise ValueError(f"k_pool must be [n_pages, page_size, {cfg.n_kv_heads}, {cfg.head_dim * bits // 8}] of torch.uint8")
+    if v_pool.shape != k_pool.shape or v_pool.dtype is not torch.uint8 or v_pool.device != k_pool.device:
+        raise ValueError("v_pool must be like k_pool")
+    for t in (k_scales, v_scales):
+        if tuple(t.shape) != (n_pages, page_size, heads, cfg.head_dim // 32) or t.dtype is not torch.uint8 or t.device != k_pool.device:
+            raise ValueError(f"scales must be [n_pages, page_size, {heads}, {cfg.head_dim // 32}] of torch.uint8 beside the pools")
+    if page_table.dtype is not torch.int32 or page_table.dim() != 2 or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table must be int32 [n_seqs, pages_per_seq], the entries of a row side by side")
+    if not k_pool.is_cuda or page_table.device != k_pool.device:
+        raise ValueError("the pools and the page table must be on one device")
+    used = [i for i in range(3) if k_pool.shape[i] > 1]
+    if [k_pool.stride(i) for i in used] != [v_pool.stride(i) for i in used] or k_pool.stride(3) != 1 or v_pool.stride(3) != 1:
+        raise ValueError("k_pool and v_pool must have the same strides, and a head's bytes side by side")
+    if any(k_pool.stride(i) == 0 for i in used):
+        raise ValueError("the pools must not be expanded tensors")
+    for t in (k_scales, v_scales):
+        if [t.stride(i) * bits * 4 for i in used] != [k_pool.stride(i) for i in used] or (t.shape[3] > 1 and t.stride(3) != 1):
+            raise ValueError("the scales' strides must be the pools' by 32 (f8) or 16 (f4), and a head's scales side by side")
+    stride = [k_pool.stride(i) if k_pool.shape[i] > 1 else 0 for i in range(3)]
+    c = flame_kvq_cache(form, k_pool.data_ptr(), v_pool.data_ptr(), k_scales.data_ptr(), v_scales.data_ptr(), *stride, n_pages, page_size, page_table.data_ptr(),
+                        page_table.stride(0) if page_table.shape[0] > 1 else 0, page_table.shape[1])
+    c.tensors = (k_pool, v_pool, k_scales, v_scales, page_table)
+    c.n_seqs, c.device, c.shape = page_table.shape[0], k_pool.get_device(), (cfg.dtype, heads, cfg.head_dim)
+    return c
+
+
+def flame_kvq_append(cfg, cache, k, v, offsets, kv_lens, q=None, q_out=None, rotation=None, faults=None, stream=None) -> None:
+    """flame_kv_append into a cache of pack_kvq_cache: keys and values are quantised as they are written."""
+    n_seqs, n, dev = len(kv_lens), len(k), torch.cuda.current_device()
+    if len(v) != n or (q is None) != (q_out is None) or (q is not None and not len(q) == len(q_out) == n):
+        raise ValueError("k, v, q and q_out must have the same rows, and q comes with q_out")
+    rc = _lib.flame_kvq_append(cfg, _kv_cache_for(cfg, cache, n_seqs, dev), _kv_rows(cfg, k, cfg.n_kv_heads, dev, "k"), _kv_rows(cfg, v, cfg.n_kv_heads, dev, "v"),
+                               None if q is None else _kv_rows(cfg, q, cfg.n_q_heads, dev, "q"), None if q is None else _kv_rows(cfg, q_out, cfg.n_q_heads, dev, "q_out", True),
+                               rotation, _kv_ints(offsets, n_seqs + 1, dev, "offsets"), _kv_ints(kv_lens, n_seqs, dev, "kv_lens"), n_seqs, n,
+                               None if faults is None else _kv_ints(faults, 1, dev, "faults"), _kv_stream(stream, dev))
+    if rc:
+        _kv_check(rc)
+
+
+def flame_kvq_read(cfg, cache, offsets, kv_lens, k, v, faults=None, stream=None) -> None:
+    """k, v: device rows [n_tokens, n_kv_heads, head_dim], written: rows offsets[b]..offsets[b + 1] are the tokens of sequence b up to its kv_lens[b]-th, as the cache holds them."""
+    n_seqs, n, dev = len(kv_lens), len(k), torch.cuda.current_device()
+    if len(v) != n:
+        raise ValueError("k and v must have the same rows")
+    rc = _lib.flame_kvq_read(cfg, _kv_cache_for(cfg, cache, n_seqs, dev), _kv_ints(offsets, n_seqs + 1, dev, "offsets"), _kv_ints(kv_lens, n_seqs, dev, "kv_lens"), n_seqs, n,
+                             _kv_rows(cfg, k, cfg.n_kv_heads, dev, "k", True), _kv_rows(cfg, v, cfg.n_kv_heads, dev, "v", True),
+                             None if faults is None else _kv_ints(faults, 1, dev, "faults"), _kv_stream(stream, dev))
+    if rc:
+        _kv_check(rc)
+
+
+def flame_kvq_extend(cfg, cache, q, q_offsets, kv_lens, out, workspace=None, faults=None, stream=None) -> None:
+    """flame_kv_extend over a cache of pack_kvq_cache (workspace: flame_kv_workspace_bytes)."""
+    n_seqs, n, dev = len(kv_lens), len(q), torch.cuda.current_device()
+    if len(out) != n:
+        raise ValueError("out must have the rows of q")
+    wp, wb = _kv_workspace(workspace, dev)
+    rc = _lib.flame_kvq_extend(cfg, _kv_cache_for(cfg, cache, n_seqs, dev), _kv_rows(cfg, q, cfg.n_q_heads, dev, "q"), _kv_ints(q_offsets, n_seqs + 1, dev, "q_offsets"),
+                               _kv_ints(kv_lens, n_seqs, dev, "kv_lens"), n_seqs, n, _kv_rows(cfg, out, cfg.n_q_heads, dev, "out", True), wp, wb,
+                               None if faults is None else _kv_ints(faults, 1, dev, "faults"), _kv_stream(stream, dev))
+    if rc:
+        _kv_check(rc)
+
+
+def flame_kvq_decode(cfg, cache, q, kv_lens, out, workspace=None, faults=None, stream=None) -> None:
+    """flame_kv_decode over a cache of pack_kvq_cache (workspace: flame_kv_workspace_bytes)."""
+    n_seqs, dev = len(kv_lens), torch.cuda.current_device()
+    if len(q) != n_seqs or len(out) != n_seqs:
+        raise ValueError("q and out must have one row per sequence")
+    wp, wb = _kv_workspace(workspace, dev)
+    rc = _lib.flame_kvq_decode(cfg, _kv_cache_for(cfg, cache, n_seqs, dev), _kv_rows(cfg, q, cfg.n_q_heads, dev, "q"), _kv_ints(kv_lens, n_seqs, dev, "kv_lens"), n_seqs,
+                               _kv_rows(cfg, out, cfg.n_q_heads, dev, "out", True), wp, wb, None if faults is None else _kv_ints(faults, 1, dev, "faults"), _kv_stream(stream, dev))
+    if rc:
+        _kv_check(rc)
+
+
+def flame_kvq_shared(cfg, cache, q, q_offsets, kv_lens, group_offsets, prefix_lens, out, workspace=None, faults=None, stream=None) -> None:
+    """flame_kv_shared over a cache of pack_kvq_cache."""
+    _kv_shared(_lib.flame_kvq_shared, cfg, _kv_cache_for(cfg, cache, len(kv_lens), torch.cuda.current_device()), q, q_offsets, kv_lens, group_offsets, prefix_lens, out, workspace, faults, stream)
 
 
 # ---------------------------------------------------------------------------------------------

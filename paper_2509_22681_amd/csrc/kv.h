@@ -4,6 +4,7 @@
 #include <stdint.h>
 
 #include "../../include/flame_kv.h"
+#include "../../include/flame_kvq.h"
 #include "kv_index.h"
 
 namespace flame {
@@ -12,6 +13,12 @@ namespace flame {
 struct KvRows {
   char *p;
   int64_t row, head;
+};
+
+// of a quantised cache: where the scale bytes lie, and its flame_kvq_form
+struct KvScales {
+  char *k, *v;
+  int32_t form;
 };
 
 constexpr int kMaxRotationPairs = 64;
@@ -39,6 +46,10 @@ struct KvAttention {
   float scale;
   int32_t splits;             // flash kernel over pages: parts of a row tile's keys
   float *parts;
+  int32_t form;               // of the pages: 0 as the element type, or a flame_kvq_form
+  const char *k_scales, *v_scales;
+  const int32_t *group_offsets, *prefix_lens;   // shared histories (else NULL)
+  int32_t n_groups;
 };
 
 // How a call runs (kv_api.cpp): split kernel, or flash kernel with so many wavefronts per 32 rows and parts of the keys.
@@ -51,6 +62,12 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
 
 hipError_t launch_kv_append(const KvBatch &batch, const KvPages &pages, const KvRows &k, const KvRows &v, const KvRows *q, const KvRows *q_out,
                             const KvRotation &rotation, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, hipStream_t stream);
+// quantised caches: as above, and rows back out of one
+hipError_t launch_kvq_append(const KvBatch &batch, const KvPages &pages, const KvScales &scales, const KvRows &k, const KvRows &v, const KvRows *q, const KvRows *q_out,
+                             const KvRotation &rotation, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, hipStream_t stream);
+hipError_t launch_kvq_read(const KvBatch &batch, const KvPages &pages, const KvScales &scales, const KvRows &k, const KvRows &v, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                           hipStream_t stream);
+hipError_t launch_kvq_attention(const KvAttention &a, hipStream_t stream);
 hipError_t launch_kv_attention(const KvAttention &a, int wavefronts, hipStream_t stream);
 // few query rows: split over the keys (kv_split.hip)
 hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream);

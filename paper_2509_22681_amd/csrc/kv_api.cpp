@@ -69,6 +69,24 @@ int take_pages(const flame_kv_config *c, const flame_kv_cache *cache, KvPages *o
   return FLAME_GR_OK;
 }
 
+// of a quantised cache: strides are bytes of codes
+int take_pages(const flame_kv_config *c, const flame_kvq_cache *cache, KvPages *out, KvScales *scales) {
+  if (!cache) return bad("the cache is NULL");
+  if (cache->form != FLAME_KVQ_F8 && cache->form != FLAME_KVQ_F4) return bad("form must be a flame_kvq_form");
+  if (!cache->k || !cache->v || !cache->k_scales || !cache->v_scales || !cache->page_table) return bad("a pointer of the cache is NULL");
+  if (cache->n_pages < 1 || cache->page_size < 1 || cache->page_size > 65536) return bad("n_pages must be positive and page_size in [1, 65536]");
+  if (cache->pages_per_seq < 1 || (int64_t)cache->pages_per_seq * cache->page_size > kMaxKeys) return bad("pages_per_seq must be positive, and a sequence within 2^31 - 65536 tokens");
+  const int64_t row = cache->form == FLAME_KVQ_F8 ? c->head_dim : c->head_dim / 2;
+  if (!aligned(cache->k) || !aligned(cache->v) || ((uintptr_t)cache->k_scales & 3) || ((uintptr_t)cache->v_scales & 3)) return bad("pools must be 16-byte and scales 4-byte aligned");
+  if (cache->page_stride % row || cache->slot_stride % row || cache->head_stride % row) return bad("the strides of a quantised cache must be multiples of a head's bytes");
+  if (cache->page_stride < 0 || cache->slot_stride < 0 || cache->head_stride < 0) return bad("the strides of a quantised cache must not be negative");
+  *out = KvPages{(char *)cache->k, (char *)cache->v, cache->page_stride, cache->slot_stride, cache->head_stride, cache->n_pages, 0, 0, 0,
+                 cache->page_table, cache->table_stride, cache->pages_per_seq * cache->page_size};
+  kv_set_page_size(out, cache->page_size);
+  *scales = KvScales{(char *)cache->k_scales, (char *)cache->v_scales, cache->form};
+  return FLAME_GR_OK;
+}
+
 int take_rotation(const flame_kv_config *c, const flame_kv_rotation *r, KvRotation *out) {
   *out = KvRotation{};
   if (!r) return FLAME_GR_OK;
@@ -129,6 +147,61 @@ int attend_cache(const flame_kv_config *cfg, const flame_kv_cache *cache, const 
   a.splits = route.splits;
   a.parts = (float *)workspace;
   return done(launch_kv_attention(a, route.wavefronts, (hipStream_t)stream));
+}
+
+// The same over a quantised cache, and with shared histories (groups; the cache is then either).
+int attend_quantised(const flame_kv_config *cfg, const flame_kvq_cache *cache, const flame_kv_rows *q, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_rows,
+                     const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream) {
+  KvAttention a{};
+  KvScales scales;
+  if (int rc = take_rows(cfg, q, &a.q)) return rc;
+  if (int rc = take_rows(cfg, out, &a.out)) return rc;
+  if (int rc = take_pages(cfg, cache, &a.pages, &scales)) return rc;
+  if (!kv_lens) return bad("kv_lens is NULL");
+  const int64_t need = workspace_bytes_for(*cfg, n_seqs, n_rows, offsets == nullptr);
+  if (need > 0 && (!workspace || !aligned(workspace))) return bad("the workspace is NULL or not 16-byte aligned");
+  if (workspace_bytes < need) return bad("the workspace is smaller than this call needs (flame_kv_workspace_bytes)", FLAME_GR_CAPACITY_EXCEEDED);
+  a.batch = KvBatch{offsets, kv_lens, n_seqs, n_rows, faults};
+  take_heads(cfg, &a);
+  a.form = scales.form;
+  a.k_scales = scales.k;
+  a.v_scales = scales.v;
+  return done(launch_kvq_attention(a, (hipStream_t)stream));
+}
+
+int check_groups(const flame_kv_config *c, int32_t n_groups, int32_t n_seqs, int64_t n_rows) {
+  if (int rc = check_batch(c, n_seqs, n_rows)) return rc;
+  if (n_groups < 0 || (int64_t)n_groups * c->n_q_heads > kMaxSequenceHeads) return bad("groups times heads must be in [0, 2^23)");
+  return FLAME_GR_OK;
+}
+
+int attend_shared(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kvq_cache *quantised, bool plain, const flame_kv_rows *q, const int32_t *offsets,
+                  const int32_t *kv_lens, const flame_kv_groups *groups, int32_t n_seqs, int64_t n_rows, const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults,
+                  void *stream) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (!groups) return bad("the groups are NULL");
+  if (int rc = check_groups(cfg, groups->n_groups, n_seqs, n_rows)) return rc;
+  if (!offsets && n_rows != n_seqs) return bad("without q_offsets there is a row per sequence");
+  if (n_seqs == 0 || n_rows == 0) return FLAME_GR_OK;
+  KvAttention a{};
+  KvScales scales{};
+  if (int rc = take_rows(cfg, q, &a.q)) return rc;
+  if (int rc = take_rows(cfg, out, &a.out)) return rc;
+  if (int rc = plain ? take_pages(cfg, cache, &a.pages) : take_pages(cfg, quantised, &a.pages, &scales)) return rc;
+  if (!kv_lens || !groups->prefix_lens || !groups->group_offsets) return bad("kv_lens, group_offsets or prefix_lens is NULL");
+  const int64_t need = 0;
+  if (need > 0 && (!workspace || !aligned(workspace))) return bad("the workspace is NULL or not 16-byte aligned");
+  if (workspace_bytes < need) return bad("the workspace is smaller than this call needs (flame_kv_shared_workspace_bytes)", FLAME_GR_CAPACITY_EXCEEDED);
+  a.batch = KvBatch{offsets, kv_lens, n_seqs, n_rows, faults};
+  take_heads(cfg, &a);
+  a.form = scales.form;
+  a.k_scales = scales.k;
+  a.v_scales = scales.v;
+  a.group_offsets = groups->group_offsets;
+  a.prefix_lens = groups->prefix_lens;
+  a.n_groups = groups->n_groups;
+  return done(launch_kvq_attention(a, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -269,6 +342,84 @@ int flame_kv_decode(const flame_kv_config *cfg, const flame_kv_cache *cache, con
   if (int rc = check_batch(cfg, n_seqs, n_seqs)) return rc;
   if (n_seqs == 0) return FLAME_GR_OK;
   return attend_cache(cfg, cache, q, nullptr, kv_lens, n_seqs, n_seqs, out, workspace, workspace_bytes, faults, stream);
+}
+
+int flame_kv_shared_workspace_bytes(const flame_kv_config *cfg, int32_t n_groups, int32_t n_seqs, int64_t n_tokens, int64_t *bytes) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (int rc = check_groups(cfg, n_groups, n_seqs, n_tokens)) return rc;
+  if (!bytes) return bad("bytes is NULL");
+  *bytes = 0;
+  return FLAME_GR_OK;
+}
+
+int flame_kv_shared(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *q_offsets, const int32_t *kv_lens, const flame_kv_groups *groups,
+                    int32_t n_seqs, int64_t n_tokens, const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream) {
+  return attend_shared(cfg, cache, nullptr, true, q, q_offsets, kv_lens, groups, n_seqs, n_tokens, out, workspace, workspace_bytes, faults, stream);
+}
+
+int flame_kvq_shared(const flame_kv_config *cfg, const flame_kvq_cache *cache, const flame_kv_rows *q, const int32_t *q_offsets, const int32_t *kv_lens, const flame_kv_groups *groups,
+                     int32_t n_seqs, int64_t n_tokens, const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream) {
+  return attend_shared(cfg, nullptr, cache, false, q, q_offsets, kv_lens, groups, n_seqs, n_tokens, out, workspace, workspace_bytes, faults, stream);
+}
+
+int flame_kvq_append(const flame_kv_config *cfg, const flame_kvq_cache *cache, const flame_kv_rows *k, const flame_kv_rows *v, const flame_kv_rows *q, const flame_kv_rows *q_out,
+                     const flame_kv_rotation *rotation, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_tokens, int32_t *faults, void *stream) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
+  if (!q != !q_out) return bad("q and q_out go together");
+  KvRotation rot;
+  if (int rc = take_rotation(cfg, rotation, &rot)) return rc;
+  if (n_seqs == 0 || n_tokens == 0) return FLAME_GR_OK;
+  KvRows kr, vr, qr, qo;
+  if (int rc = take_rows(cfg, k, &kr)) return rc;
+  if (int rc = take_rows(cfg, v, &vr)) return rc;
+  if (q) {
+    if (int rc = take_rows(cfg, q, &qr)) return rc;
+    if (int rc = take_rows(cfg, q_out, &qo)) return rc;
+  }
+  KvPages pages;
+  KvScales scales;
+  if (int rc = take_pages(cfg, cache, &pages, &scales)) return rc;
+  if (!offsets || !kv_lens) return bad("offsets or kv_lens is NULL");
+  return done(launch_kvq_append(KvBatch{offsets, kv_lens, n_seqs, n_tokens, faults}, pages, scales, kr, vr, q ? &qr : nullptr, &qo, rot, cfg->n_q_heads, cfg->n_kv_heads, cfg->head_dim,
+                                cfg->dtype, (hipStream_t)stream));
+}
+
+int flame_kvq_read(const flame_kv_config *cfg, const flame_kvq_cache *cache, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_tokens, const flame_kv_rows *k,
+                   const flame_kv_rows *v, int32_t *faults, void *stream) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
+  if (n_seqs == 0 || n_tokens == 0) return FLAME_GR_OK;
+  KvRows kr, vr;
+  if (int rc = take_rows(cfg, k, &kr)) return rc;
+  if (int rc = take_rows(cfg, v, &vr)) return rc;
+  KvPages pages;
+  KvScales scales;
+  if (int rc = take_pages(cfg, cache, &pages, &scales)) return rc;
+  if (!offsets || !kv_lens) return bad("offsets or kv_lens is NULL");
+  return done(launch_kvq_read(KvBatch{offsets, kv_lens, n_seqs, n_tokens, faults}, pages, scales, kr, vr, cfg->n_kv_heads, cfg->head_dim, cfg->dtype, (hipStream_t)stream));
+}
+
+int flame_kvq_extend(const flame_kv_config *cfg, const flame_kvq_cache *cache, const flame_kv_rows *q, const int32_t *q_offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_tokens,
+                     const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (int rc = check_batch(cfg, n_seqs, n_tokens)) return rc;
+  if (n_seqs == 0 || n_tokens == 0) return FLAME_GR_OK;
+  if (!q_offsets) return bad("q_offsets is NULL");
+  return attend_quantised(cfg, cache, q, q_offsets, kv_lens, n_seqs, n_tokens, out, workspace, workspace_bytes, faults, stream);
+}
+
+int flame_kvq_decode(const flame_kv_config *cfg, const flame_kvq_cache *cache, const flame_kv_rows *q, const int32_t *kv_lens, int32_t n_seqs, const flame_kv_rows *out, void *workspace,
+                     int64_t workspace_bytes, int32_t *faults, void *stream) {
+  g_kv_error = "";
+  if (int rc = check_config(cfg)) return rc;
+  if (int rc = check_batch(cfg, n_seqs, n_seqs)) return rc;
+  if (n_seqs == 0) return FLAME_GR_OK;
+  return attend_quantised(cfg, cache, q, nullptr, kv_lens, n_seqs, n_seqs, out, workspace, workspace_bytes, faults, stream);
 }
 
 }  // extern "C"

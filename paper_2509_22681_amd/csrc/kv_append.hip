@@ -7,11 +7,7 @@
 // the cosine and sine of pair j once (up to 64 pairs: one per lane) and leaves them in LDS, from where the rows' lanes read theirs.  A row of
 // D features is D * size / 32 lanes with two 16-byte pieces each: with pairs (j, j + r/2) the pieces hold the two features of every pair, with
 // neighbours as pairs each piece has its own.
-//
-// Angle: revolutions per position are a 64-bit fraction, so position * turns modulo 2^64 is the fraction of a revolution up to that fraction's own error times the position.  It is
-// three roundings of 64-bit mantissas and the cut to 64 bits, below 2^-61 of a revolution (times the revolutions per position, where there are more than one): 2^-30 at position 2^31.
-// The top two bits after adding an eighth give the quadrant, the rest is an angle within +-1/8 revolution, for which fp32 has 2^-28.
-#include "kv_device.h"
+#include "kv_rotate.h"
 
 namespace flame {
 
@@ -20,19 +16,6 @@ namespace {
 constexpr int kTokensPerBlock = 4;
 
 template <typename T> struct Piece { typedef T vec __attribute__((ext_vector_type(16 / sizeof(T)))); };
-
-__device__ __forceinline__ float2 cos_sin_of_turn(uint64_t turn) {
-  const uint64_t shifted = turn + (1ull << 61);
-  const int quadrant = (int)(shifted >> 62);
-  const int64_t rest = (int64_t)(turn - ((uint64_t)quadrant << 62));      // within +-2^61
-  const float half_turns = (float)(int32_t)(rest >> 32) * 0x1p-31f;       // a revolution is 2^64, so half ones are rest / 2^63
-  float s, c;
-  sincospif(half_turns, &s, &c);
-  float2 r;
-  r.x = quadrant == 0 ? c : quadrant == 1 ? -s : quadrant == 2 ? -c : s;
-  r.y = quadrant == 0 ? s : quadrant == 1 ? c : quadrant == 2 ? -s : -c;
-  return r;
-}
 
 template <typename T>
 __global__ __launch_bounds__(64 * kTokensPerBlock) void kv_append_kernel(KvBatch batch, KvPages pages, KvRows k, KvRows v, KvRows q, KvRows q_out, KvRotation rot,

@@ -1,0 +1,582 @@
+"""The cache of 8 or 4 bits (include/flame_kvq.h) and attention over shared histories (flame_kv_shared, flame_kvq_shared) against the oracle in 64 bits.
+
+Tolerances.  Without rotation codes, scales and values read back are exact.  With it, a stored value is off by the half step that the header states (2^-4 or 2^-2 of the value, or
+2^-10 or 2^-2 of the block's scale), where the scale is at most twice the block's largest size over 464 or 7, and by the rotation's error ahead of it, 2^-21 of the pair's sizes.
+Attention is held to what flame_kv.h allows (tests/test_gpu_kv.py derives it) against the oracle on the values that the cache holds:
+u |o| + W (u_w + 2 ((dim + 7) 2^-24 Z + 2^-22) + 4 n 2^-24), and for f16 outputs 2^-24 and weights 2^-25 n max|v|."""
+import math
+
+import numpy as np
+import pytest
+
+from oracle import kv_oracle
+from test_gpu_kv import B, DEV, HALF_STEP, generator, host, ints, offsets, rand, torch_type  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+FORMS = ("f8", "f4")
+HALF = {"f8": (2.0 ** -4, 2.0 ** -10, 464.0), "f4": (2.0 ** -2, 2.0 ** -2, 7.0)}
+
+
+def check_attention(got, q, k, v, dtype, seen=None, what=""):
+    dim, n = q.shape[2], k.shape[0]
+    want, spread, size = kv_oracle.attend(q, k, v, dim ** -0.5, seen)
+    u = HALF_STEP[dtype]
+    d = (dim + 7) * 2.0 ** -24 * size[..., None] + 2.0 ** -22
+    bound = u * np.abs(want) + spread * ((0 if dtype == "f32" else u) + 2 * d + 4 * n * 2.0 ** -24) + 1e-30
+    if dtype == "f16":
+        bound = bound + 2.0 ** -24 + n * 2.0 ** -25 * (np.abs(v).max() if n else 0)
+    off = np.abs(got - want)
+    assert np.isfinite(got).all(), what
+    assert (off <= bound).all(), (what, float((off / bound).max()), float(off.max()))
+
+
+class Cache:
+    """Sequences of n tokens in scattered pages of a quantised pool (form None: a plain one) of random values, with pages that nobody has; groups: lists of sequences that share their
+    first p tokens' pages."""
+
+    def __init__(self, B, gen, form, dtype, hq, hkv, dim, lens, page, head_major=False, seed=0, tokens=0, groups=(), prefix=()):
+        import torch
+        self.B, self.form, self.page, self.lens, self.dtype = B, form, page, list(lens), dtype
+        self.cfg = B.make_kv_config(dtype, hq, hkv, dim)
+        full = np.zeros(len(lens), np.int64)
+        for g, p in zip(groups, prefix):
+            for b in g:
+                full[b] = p // page
+        need = np.array([max(0, -(-n // page)) for n in lens])
+        for g, p in zip(groups, prefix):
+            if g:
+                need[g[0]] = max(need[g[0]], -(-p // page))            # the first sequence's row names the whole history
+        own = np.maximum(0, need - full)
+        trunk = [p // page for g, p in zip(groups, prefix)]
+        self.n_pages = int(own.sum() + sum(trunk)) + 3
+        order = list(np.random.default_rng(seed).permutation(self.n_pages))
+        self.table_host = np.full((len(lens), max(int(need.max(initial=1)) + 1, -(-tokens // page))), -7, np.int32)
+        for g, t in zip(groups, trunk):
+            pages = [order.pop() for _ in range(t)]
+            for i, b in enumerate(g):
+                # (the rows of others name no pages where these are shared alone)
+                self.table_host[b, :t] = pages if i == 0 else -7
+        for b in range(len(lens)):
+            self.table_host[b, full[b]:full[b] + own[b]] = [order.pop() for _ in range(own[b])]
+        self.table = ints(self.table_host)
+        shape = (self.n_pages, hkv, page, dim) if head_major else (self.n_pages, page, hkv, dim)
+        turn = (lambda t: t.transpose(1, 2)) if head_major else (lambda t: t)
+        if form is None:
+            self.k, self.v = turn(rand(gen, dtype, *shape)), turn(rand(gen, dtype, *shape))
+            self.pack()
+            return
+        parts = {}
+        for x in "kv":
+            codes, scales, _ = kv_oracle.quantise(host(rand(gen, dtype, *shape)), form, dtype)
+            codes = codes if form == "f8" else codes[..., 0::2] | codes[..., 1::2] << 4
+            parts[x] = turn(torch.tensor(codes.astype(np.uint8), device=DEV))
+            parts[x + "s"] = turn(torch.tensor(scales.astype(np.uint8), device=DEV))
+        self.k, self.v, self.ks, self.vs = parts["k"], parts["v"], parts["ks"], parts["vs"]
+        self.pack()
+
+    def pack(self):
+        self.packed = self.B.pack_kv_cache(self.cfg, self.k, self.v, self.table) if self.form is None else \
+            self.B.pack_kvq_cache(self.cfg, self.form, self.k, self.v, self.ks, self.vs, self.table)
+
+    def pools(self):
+        """Values of the pools, in 64 bits."""
+        if self.form is None:
+            return host(self.k), host(self.v)
+        return tuple(kv_oracle.stored_values(kv_oracle.unpack(p.cpu().numpy(), self.form), s.cpu().numpy(), self.form) for p, s in ((self.k, self.ks), (self.v, self.vs)))
+
+    def rows(self, b, n, trunk=0, trunk_seq=0, pools=None):
+        """Keys and values of tokens 0..n-1 of sequence b, the first `trunk` of them where sequence trunk_seq has them."""
+        k, v = pools or self.pools()
+        t = np.arange(n)
+        page = np.where(t < trunk, self.table_host[trunk_seq, t // self.page], self.table_host[b, t // self.page])
+        return k[page, t % self.page], v[page, t % self.page]
+
+
+def call(B, c, op, *args, **more):
+    return getattr(B, ("flame_kv_" if c.form is None else "flame_kvq_") + op)(c.cfg, c.packed, *args, **more)
+
+
+# ---------------------------------------------------------------------------------------------- append and read
+APPENDS = [("f8", "bf16", 8, 2, 64, 64, False, 16, False), ("f4", "bf16", 32, 8, 128, 128, True, 24, True), ("f8", "f16", 4, 4, 32, 32, False, 1, False), ("f4", "f16", 6, 1, 128, 64, False, 7, False),
+           ("f8", "f32", 8, 8, 64, 32, True, 100, True), ("f4", "f32", 3, 3, 128, 128, False, 16, False), ("f4", "bf16", 5, 5, 32, 16, True, 64, False), ("f8", "bf16", 4, 2, 128, 16, False, 16, True),
+           ("f8", "f32", 2, 1, 32, 0, False, 5, False), ("f4", "bf16", 3, 3, 64, 0, False, 16, True), ("f8", "f16", 20, 20, 128, 48, False, 33, False), ("f4", "f32", 2, 2, 32, 0, False, 16, False)]
+
+
+@pytest.mark.parametrize("form,dtype,hq,hkv,dim,rot,inter,page,head_major", APPENDS)
+def test_append(B, form, dtype, hq, hkv, dim, rot, inter, page, head_major):  # noqa: F811
+    import torch
+    gen = generator(dim + page)
+    new, before = [1, 0, 5, 70, 1, 33], [0, 9, 100, 3, 47, 64]
+    lens = [a + b for a, b in zip(new, before)]
+    c = Cache(B, gen, form, dtype, hq, hkv, dim, lens, page, head_major)
+    n = sum(new)
+    rows = rand(gen, dtype, n + 3, hq + 2 * hkv, dim)                   # slices of wider rows, three rows behind the last sequence
+    q, k, v = rows[:, :hq], rows[:, hq:hq + hkv], rows[:, hq + hkv:]
+    q_out = torch.full((n + 3, hq, dim), 7.0, device=DEV, dtype=torch_type(dtype))
+    f = B.flame_kv_rotation_frequencies(rot) if rot else np.zeros(0)
+    rotation = B.make_kv_rotation(f, inter) if rot else None
+    keep = [t.clone() for t in (c.k, c.v, c.ks, c.vs)]
+    faults = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kvq_append(c.cfg, c.packed, k, v, ints(offsets(new)), ints(lens), q=q, q_out=q_out, rotation=rotation, faults=faults)
+    torch.cuda.synchronize()
+    assert int(faults[0]) == 0
+    position = np.concatenate([np.arange(a, a + m) for a, m in zip(before, new)])
+    seq = np.repeat(np.arange(len(new)), new)
+    where = c.table_host[seq, position // page], position % page
+    pool_k, pool_v = c.pools()
+    codes, scales, values = kv_oracle.quantise(host(v[:n]), form, dtype)
+    assert np.array_equal(kv_oracle.unpack(c.v.cpu().numpy(), form)[where], codes) and np.array_equal(c.vs.cpu().numpy()[where], scales) and np.array_equal(pool_v[where], values)
+    turned = kv_oracle.rotate(host(k[:n]), position, f, inter)
+    if not rot:
+        codes, scales, _ = kv_oracle.quantise(turned, form, dtype)
+        assert np.array_equal(kv_oracle.unpack(c.k.cpu().numpy(), form)[where], codes) and np.array_equal(c.ks.cpu().numpy()[where], scales)
+    relative, least, limit = HALF[form]
+    pair = np.abs(host(k[:n])).max(-1, keepdims=True) * 2 * 2.0 ** -21 if rot else 0
+    scale = np.repeat((np.abs(turned).reshape(*turned.shape[:-1], -1, 32).max(-1) + pair) * 2 / limit, 32, -1)
+    assert (np.abs(pool_k[where] - turned) <= pair * (1 + relative) + np.maximum(relative * np.abs(turned), least * scale)).all()
+    want_q = kv_oracle.rotate(host(q[:n]), position, f, inter)
+    wide = np.abs(host(q[:n])).max(-1, keepdims=True) * 2
+    assert (np.abs(host(q_out)[:n] - want_q) <= HALF_STEP[dtype] * np.abs(want_q) + (wide * 2.0 ** -21 if rot else 0) + (2.0 ** -25 if dtype == "f16" else 0)).all()
+    assert bool((q_out[n:] == 7.0).all())                               # rows behind the last sequence
+    untouched = np.ones(c.k.shape[:2], bool)
+    untouched[where] = False
+    untouched = torch.tensor(untouched, device=DEV)
+    for was, now in zip(keep, (c.k, c.v, c.ks, c.vs)):
+        assert torch.equal(was[untouched], now[untouched])
+    # in place, and without queries: the same bits
+    first, again = [t.clone() for t in (c.k, c.ks)], q.clone()
+    B.flame_kvq_append(c.cfg, c.packed, k, v, ints(offsets(new)), ints(lens), q=again, q_out=again, rotation=rotation)
+    assert torch.equal(again[:n], q_out[:n]) and torch.equal(again[n:], q[n:])
+    c.k.copy_(keep[0]), c.ks.copy_(keep[2])
+    B.flame_kvq_append(c.cfg, c.packed, k, v, ints(offsets(new)), ints(lens), rotation=rotation)
+    assert torch.equal(c.k, first[0]) and torch.equal(c.ks, first[1])
+    # and back: exactly the values, in rows of both layouts
+    for turn in (False, True):
+        shape = (hkv, n + 3, dim) if turn else (n + 3, hkv, dim)
+        rk, rv = (torch.full(shape, 7.0, device=DEV, dtype=torch_type(dtype)) for _ in range(2))
+        rk, rv = (rk.transpose(0, 1), rv.transpose(0, 1)) if turn else (rk, rv)
+        B.flame_kvq_read(c.cfg, c.packed, ints(offsets(new)), ints(lens), rk, rv, faults=faults)
+        assert np.array_equal(host(rk)[:n], pool_k[where]) and np.array_equal(host(rv)[:n], pool_v[where]) and int(faults[0]) == 0
+        assert bool((rk[n:] == 7.0).all()) and bool((rv[n:] == 7.0).all())
+
+
+def edge_blocks(dtype):
+    """Blocks of 32 whose largest sizes lie on both sides of every border, over the type's range, with each of the other features anywhere below."""
+    import torch
+    rng = np.random.default_rng(5)
+    step = {"bf16": 2.0 ** -7, "f16": 2.0 ** -10, "f32": 2.0 ** -23}[dtype]
+    exps = np.arange(-24, 16) if dtype == "f16" else np.concatenate([np.arange(-149, -100), np.arange(-20, 20), np.arange(110, 128)])
+    blocks = []
+    for e in exps:
+        for f in (1.0, 1.5, 1.75 - step, 1.75, 1.75 + step, 1.8125 - step, 1.8125, 1.8125 + step, 1.875, 2 - step):
+            top = f * 2.0 ** float(e)
+            x = top * rng.choice([1, -1], 32) * np.concatenate([[1], 2.0 ** rng.uniform(-12, 0, 15), np.arange(16) / 16])
+            blocks.append(x)
+    blocks.append(np.zeros(32))
+    blocks.append(np.where(np.arange(32) % 2, -0.0, 0.0))
+    t = torch.tensor(np.array(blocks), dtype=torch.float64).to(torch_type(dtype))
+    odd = t[:6].clone()
+    for i, x in enumerate((math.inf, -math.inf, math.nan, math.inf, 65504.0, -math.nan)):
+        odd[i, 7 * i % 32] = x
+    t = torch.cat([t, odd])
+    return t[torch.isfinite(t).all(1) | (torch.arange(len(t)) >= len(t) - 6)]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("form", FORMS)
+def test_every_border_of_the_codes(B, form, dtype):  # noqa: F811
+    """Largest sizes at the borders of the exponents, halves between codes, the smallest and largest values of the type, signs of zero, infinities and NaN: codes and scales bit for bit, and
+    the values back (a value below the normal range of fp32 may be taken as zero)."""
+    import torch
+    x = edge_blocks(dtype)
+    x = x[:len(x) // 4 * 4].reshape(-1, 1, 128).to(DEV)
+    n = len(x)
+    cfg = B.make_kv_config(dtype, 1, 1, 128)
+    pool = B.make_kvq_pool(cfg, form, 2, n)
+    cache = B.pack_kvq_cache(cfg, form, *pool, ints([[1]]))
+    B.flame_kvq_append(cfg, cache, x, x.flip(2).contiguous(), ints([0, n]), ints([n]))
+    back_k, back_v = torch.empty_like(x), torch.empty_like(x)
+    B.flame_kvq_read(cfg, cache, ints([0, n]), ints([n]), back_k, back_v)
+    for data, codes_t, scales_t, back in ((x, pool[0], pool[2], back_k), (x.flip(2), pool[1], pool[3], back_v)):
+        codes, scales, values = kv_oracle.quantise(host(data), form, dtype)
+        got = kv_oracle.unpack(codes_t[1].cpu().numpy(), form)
+        whole = np.repeat(scales != 255, 32, -1)
+        flushed = (np.abs(host(data)) < 2.0 ** -126) & (got % (128 if form == "f8" else 8) == 0)
+        assert np.array_equal(scales_t[1].cpu().numpy(), scales)
+        assert (got == codes)[whole & ~flushed].all(), np.argwhere((got != codes) & whole & ~flushed)[:5]
+        assert np.array_equal(host(back)[whole & ~flushed], values[whole & ~flushed]) and np.isnan(host(back)[~whole]).all()
+        assert np.isfinite(host(back)[whole]).all()
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_append_and_read_report_what_they_cannot_place(B, form):  # noqa: F811
+    """Bad pages, lengths beyond the table's row and below the new tokens, offsets that decrease: nothing out of range is touched, and the rest is done."""
+    import torch
+    gen = generator(2)
+    cfg = B.make_kv_config("bf16", 2, 1, 32)
+    pool = B.make_kvq_pool(cfg, form, 6, 4)
+    guarded = [p[1:5] for p in pool]                                    # pages on both sides that no entry may reach
+    k = rand(gen, "bf16", 12, 1, 32).abs() + 0.5
+
+    def both(table, off, lens):
+        [p.zero_() for p in pool]
+        faults = torch.zeros(2, dtype=torch.int32, device=DEV)
+        cache = B.pack_kvq_cache(cfg, form, *guarded, ints(table))
+        B.flame_kvq_append(cfg, cache, k, k, ints(off), ints(lens), faults=faults[:1])
+        torch.cuda.synchronize()
+        for p in pool:
+            assert not p[0].any() and not p[5].any()
+        assert torch.equal(pool[0], pool[1]) and torch.equal(pool[2], pool[3])
+        rk, rv = torch.full_like(k, 7.0), torch.full_like(k, 7.0)
+        B.flame_kvq_read(cfg, cache, ints(off), ints(lens), rk, rv, faults=faults[1:])
+        assert int(faults[0]) == int(faults[1]) and torch.equal(rk, rv)
+        return int(faults[0]), [tuple(x) for x in (pool[0][1:5].int().sum((2, 3)) > 0).nonzero().tolist()], [i for i in range(12) if bool((rk[i] != 7.0).any())]
+
+    assert both([[0, 1], [2, 3]], [0, 2, 4], [2, 8]) == (0, [(0, 0), (0, 1), (3, 2), (3, 3)], [0, 1, 2, 3])
+    assert both([[0, 4], [-1, 3]], [0, 2, 6], [6, 6]) == (1, [(3, 0), (3, 1)], [4, 5])
+    assert both([[0, 1], [2, 3]], [0, 3, 5], [2, 9]) == (2, [(0, 0), (0, 1), (3, 3)], [1, 2, 3])
+    both([[0, 1], [2, 3]], [0, 4, 2], [4, 2])                           # offsets that decrease
+    both([[0, 1], [2, 3]], [-3, 4, 5], [4, 2])
+    fault, there, _ = both([[0, 1], [2, 3]], [0, 8, 20], [8, 8])        # twelve rows are there, and eight of the second sequence are not
+    assert fault & 4 and all(p in (0, 1, 2, 3) for p, _ in there)
+
+
+# ---------------------------------------------------------------------------------------------- attention over quantised caches
+HEADS = [("bf16", 8, 2, 64), ("bf16", 4, 4, 128), ("f16", 6, 2, 128), ("f16", 3, 3, 32), ("bf16", 8, 1, 32), ("f16", 4, 4, 64), ("f32", 4, 2, 64), ("f32", 2, 2, 128), ("f32", 3, 1, 32)]
+
+
+def workspace_for(B, cfg, n_seqs, n_tokens=None):  # noqa: F811
+    import torch
+    return torch.full((B.flame_kv_workspace_bytes(cfg, n_seqs, n_tokens),), 0xff, dtype=torch.uint8, device=DEV)     # it holds nothing between calls: NaN
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype,hq,hkv,dim", HEADS + [("bf16", 32, 1, 64), ("f16", 40, 2, 32), ("f32", 20, 1, 64)])
+@pytest.mark.parametrize("page,head_major", [(16, False), (24, True), (1, False), (300, True)])
+def test_decode(B, form, dtype, hq, hkv, dim, page, head_major):  # noqa: F811
+    import torch
+    gen, lens = generator(page), [1, 0, 31, 32, 33, 700, 64, 129]
+    c = Cache(B, gen, form, dtype, hq, hkv, dim, lens, page, head_major)
+    q = rand(gen, dtype, len(lens), hq, dim)
+    out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kvq_decode(c.cfg, c.packed, q, ints(lens), out, workspace_for(B, c.cfg, len(lens)), faults=faults)
+    assert int(faults[0]) == 0
+    pools = c.pools()
+    for b, n in enumerate(lens):
+        check_attention(host(out[b:b + 1]), host(q[b:b + 1]), *c.rows(b, n, pools=pools), dtype, what=(b, n))
+
+
+EXTENDS = [([1, 3, 0, 2, 5], [1, 40, 7, 300, 90], 0), ([70, 200, 1], [700, 200, 33], 0), ([300], [900], 4096), ([3, 1, 17], [2000, 1500, 40], 8192), ([9, 5], [4, 5], 0), ([130, 60, 2], [1100, 61, 1], 2048),
+           ([33] * 70, [50] * 70, 0)]
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype,hq,hkv,dim", HEADS)
+@pytest.mark.parametrize("new,lens,tokens", EXTENDS, ids=lambda x: str(x)[:24])
+def test_extend(B, form, dtype, hq, hkv, dim, new, lens, tokens):  # noqa: F811
+    """Few rows and many, short caches and long ones, rows that see nothing, a row behind the last sequence."""
+    import torch
+    gen = generator(len(new) + dim)
+    c = Cache(B, gen, form, dtype, hq, hkv, dim, lens, 24, tokens=tokens)
+    n, off = sum(new), offsets(new)
+    q = rand(gen, dtype, n + 2, hq, dim)
+    out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kvq_extend(c.cfg, c.packed, q, ints(off), ints(lens), out, workspace_for(B, c.cfg, len(new), n + 2), faults=faults)
+    assert int(faults[0]) == 0 and bool((out[n:] == 7.0).all())
+    pools = c.pools()
+    for b in ([0, len(new) - 1] if len(new) > 20 else range(len(new))):
+        s = slice(off[b], off[b + 1])
+        if new[b]:
+            check_attention(host(out[s]), host(q[s]), *c.rows(b, lens[b], pools=pools), dtype, what=(b, new[b], lens[b]))
+            assert not out[s][:max(0, new[b] - lens[b])].any()
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+@pytest.mark.parametrize("room", [0, 4096])
+def test_rows_do_not_feel_what_they_do_not_see(B, form, dtype, dim, room):  # noqa: F811
+    """Blocks of NaN at later tokens: earlier rows keep their bits; rows that see them are NaN in the block's 32 features (values) or all over (keys); and pages that the table does
+    not name are no keys."""
+    import torch
+    gen = generator(3)
+    lens, new = [200, 90], [150, 90]
+    c = Cache(B, gen, form, dtype, 4, 2, dim, lens, 16, tokens=room)
+    off, ws = ints(offsets(new)), workspace_for(B, c.cfg, 2, 240)
+    q = rand(gen, dtype, 240, 4, dim)
+    clean, dirty = torch.empty_like(q), torch.empty_like(q)
+    B.flame_kvq_extend(c.cfg, c.packed, q, off, ints(lens), clean, ws)
+    last = q[[149, 239]].contiguous()
+    for at in (50, 77, 130, 199):
+        page, slot, row = c.table_host[0, at // 16], at % 16, max(0, at - 50)
+        for scales, where in ((c.vs, "v"), (c.ks, "k")):
+            was = int(scales[page, slot, 1, dim // 32 - 1])
+            scales[page, slot, 1, dim // 32 - 1] = 255
+            B.flame_kvq_extend(c.cfg, c.packed, q, off, ints(lens), dirty, ws)
+            assert torch.equal(dirty[:row], clean[:row]) and torch.equal(dirty[150:], clean[150:]), (at, where)
+            assert torch.equal(dirty[:, :2], clean[:, :2])
+            if where == "v":
+                assert bool(dirty[row:150, 2:, dim - 32:].isnan().all()) and torch.equal(dirty[..., :dim - 32], clean[..., :dim - 32])
+            else:
+                assert bool(dirty[row:150, 2:].isnan().all())
+            single = torch.empty_like(last)
+            B.flame_kvq_decode(c.cfg, c.packed, last, ints(lens), single, ws)
+            assert bool(single[0, 2:, dim - 32:].isnan().all()) and bool(single[:, :2].isfinite().all()) and bool(single[1].isfinite().all())
+            scales[page, slot, 1, dim // 32 - 1] = was
+    B.flame_kvq_extend(c.cfg, c.packed, q, off, ints(lens), dirty, ws)
+    assert torch.equal(dirty, clean)
+    # a page that is none
+    c.table_host[0, 3] = 1 << 20
+    c.table.copy_(ints(c.table_host))
+    faults = torch.zeros(1, dtype=torch.int32, device=DEV)
+    B.flame_kvq_extend(c.cfg, c.packed, q, off, ints(lens), dirty, ws, faults=faults)
+    seen = np.ones(200, bool)
+    seen[48:64] = False
+    c.table_host[0, 3] = 0
+    check_attention(host(dirty[:150]), host(q[:150]), *c.rows(0, 200), dtype, seen=seen)
+    assert int(faults[0]) == 1 and torch.equal(dirty[150:], clean[150:])
+    B.flame_kvq_decode(c.cfg, c.packed, last, ints([200, 90]), single, ws)
+    check_attention(host(single[:1]), host(last[:1]), *c.rows(0, 200), dtype, seen=seen)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_offsets_and_lengths_that_are_none(B, form):  # noqa: F811
+    import torch
+    gen = generator(8)
+    c = Cache(B, gen, form, "bf16", 4, 2, 64, [60, 40, 20], 16)
+    q = rand(gen, "bf16", 30, 4, 64)
+    for off, lens, fault, good in (([0, 10, 5, 30], [60, 40, 20], 4, 1), ([0, 10, 20, 40], [60, 40, 20], 4, 2), ([-5, 10, 20, 30], [60, 40, 20], 4, 0), ([0, 10, 20, 30], [60, -3, 1 << 30], 2, 1)):
+        for room in (c.table, ints(np.concatenate([c.table_host, np.full((3, 200), -7, np.int32)], 1))):
+            cache = B.pack_kvq_cache(c.cfg, form, c.k, c.v, c.ks, c.vs, room)
+            out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+            B.flame_kvq_extend(c.cfg, cache, q, ints(off), ints(lens), out, workspace_for(B, c.cfg, 3, 30), faults=faults)
+            assert int(faults[0]) & fault
+            for b in range(good):
+                s = slice(off[b], off[b + 1])
+                check_attention(host(out[s]), host(q[s]), *c.rows(b, lens[b]), "bf16", what=(off, b))
+
+
+# ---------------------------------------------------------------------------------------------- shared histories
+def shared_workspace(B, cfg, n_groups, n_seqs, n_tokens=None):  # noqa: F811
+    import torch
+    return torch.full((B.flame_kv_shared_workspace_bytes(cfg, n_groups, n_seqs, n_tokens),), 0xff, dtype=torch.uint8, device=DEV)
+
+
+# groups of (shared tokens, [(tokens in all, new ones, where it leaves the history (None: at its end))])
+SHARED = {
+    "one": [(100, [(101, 1, None)] * 5)],
+    "several": [(70, [(71, 1, None), (90, 1, None)]), (0, [(5, 1, None), (1, 1, None)]), (333, [(400, 1, None)]), (48, [(48 + i, 1, None) for i in range(1, 20)])],
+    "pieces": [(200, [(240, 7, None), (201, 1, None), (260, 60, None)]), (33, [(40, 3, None)]), (64, [(200, 100, None), (64, 1, None)])],
+    "within": [(150, [(40, 10, None), (150, 150, None), (0, 2, None), (10, 20, None), (160, 30, None)]), (20, [(3, 1, None), (90, 2, None)])],
+    "forks": [(300, [(320, 2, None), (310, 5, 100), (120, 4, 0), (250, 1, 299)])],
+    "long": [(2500, [(2500 + 7 * i, 1 + i % 3, None) for i in range(1, 12)]), (1100, [(1101, 1, None)])],
+    "many": [(30 + g, [(31 + g + i, 1, None) for i in range(1 + g % 3)]) for g in range(90)],
+}
+
+
+def shared_case(B, gen, form, dtype, hq, hkv, dim, groups, page=16, tokens=0, seed=0, head_major=False):  # noqa: F811
+    lens, new, prefix, lists, first = [], [], [], [], [0]
+    for p, seqs in groups:
+        lists.append(list(range(len(lens), len(lens) + len(seqs))))
+        for i, (n, m, leaves) in enumerate(seqs):
+            lens.append(n), new.append(m), prefix.append(p if leaves is None else leaves)
+        first.append(len(lens))
+    ps = [p for p, _ in groups]
+    c = Cache(B, gen, form, dtype, hq, hkv, dim, lens, page, head_major, seed, tokens, lists, ps)
+    # a sequence that leaves the history has pages of its own from there on
+    extra = [(b, prefix[b] // page, -(-lens[b] // page)) for g, p in zip(lists, ps) for b in g if prefix[b] < p]
+    taken = set(c.table_host[c.table_host >= 0].ravel().tolist())
+    spare = [x for x in range(c.n_pages) if x not in taken]
+    for b, lo, hi in extra:
+        for i in range(lo, hi):
+            if c.table_host[b, i] < 0:
+                c.table_host[b, i] = spare[(b + i) % len(spare)]        # (pages may be any: they are read alone)
+    c.table.copy_(ints(c.table_host))
+    return c, lens, new, prefix, lists, first
+
+
+def check_shared(B, c, q, out, lens, new, prefix, lists, dtype, single, every=1):  # noqa: F811
+    off, pools = offsets([1] * len(lens) if single else new), c.pools()
+    for g in lists:
+        for b in g[::every]:
+            s = slice(off[b], off[b + 1])
+            if off[b + 1] > off[b]:
+                check_attention(host(out[s]), host(q[s]), *c.rows(b, lens[b], prefix[b], g[0], pools), dtype, what=(b, lens[b], prefix[b]))
+
+
+@pytest.mark.parametrize("form", [None, "f8", "f4"])
+@pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 8, 2, 64), ("bf16", 4, 4, 128), ("f16", 6, 2, 128), ("f16", 3, 3, 32), ("bf16", 32, 1, 32), ("f16", 4, 4, 64), ("f32", 4, 2, 64), ("f32", 2, 2, 128), ("f32", 3, 1, 32)])
+@pytest.mark.parametrize("name", SHARED)
+def test_shared(B, form, dtype, hq, hkv, dim, name):  # noqa: F811
+    import torch
+    gen = generator(dim)
+    c, lens, new, prefix, lists, first = shared_case(B, gen, form, dtype, hq, hkv, dim, SHARED[name], tokens=4096 if name in ("long", "pieces") else 0, head_major=dim == 64)
+    for single in (True, False):
+        n = len(lens) if single else sum(new)
+        q = rand(gen, dtype, n + (0 if single else 2), hq, dim)
+        out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+        ws = shared_workspace(B, c.cfg, len(first) - 1, len(lens), len(q))
+        call(B, c, "shared", q, None if single else ints(offsets(new)), ints(lens), ints(first), ints(prefix), out, ws, faults=faults)
+        assert int(faults[0]) == 0 and bool((out[n:] == 7.0).all())
+        check_shared(B, c, q, out, lens, new, prefix, lists, dtype, single, 7 if name == "many" else 1)
+        again = torch.empty_like(out)
+        call(B, c, "shared", q, None if single else ints(offsets(new)), ints(lens), ints(first), ints(prefix), again, ws.random_(0, 256))
+        assert torch.equal(again[:n], out[:n])                          # the same call, the same bits
+
+
+@pytest.mark.parametrize("form", [None, "f8"])
+def test_shared_rows_do_not_feel_what_they_do_not_see(B, form):  # noqa: F811
+    """NaN at a token of the history: rows before it, sequences that left before it and other groups keep their bits."""
+    import torch
+    gen = generator(11)
+    c, lens, new, prefix, lists, first = shared_case(B, gen, form, "bf16", 4, 2, 64, [(120, [(130, 3, None), (125, 80, None), (140, 2, 60)]), (50, [(60, 2, None)])])
+    q = rand(gen, "bf16", sum(new), 4, 64)
+    clean, dirty = torch.empty_like(q), torch.empty_like(q)
+    ws, off = shared_workspace(B, c.cfg, 2, 4, len(q)), offsets(new)
+    call(B, c, "shared", q, ints(off), ints(lens), ints(first), ints(prefix), clean, ws)
+    for at in (60, 100, 119):
+        page, slot = c.table_host[0, at // 16], at % 16
+        keep = (c.v if form is None else c.vs)[page, slot].clone()
+        (c.v if form is None else c.vs)[page, slot, 1] = math.nan if form is None else 255
+        call(B, c, "shared", q, ints(off), ints(lens), ints(first), ints(prefix), dirty, ws)
+        (c.v if form is None else c.vs)[page, slot] = keep
+        before = at - 45                                                # rows of the second sequence: positions 45..124
+        assert bool(dirty[:3, 2:].isnan().all()) and torch.equal(dirty[:3, :2], clean[:3, :2])
+        assert torch.equal(dirty[3:3 + before], clean[3:3 + before]) and bool(dirty[3 + before:83, 2:].isnan().all())
+        assert torch.equal(dirty[83:], clean[83:])
+
+
+def test_shared_reports_groups_that_are_none(B):  # noqa: F811
+    """Wrong group offsets and shared lengths: faults, no access out of range, and sequences outside of every group see their own tokens alone."""
+    import torch
+    gen = generator(12)
+    c, lens, new, prefix, lists, first = shared_case(B, gen, None, "bf16", 4, 2, 64, [(64, [(70, 1, None), (80, 1, None)]), (32, [(40, 1, None), (33, 1, None)])])
+    q = rand(gen, "bf16", 4, 4, 64)
+    pools = c.pools()
+
+    def run(group_offsets, prefix_lens):
+        out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+        call(B, c, "shared", q, None, ints(lens), ints(group_offsets), ints(prefix_lens), out, shared_workspace(B, c.cfg, 8, 4), faults=faults)
+        return int(faults[0]), out
+
+    def check(out, b, trunk, first_seq, own_from):
+        k, v = c.rows(b, lens[b], trunk, first_seq, pools)
+        seen = np.ones(lens[b], bool)
+        seen[trunk:own_from] = False
+        check_attention(host(out[b:b + 1]), host(q[b:b + 1]), k, v, "bf16", seen=seen, what=(b, trunk))
+
+    fault, out = run([0, 2, 4], prefix)
+    assert fault == 0
+    for b in range(4):
+        check(out, b, prefix[b], 0 if b < 2 else 2, prefix[b])
+    for groups in ([0, 2], [0, 2, 3], [0, 2, 9], [2, 4], [-1, 2, 4], [0, 4, 2], [0]):
+        fault, out = run(groups, prefix)
+        assert fault & 4, groups
+        for b in range(4):
+            if groups[0] == 0 and len(groups) > 1 and groups[1] == 2 and b < 2:
+                check(out, b, 64, 0, 64)
+    fault, out = run([2, 4], prefix)
+    check(out, 0, 0, 0, 64), check(out, 1, 0, 1, 64), check(out, 2, 32, 2, 32)
+    fault, out = run([0, 2, 4], [64, 80, 32, 32])                       # the second says that it shares more than there is
+    assert fault == 2
+    check(out, 1, 64, 0, 80)
+    fault, out = run([0, 2, 4], [64, -5, 32, 1 << 30])                  # (taken as sharing nothing, the second has no pages for its first tokens)
+    assert fault == 3
+
+
+# ---------------------------------------------------------------------------------------------- a run of them together
+@pytest.mark.parametrize("form", FORMS)
+def test_a_history_and_its_candidates(B, form):  # noqa: F811
+    """A user's history appended in pieces and attended over, read back, then candidates behind it: each a sequence of one token that shares the history; the last piece captured into a
+    graph that follows the device arrays, replayed with other work in between."""
+    import torch
+    gen = generator(21)
+    dtype, hq, hkv, dim, page = "bf16", 4, 2, 64, 16
+    cfg = B.make_kv_config(dtype, hq, hkv, dim)
+    pool = B.make_kvq_pool(cfg, form, 40, page)
+    table = np.full((9, 10), -7, np.int32)
+    table[0, :7] = [5, 9, 2, 30, 11, 12, 13]
+    for b in range(1, 9):
+        table[b, 6] = 13 + b                                            # the page that holds its candidate; the history ends within it
+    cache = B.pack_kvq_cache(cfg, form, *pool, ints(table))
+    rotation = B.make_kv_rotation(B.flame_kv_rotation_frequencies(dim))
+    rows = rand(gen, dtype, 100, hq + 2 * hkv, dim)
+    ws = workspace_for(B, cfg, 1, 60)
+    history = 0
+    for m in (60, 1, 39):
+        part = rows[history:history + m]
+        history += m
+        q, out = torch.empty(m, hq, dim, device=DEV, dtype=torch_type(dtype)), torch.empty(m, hq, dim, device=DEV, dtype=torch_type(dtype))
+        B.flame_kvq_append(cfg, cache, part[:, hq:hq + hkv], part[:, hq + hkv:], ints([0, m]), ints([history]), q=part[:, :hq], q_out=q, rotation=rotation)
+        B.flame_kvq_extend(cfg, cache, q, ints([0, m]), ints([history]), out, ws)
+        k, v = (torch.empty(history, hkv, dim, device=DEV, dtype=torch_type(dtype)) for _ in range(2))
+        B.flame_kvq_read(cfg, cache, ints([0, history]), ints([history]), k, v)
+        check_attention(host(out), host(q), host(k), host(v), dtype, what=m)
+    # eight candidates: positions 100, each in its own copy of the history's last page's place
+    new = rand(gen, dtype, 8, hq + 2 * hkv, dim)
+    cand = B.pack_kvq_cache(cfg, form, *pool, ints(table[1:]))
+    lens = ints([101] * 8)
+    q, out = torch.empty(8, hq, dim, device=DEV, dtype=torch_type(dtype)), torch.empty(9, hq, dim, device=DEV, dtype=torch_type(dtype))
+    # the group's first sequence is the history itself, with a query of its own
+    everyone = ints([100] + [101] * 8)
+    group, prefix, wss = ints([0, 9]), ints([100] * 9), shared_workspace(B, cfg, 1, 9)
+    off = ints(np.arange(9))
+
+    def step():
+        B.flame_kvq_append(cfg, cand, new[:, hq:hq + hkv], new[:, hq + hkv:], off, lens, q=new[:, :hq], q_out=q, rotation=rotation)
+        B.flame_kvq_shared(cfg, cache, torch_cat[:9], None, everyone, group, prefix, out, wss)
+
+    torch_cat = torch.zeros(9, hq, dim, device=DEV, dtype=torch_type(dtype))
+
+    def check():
+        values = [kv_oracle.stored_values(kv_oracle.unpack(p.cpu().numpy(), form), s.cpu().numpy(), form) for p, s in ((pool[0], pool[2]), (pool[1], pool[3]))]
+        assert np.array_equal(values[0][table[0, np.arange(100) // page], np.arange(100) % page], host(k))
+        for b in range(9):
+            kk, vv = host(k), host(v)
+            if b:
+                kk, vv = (np.concatenate([x, y[table[b, 6], 4][None]]) for x, y in ((kk, values[0]), (vv, values[1])))
+            check_attention(host(out[b:b + 1]), host(torch_cat[b:b + 1]), kk, vv, dtype, what=b)
+
+    torch_cat.copy_(rand(gen, dtype, 9, hq, dim))
+    step()
+    check()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=side):
+        step()
+    for i in range(4):
+        torch_cat.copy_(rand(gen, dtype, 9, hq, dim))
+        new.copy_(rand(gen, dtype, 8, hq + 2 * hkv, dim))
+        wss.fill_(255)
+        out.fill_(3.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check()
+        eager = out.clone()
+        step()
+        assert torch.equal(eager, out)
+
+
+@pytest.mark.parametrize("form", [None, "f8"])
+def test_two_calls_at_once(B, form):  # noqa: F811
+    """Two streams, a workspace each, over one cache: the bits of one call after the other."""
+    import torch
+    gen = generator(31)
+    c, lens, new, prefix, lists, first = shared_case(B, gen, form, "bf16", 8, 2, 64, SHARED["long"], tokens=4096)
+    qs = [rand(gen, "bf16", sum(new), 8, 64) for _ in range(2)]
+    want = [torch.empty_like(qs[0]) for _ in range(2)]
+    args = ints(offsets(new)), ints(lens), ints(first), ints(prefix)
+    spaces = [shared_workspace(B, c.cfg, len(first) - 1, len(lens), sum(new)) for _ in range(2)]
+    for q, o, ws in zip(qs, want, spaces):
+        call(B, c, "shared", q, *args, o, ws)
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    for _ in range(5):
+        got = [torch.zeros_like(qs[0]) for _ in range(2)]
+        torch.cuda.synchronize()
+        for q, o, ws, s in zip(qs, got, spaces, streams):
+            call(B, c, "shared", q, *args, o, ws, stream=s)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
