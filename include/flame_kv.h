@@ -140,7 +140,8 @@ typedef struct {
  *   faults       FLAME_KV_FAULT_LENGTH also for a prefix_lens below 0, beyond the table's row, or beyond that of the group's first sequence (tokens from there on are not seen);
  *                FLAME_KV_FAULT_OFFSET also for group_offsets that decrease, are below 0, or do not go from 0 to n_seqs: a sequence that is in no group, or of up to 64 groups in one
  *                behind offsets that are none, sees its own tokens alone.  (Of more groups, which rows see what is not defined.)
- *   workspace    of flame_kv_shared_workspace_bytes bytes for these numbers or larger ones; as in flame_kv_extend */
+ *   workspace    of flame_kv_shared_workspace_bytes bytes for these numbers or larger ones; as in flame_kv_extend
+ * n_tokens is below 2^24. */
 int flame_kv_shared(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *q_offsets, const int32_t *kv_lens, const flame_kv_groups *groups,
                     int32_t n_seqs, int64_t n_tokens, const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream);
 

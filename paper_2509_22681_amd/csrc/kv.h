@@ -60,6 +60,13 @@ struct KvRoute {
 };
 KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool paged, bool decode, int64_t capacity);
 
+// The same for groups that share histories, and where the split part's workspace begins.
+struct KvSharedRoute {
+  int32_t wavefronts, splits;
+  int64_t split_at, workspace;
+};
+KvSharedRoute kv_shared_route(const flame_kv_config &c, int32_t n_groups, int64_t n_rows, int64_t capacity);
+
 hipError_t launch_kv_append(const KvBatch &batch, const KvPages &pages, const KvRows &k, const KvRows &v, const KvRows *q, const KvRows *q_out,
                             const KvRotation &rotation, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, hipStream_t stream);
 // quantised caches: as above, and rows back out of one
@@ -67,10 +74,16 @@ hipError_t launch_kvq_append(const KvBatch &batch, const KvPages &pages, const K
                              const KvRotation &rotation, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, hipStream_t stream);
 hipError_t launch_kvq_read(const KvBatch &batch, const KvPages &pages, const KvScales &scales, const KvRows &k, const KvRows &v, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
                            hipStream_t stream);
-hipError_t launch_kvq_attention(const KvAttention &a, hipStream_t stream);
+hipError_t launch_kvq_attention_f8(const KvAttention &a, int wavefronts, hipStream_t stream);
+hipError_t launch_kvq_attention_f4(const KvAttention &a, int wavefronts, hipStream_t stream);
+// shared histories (kv_shared.h)
+hipError_t launch_kv_shared_plain(const KvAttention &a, int wavefronts, void *split_workspace, hipStream_t stream);
+hipError_t launch_kv_shared_f8(const KvAttention &a, int wavefronts, void *split_workspace, hipStream_t stream);
+hipError_t launch_kv_shared_f4(const KvAttention &a, int wavefronts, void *split_workspace, hipStream_t stream);
 hipError_t launch_kv_attention(const KvAttention &a, int wavefronts, hipStream_t stream);
 // few query rows: split over the keys (kv_split.hip)
 hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream);
+hipError_t launch_kvq_split(const KvAttention &a, void *workspace, hipStream_t stream);
 int64_t kv_split_workspace_bytes(int32_t head_dim, int64_t rows);   // rows times heads
 
 }  // namespace flame

@@ -22,7 +22,8 @@ int done(hipError_t e) {
 
 // A grid dimension may have 2^32 - 1 threads.  Attention on row tiles has two of them per row and head, and 256 per sequence and head; the join of split attention has up to 2^22,
 // and 256 per 64 rows and heads where those are more than 2^20.
-constexpr int64_t kMaxRowHeads = (int64_t)1 << 25, kMaxSequenceHeads = ((int64_t)1 << 23) - 1;
+// The join of shared histories has 256 for a row and up to 8, 16 or 32 heads.
+constexpr int64_t kMaxRowHeads = (int64_t)1 << 25, kMaxSequenceHeads = ((int64_t)1 << 23) - 1, kMaxSharedRows = (int64_t)1 << 24;
 constexpr int64_t kSmallCache = 1024;                          // tokens that a sequence has room for, up to which its keys are not split over the chip
 constexpr int64_t kMaxKeys = ((int64_t)1 << 31) - 65536;     // of a sequence: room for a tile's end behind them in 32 bits
 // Limits of kv_route, for the workspace of every call up to a size: rows times heads of an extend that is split, parts of a row tile's keys, and workgroups of a launch whose keys are cut.
@@ -166,12 +167,25 @@ int attend_quantised(const flame_kv_config *cfg, const flame_kvq_cache *cache, c
   a.form = scales.form;
   a.k_scales = scales.k;
   a.v_scales = scales.v;
-  return done(launch_kvq_attention(a, (hipStream_t)stream));
+  const KvRoute route = kv_route(*cfg, n_seqs, n_rows, true, offsets == nullptr, a.pages.capacity);
+  if (route.split) return done(launch_kvq_split(a, workspace, (hipStream_t)stream));
+  a.splits = route.splits;
+  a.parts = (float *)workspace;
+  return done((a.form == FLAME_KVQ_F8 ? launch_kvq_attention_f8 : launch_kvq_attention_f4)(a, route.wavefronts, (hipStream_t)stream));
+}
+
+// What any flame_kv_shared of up to this many groups, sequences and rows may need: kv_shared_route's parts times rows and heads stay below the bound of workspace_bound (whose sequences
+// are the groups here), and there is a plane for the sequences' own keys and the split kernel's workspace.
+int64_t shared_workspace_bound(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows) {
+  if (n_seqs == 0 || n_rows == 0) return 0;
+  const int64_t heads = n_rows * c.n_q_heads;
+  return (heads + std::max(heads, std::min(kMostParts * heads, (int64_t)1024 * 129))) * (c.head_dim + 2) * 4 + 16 + kv_split_workspace_bytes(c.head_dim, heads);
 }
 
 int check_groups(const flame_kv_config *c, int32_t n_groups, int32_t n_seqs, int64_t n_rows) {
   if (int rc = check_batch(c, n_seqs, n_rows)) return rc;
   if (n_groups < 0 || (int64_t)n_groups * c->n_q_heads > kMaxSequenceHeads) return bad("groups times heads must be in [0, 2^23)");
+  if (n_rows >= kMaxSharedRows) return bad("rows of a call with shared histories must be below 2^24");
   return FLAME_GR_OK;
 }
 
@@ -190,7 +204,8 @@ int attend_shared(const flame_kv_config *cfg, const flame_kv_cache *cache, const
   if (int rc = take_rows(cfg, out, &a.out)) return rc;
   if (int rc = plain ? take_pages(cfg, cache, &a.pages) : take_pages(cfg, quantised, &a.pages, &scales)) return rc;
   if (!kv_lens || !groups->prefix_lens || !groups->group_offsets) return bad("kv_lens, group_offsets or prefix_lens is NULL");
-  const int64_t need = 0;
+  const KvSharedRoute route = kv_shared_route(*cfg, groups->n_groups, n_rows, a.pages.capacity);
+  const int64_t need = kv_shared_route(*cfg, groups->n_groups, n_rows, kMaxKeys).workspace;
   if (need > 0 && (!workspace || !aligned(workspace))) return bad("the workspace is NULL or not 16-byte aligned");
   if (workspace_bytes < need) return bad("the workspace is smaller than this call needs (flame_kv_shared_workspace_bytes)", FLAME_GR_CAPACITY_EXCEEDED);
   a.batch = KvBatch{offsets, kv_lens, n_seqs, n_rows, faults};
@@ -201,7 +216,10 @@ int attend_shared(const flame_kv_config *cfg, const flame_kv_cache *cache, const
   a.group_offsets = groups->group_offsets;
   a.prefix_lens = groups->prefix_lens;
   a.n_groups = groups->n_groups;
-  return done(launch_kvq_attention(a, (hipStream_t)stream));
+  a.splits = route.splits;
+  a.parts = (float *)workspace;
+  const auto launch = plain ? launch_kv_shared_plain : a.form == FLAME_KVQ_F8 ? launch_kv_shared_f8 : launch_kv_shared_f4;
+  return done(launch(a, route.wavefronts, (char *)workspace + route.split_at, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -253,6 +271,21 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
     const int64_t parts = std::min({(likely > 256 ? 1024 : 512) / std::max(likely, (int64_t)1), std::min(capacity / 256, std::max((int64_t)32, capacity / 512)), kMostParts});
     if (parts > 1) r = KvRoute{false, kp, (int32_t)parts, parts * heads * (c.head_dim + 2) * 4};
   }
+  return r;
+}
+
+// The histories' rows are those of whole groups.
+KvSharedRoute kv_shared_route(const flame_kv_config &c, int32_t n_groups, int64_t n_rows, int64_t capacity) {
+  const bool wide = c.dtype == FLAME_KV_F32 && c.head_dim == 128;
+  const int64_t group = c.n_q_heads / c.n_kv_heads, heads = n_rows * c.n_q_heads, rows = n_rows * group / std::max(n_groups, 1);
+  const int32_t kp = rows <= 32 && !wide ? 4 : rows <= 64 ? 2 : 1;
+  KvSharedRoute r{kp, 1, 0, 0};
+  if ((n_rows * group / 128 + n_groups) * c.n_kv_heads <= kPartWorkgroups && capacity >= kSmallCache) {
+    const int64_t likely = std::max(n_groups * ((rows * kp + 127) / 128) * c.n_kv_heads, (int64_t)1);
+    r.splits = (int32_t)std::max((int64_t)1, std::min({(likely > 256 ? 1024 : 512) / likely, std::min(capacity / 256, std::max((int64_t)32, capacity / 512)), kMostParts}));
+  }
+  r.split_at = ((r.splits + 1) * heads * (c.head_dim + 2) * 4 + 15) / 16 * 16;
+  r.workspace = r.split_at + kv_split_workspace_bytes(c.head_dim, heads);
   return r;
 }
 
@@ -349,7 +382,7 @@ int flame_kv_shared_workspace_bytes(const flame_kv_config *cfg, int32_t n_groups
   if (int rc = check_config(cfg)) return rc;
   if (int rc = check_groups(cfg, n_groups, n_seqs, n_tokens)) return rc;
   if (!bytes) return bad("bytes is NULL");
-  *bytes = 0;
+  *bytes = shared_workspace_bound(*cfg, n_seqs, n_tokens);
   return FLAME_GR_OK;
 }
 

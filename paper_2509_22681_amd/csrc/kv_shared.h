@@ -1,0 +1,112 @@
+// Attention of groups of sequences over histories that they share, and over their own tokens behind them (flame_kv_shared, flame_kvq_shared).
+//
+// A row's softmax is cut at the end of what its sequence shares.  Row tiles (kv_flash.h) take the rows of a whole group over the history, cut into parts along the keys where tiles are few, so that a history
+// is read once for 128 rows (tokens times heads of a key head) and not once for each sequence; split attention (kv_split.h) takes each sequence's rows over its own tokens; both leave maxima,
+// sums and unnormalised rows, which the kernel here joins, planes in their order: the same call gives the same bits.
+#pragma once
+#include "kv_flash.h"
+#include "kv_split.h"
+
+namespace flame {
+
+namespace {
+
+// Bound by latency and by the planes, which it reads once.  DH / 4 lanes a head, and a workgroup 256 / (DH / 4) heads of a row.
+template <typename T, int DH, int KP>
+__global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, const float *__restrict__ split_parts) {
+  constexpr int KW = KP * key_block<T, DH, KP>();
+  constexpr int H = 256 / (DH / 4);
+  const int lane = threadIdx.x & 63;
+  if (blockIdx.x == 0 && a.batch.faults) {
+    if (threadIdx.x == 0 && (a.group_offsets[0] != 0 || a.group_offsets[a.n_groups] != a.batch.n_seqs)) kv_fault(a.batch.faults, FLAME_KV_FAULT_OFFSET);
+    for (int g = threadIdx.x; g < a.n_groups; g += 256) kv_report_offsets(a.group_offsets[g], a.group_offsets[g + 1], a.batch.n_seqs, a.batch.faults);
+    for (int b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
+      int lo = 0, hi = a.n_groups;                                // the first group that ends behind the sequence
+      while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (a.group_offsets[mid + 1] > b) hi = mid;
+        else lo = mid + 1;
+      }
+      const int b0 = lo < a.n_groups ? a.group_offsets[lo] : b;
+      if (b0 >= 0 && b0 < b && kv_clip(a.prefix_lens[b], a.pages.capacity) > kv_clip(a.prefix_lens[b0], a.pages.capacity)) kv_fault(a.batch.faults, FLAME_KV_FAULT_LENGTH);
+    }
+  }
+  const int blocks = (a.n_q_heads + H - 1) / H;
+  const int64_t q_row = blockIdx.x / blocks;
+  const int head = blockIdx.x % blocks * H + threadIdx.x / (DH / 4), f = threadIdx.x % (DH / 4) * 4;
+  int seq = (int)q_row;
+  int64_t first = q_row;
+  if (a.batch.offsets) {
+    seq = kv_find_sequence(a.batch.offsets, a.batch.n_seqs, q_row, lane);
+    if (seq >= a.batch.n_seqs) return;
+    first = a.batch.offsets[seq];
+    if (first < 0 || q_row < first || q_row >= a.batch.offsets[seq + 1]) return;
+  }
+  // parts of the history
+  int parts = 0;
+  const int g = kv_find_sequence(a.group_offsets, a.n_groups, seq, lane);
+  if (g < a.n_groups) {
+    const int b0 = a.group_offsets[g];
+    if (b0 >= 0 && b0 <= seq) {
+      const int history = kv_clip(a.prefix_lens[b0], a.pages.capacity);
+      if (history > 0) parts = flash_parts<KW>(history, a.splits).parts;
+    }
+  }
+  if (head >= a.n_q_heads) return;
+  const int64_t step = a.batch.n_rows * a.n_q_heads, from = q_row * a.n_q_heads + head;
+  const float2 *state = kv_part_state(a, a.splits + 1) + from;
+  const float *sums = a.parts + from * DH + f;
+  float m = -INFINITY, l = 0.f;
+  f32x4 o = {0.f, 0.f, 0.f, 0.f};
+  const auto add = [&](float mw, float lw, f32x4 ow) {
+    const float m_new = fmaxf(m, mw), m_at = m_new == -INFINITY ? 0.f : m_new;
+    const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_at), take = mw == m_new ? 1.f : __builtin_amdgcn_exp2f(mw - m_at);
+    l = l * keep + lw * take;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[i] = o[i] * keep + ow[i] * take;
+    m = m_new;
+  };
+#pragma unroll 4
+  for (int p = 0; p < parts; ++p) {
+    const float2 ml = state[p * step];
+    add(ml.x, ml.y, *(const f32x4 *)(sums + p * step * DH));
+  }
+  // the sequence's own keys: one plane, or parts of wavefronts
+  const int2 of = ((const int2 *)(split_parts + split_parts_floats(DH)))[from];
+  if (of.x >= 0 && of.x >> 1 < of.y && of.y < split_workers(DH)) {
+    const int group = a.n_q_heads / a.n_kv_heads, r = (int)(((q_row - first) * group + head % group) % kRows);
+    for (int w = of.x >> 1; w <= of.y; ++w) {
+      const float *part = split_parts + ((int64_t)w * 2 + (w == of.x >> 1 ? of.x & 1 : 0)) * split_part_floats(DH);
+      add(part[r], part[kRows + r], *(const f32x4 *)(part + 2 * kRows + r * DH + f));
+    }
+  } else {
+    const float2 ml = state[a.splits * step];
+    add(ml.x, ml.y, *(const f32x4 *)(sums + a.splits * step * DH));
+  }
+  const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
+  typedef T out4 __attribute__((ext_vector_type(4)));
+  out4 y;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = kv_round<T>(o[i] * inv);
+  *(out4 *)(a.out.p + q_row * a.out.row + head * a.out.head + f * sizeof(T)) = y;
+}
+
+template <int FORM> hipError_t launch_shared(const KvAttention &a, int wavefronts, void *split_workspace, hipStream_t stream) {
+  hipError_t e = hipErrorInvalidValue;
+  flash_with_shape(a, wavefronts, [&](auto t, auto width, auto kp) {
+    using T = decltype(t);
+    constexpr int DH = decltype(width)::value, KP = decltype(kp)::value;
+    if (a.n_groups > 0) {
+      e = launch_flash<T, DH, true, KP, FORM, true>(a, stream);
+      if (e != hipSuccess) return;
+    }
+    kv_split_kernel<T, DH, FORM, true><<<split_workers(DH) / 4, 256, 0, stream>>>(a, (float *)split_workspace);
+    kv_shared_join_kernel<T, DH, KP><<<(unsigned)(a.batch.n_rows * ((a.n_q_heads * (DH / 4) + 255) / 256)), 256, 0, stream>>>(a, (const float *)split_workspace);
+    e = hipGetLastError();
+  });
+  return e;
+}
+
+}  // namespace
+
+}  // namespace flame

@@ -65,7 +65,7 @@ REFUSED = [(ALL, dict(cfg=None), INVALID), (ALL, dict(dtype=3), INVALID), (ALL, 
            (("append", "read", "extend", "shared", "shared_q"), dict(n_tokens=-1), INVALID), (("append", "read", "extend", "shared", "shared_q"), dict(n_tokens=1 << 23), INVALID),
            (("append", "read", "extend", "shared", "shared_q"), dict(n_tokens=1 << 61), INVALID), (("append", "read", "extend"), dict(offsets=None), INVALID),
            (SHARED, dict(offsets=None), INVALID),                       # ten rows of three sequences
-           (SHARED, dict(group=0), INVALID), (SHARED, dict(n_groups=-1), INVALID), (SHARED, dict(n_groups=1 << 21), INVALID), (SHARED, dict(groups=None), INVALID), (SHARED, dict(prefix=None), INVALID),
+           (SHARED, dict(hq=1, hkv=1, n_tokens=1 << 24), INVALID), (SHARED, dict(group=0), INVALID), (SHARED, dict(n_groups=-1), INVALID), (SHARED, dict(n_groups=1 << 21), INVALID), (SHARED, dict(groups=None), INVALID), (SHARED, dict(prefix=None), INVALID),
            (("append",), dict(rot_dim=8), INVALID), (("append",), dict(rot_dim=80), INVALID), (("append",), dict(frequencies=None), INVALID), (("append",), dict(q=False), INVALID)]
 
 
