@@ -11,6 +11,9 @@ template <typename T, int FORM> constexpr int kv_row_bytes(int features) { retur
 template <int FORM> constexpr int kv_scale_shift() { return FORM == kF8 ? 5 : 4; }
 __device__ __forceinline__ float kv_scale(uint32_t byte) { return __uint_as_float(byte << 23); }   // (2^-127 and NaN, bytes 0 and 255, are what the conversions take them for)
 
+// The scale of block `i` of up to four, from a word of their bytes.
+__device__ __forceinline__ float kv_scale_of(uint32_t bytes, int i) { return kv_scale(bytes >> (8 * i) & 0xff); }
+
 // Form as a template argument of the launches.
 template <typename F> inline void kv_with_form(int32_t form, F f) {
   if (form == kPlain) f(std::integral_constant<int, kPlain>{});

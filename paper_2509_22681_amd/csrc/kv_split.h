@@ -33,6 +33,8 @@ namespace {
 // memory speed all the same.
 constexpr int split_occupancy(int dh) { return dh == 128 ? 2 : dh == 64 ? 3 : 4; }
 constexpr int split_workers(int dh) { return 1024 * split_occupancy(dh); }
+// Tiles of codes that a wavefront has requested ahead of the one at work.
+constexpr int split_ahead(int dh, int form) { return 1; }
 constexpr int kRows = 16;           // query rows of a unit
 
 template <typename T, int DH, int FORM> struct SplitShape {
@@ -127,7 +129,7 @@ struct SplitPlace {
   SplitSeq mine;      // the lane's sequence, of up to 64
 };
 
-template <int KT, bool SHARED, typename F> __device__ __forceinline__ SplitPlace split_find(const KvAttention &a, int lane, F target) {
+template <int KT, bool SHARED, typename F> __device__ __forceinline__ SplitPlace split_find(const KvAttention &a, int lane, int heads, F target) {
   SplitPlace p{0, 0, a.batch.n_seqs, SplitSeq{}};
   int lo = 0, n = a.batch.n_seqs;
   int64_t base = 0, at = 0;
@@ -160,7 +162,7 @@ template <int KT, bool SHARED, typename F> __device__ __forceinline__ SplitPlace
         if (lane == i) mine = all;
       }
     }
-    mine *= a.n_kv_heads;
+    mine *= heads;
     const int64_t sums = split_scan(mine);
     if (top) {
       p.total = split_lane(sums, 63);
@@ -229,15 +231,21 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
   constexpr int VW = VB / 4;
   typedef uint32_t word4 __attribute__((ext_vector_type(4)));
   __shared__ int64_t offset_s[4][2][KT];
+  __shared__ __attribute__((aligned(16))) uint32_t scale_s[4][FORM == kPlain ? 1 : 64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int l16 = lane & 15, g = lane >> 4;
-  const int worker = blockIdx.x * 4 + wave;
+  // Codes of a token's heads lie side by side where its page is laid out token by token, several heads to a line of the caches, and so do scales.  So of codes, up to four wavefronts of a workgroup take the
+  // same tiles of neighbouring heads: `together` of them share a stretch of the line, which is shorter by as much.  Storage for parts goes by head first, so that a head's parts are neighbours.
+  const int together = FORM == kPlain ? 1 : a.n_kv_heads % 4 == 0 ? 4 : a.n_kv_heads % 2 == 0 ? 2 : 1;
+  const int stretches = split_workers(DH) / together, stretch = FORM == kPlain ? blockIdx.x * 4 + wave : blockIdx.x * (4 / together) + wave / together;
+  const int my_head = FORM == kPlain ? 0 : wave % together, worker = FORM == kPlain ? stretch : my_head * stretches + stretch;
+  const int heads = FORM == kPlain ? a.n_kv_heads : a.n_kv_heads / together;
   int64_t per = 0;
-  SplitPlace place = split_find<KT, SHARED>(a, lane, [&](int64_t total) {
-    per = (total + split_workers(DH) - 1) / split_workers(DH);
-    return (int64_t)worker * per;
+  SplitPlace place = split_find<KT, SHARED>(a, lane, heads, [&](int64_t total) {
+    per = (total + stretches - 1) / stretches;
+    return (int64_t)stretch * per;
   });
-  int64_t tile = (int64_t)worker * per;                           // on the line of all tiles
+  int64_t tile = (int64_t)stretch * per;                          // on the line of all tiles
   const int64_t tile_end = min(tile + per, place.total);
   const float scale = a.scale * kLog2e;
   const int group = a.n_q_heads / a.n_kv_heads;
@@ -247,7 +255,7 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
   while (tile < tile_end && seq < a.batch.n_seqs) {
     const SplitSeq s = a.batch.n_seqs <= 64 ? split_from_lane<SHARED>(place.mine, seq) : split_sequence<KT, SHARED>(a, seq, false);
     int64_t in_seq = tile - seq_tile;
-    const int64_t seq_tiles = (int64_t)a.n_kv_heads * s.blocks * s.tiles;
+    const int64_t seq_tiles = (int64_t)heads * s.blocks * s.tiles;
     if (in_seq >= seq_tiles) {                                    // (sequences without rows have none)
       seq_tile += seq_tiles;
       ++seq;
@@ -255,7 +263,7 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
     }
     const int unit = (int)(in_seq / s.tiles), t0 = (int)(in_seq - (int64_t)unit * s.tiles);
     const int t1 = (int)min((int64_t)s.tiles, t0 + (tile_end - tile));
-    const int kvh = unit / s.blocks, block = unit - kvh * s.blocks;
+    const int head_group = unit / s.blocks, block = unit - head_group * s.blocks, kvh = FORM == kPlain ? head_group : head_group * together + my_head;
     const int32_t *table = a.pages.table + seq * a.pages.table_stride;
     const char *kp = a.pages.k + kvh * a.pages.head, *vp = a.pages.v + kvh * a.pages.head;
     // my query row (the column of the accumulators), and the keys it sees
@@ -279,6 +287,8 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
     for (int j = 0; j < VF; ++j) o[j] = f32x4{0.f, 0.f, 0.f, 0.f};
     float m = -INFINITY, l = 0.f;
 
+    const char *scales_of_lane = (lane < 32 ? a.v_scales : a.k_scales) + (FORM == kPlain ? 0 : kvh * a.pages.head >> kv_scale_shift<FORM>());
+
     // Row offsets of a tile: key k by lane k; keys behind the last one repeat it, keys in pages that the table does not name get the pool's first row, and neither counts.
     auto look_up = [&](int t) -> int64_t {
       const int key = min(t * KT + (lane & (KT - 1)), s.n - 1);
@@ -291,7 +301,7 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
     struct Codes {
       SplitWords<S::PB> kc[KB][S::NP];
       SplitWords<kv_row_bytes<T, FORM>(VF)> vc[VK];
-      uint32_t ks[KB][S::NP], vs[VK];
+      uint32_t scales;                                            // of key lane % KT: of its value in the lower half of the wavefront, else of the key itself
     };
     struct Tile : std::conditional_t<FORM == kPlain, Values, Codes> {
       uint64_t there;                                             // lanes' keys that count
@@ -303,22 +313,18 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
       if (lane < KT) at[lane] = max(offset, (int64_t)0);
       __builtin_amdgcn_wave_barrier();
       if constexpr (FORM != kPlain) {
-        constexpr int shift = kv_scale_shift<FORM>(), VBC = kv_row_bytes<T, FORM>(VF);
+        const char *k_at = kp + g * S::PB, *v_at = vp + l16 * kv_row_bytes<T, FORM>(VF);
 #pragma unroll
         for (int b = 0; b < KB; ++b) {
-          const int64_t row_at = kvh * a.pages.head + at[F32 ? l16 : 8 * (l16 >> 2) + 4 * b + (l16 & 3)];
+          const char *row_at = k_at + at[F32 ? l16 : 8 * (l16 >> 2) + 4 * b + (l16 & 3)];
 #pragma unroll
-          for (int p = 0; p < S::NP; ++p) {
-            x.kc[b][p].load(a.pages.k + row_at + (p * 4 + g) * S::PB);
-            x.ks[b][p] = *(const uint8_t *)(a.k_scales + (row_at >> shift) + (((p * 4 + g) * S::PB) >> shift));
-          }
+          for (int p = 0; p < S::NP; ++p) x.kc[b][p].load(row_at + p * 4 * S::PB);
         }
 #pragma unroll
-        for (int i = 0; i < VK; ++i) {
-          const int64_t row_at = kvh * a.pages.head + at[VK * g + i];
-          x.vc[i].load(a.pages.v + row_at + l16 * VBC);
-          x.vs[i] = *(const uint8_t *)(a.v_scales + (row_at >> shift) + ((l16 * VBC) >> shift));
-        }
+        for (int i = 0; i < VK; ++i) x.vc[i].load(v_at + at[VK * g + i]);
+        SplitWords<DH / 32> w;
+        w.load(scales_of_lane + (max(offset, (int64_t)0) >> kv_scale_shift<FORM>()));
+        x.scales = w.w[0];
       } else {
 #pragma unroll
       for (int b = 0; b < KB; ++b) {
@@ -348,13 +354,16 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
       if constexpr (FORM != kPlain) {
         typedef typename KvPair<T>::vec pair;
         constexpr int W8 = FORM == kF8 ? 2 : 1, KE = F32 ? 2 : 1;       // words of eight features' codes, steps that they make
+        scale_s[wave][lane] = loaded.scales;
+        __builtin_amdgcn_wave_barrier();
 #pragma unroll
         for (int b = 0; b < KB; ++b)
 #pragma unroll
           for (int e = 0; e < DH / 32; ++e) {
             const int p = e / (S::PF / 8), sub = e % (S::PF / 8);
             pair y[4];
-            kv_eight<T, FORM>(loaded.kc[b][p].w + sub * W8, kv_scale(loaded.ks[b][p]), y);
+            const uint32_t scales = scale_s[wave][32 + (F32 ? l16 : 8 * (l16 >> 2) + 4 * b + (l16 & 3))];
+            kv_eight<T, FORM>(loaded.kc[b][p].w + sub * W8, kv_scale_of(scales, (p * 4 + g) * S::PF / 32), y);
             if constexpr (F32) {
               made.k[b][KE * e] = word4{__float_as_uint(y[0][0]), __float_as_uint(y[0][1]), __float_as_uint(y[1][0]), __float_as_uint(y[1][1])};
               made.k[b][KE * e + 1] = word4{__float_as_uint(y[2][0]), __float_as_uint(y[2][1]), __float_as_uint(y[3][0]), __float_as_uint(y[3][1])};
@@ -398,7 +407,8 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
       for (int i = 1; i < VK; ++i) top = fmaxf(top, w[i]);
       const float m_new = fmaxf(m, split_max(top) - kv_lowered<T>(0));   // the reference of the exponents
       const float m_at = m_new == -INFINITY ? 0.f : m_new;       // (nothing seen yet: all weights are 2^-inf)
-      if (__builtin_amdgcn_ballot_w64(m_new != m)) {
+      // (codes: without the branch, around which the compiler copies all sums: 32 products in place of 50 moves a tile of 128 features)
+      if (FORM != kPlain || __builtin_amdgcn_ballot_w64(m_new != m)) {
         const float keep = m == m_new ? 1.f : __builtin_amdgcn_exp2f(m - m_at);
         l *= keep;
 #pragma unroll
@@ -413,10 +423,50 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
         l += w[i];
       }
       if constexpr (FORM != kPlain) {
+        float vs[VK];
 #pragma unroll
-        for (int i = 0; i < VK; ++i) split_values<T, FORM, VF>(loaded.vc[i].w, kv_scale(loaded.vs[i]), x.v[i]);
-      }
-      if (masked) {
+        for (int i = 0; i < VK; ++i) vs[i] = kv_scale_of(scale_s[wave][VK * g + i], l16 * VF / 32);
+        if (masked) {
+          // Codes of keys that do not count are zeros, and a block that is NaN, which a row that does not see it must not meet in a product, is taken out and added to the rows that do see it.  (A lane's
+          // features are of one block.)
+          constexpr float kNone = INFINITY;                             // (the bits of scale byte 255)
+          const auto take_out = [&](int i) {
+            vs[i] = 0.f;
+#pragma unroll
+            for (int n = 0; n < loaded.vc[i].N; ++n) loaded.vc[i].w[n] = 0;
+          };
+          bool odd = false;
+#pragma unroll
+          for (int i = 0; i < VK; ++i) {
+            if (!(here >> i & 1)) take_out(i);
+            odd |= vs[i] == kNone;
+          }
+          if (__builtin_amdgcn_ballot_w64(odd)) {
+            f32x4 nans = {0.f, 0.f, 0.f, 0.f};
+            if constexpr (F32) {
+#pragma unroll
+              for (int i = 0; i < VK; ++i) nans = __builtin_amdgcn_mfma_f32_16x16x4f32(vs[i] == kNone ? 1.f : 0.f, (float)(seen >> i & 1), nans, 0, 0, 0);
+            } else {
+              typename Matrix16<T>::frag of, ones;
+#pragma unroll
+              for (int i = 0; i < VK; ++i) {
+                of[i] = (T)(vs[i] == kNone ? 1.f : 0.f);
+                ones[i] = (T)(float)(seen >> i & 1);
+              }
+              nans = Matrix16<T>::mul(of, ones, nans);
+            }
+#pragma unroll
+            for (int j = 0; j < VF; ++j)
+#pragma unroll
+              for (int e = 0; e < 4; ++e) o[j][e] += nans[e] > 0.f ? NAN : 0.f;
+#pragma unroll
+            for (int i = 0; i < VK; ++i)
+              if (vs[i] == kNone) take_out(i);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < VK; ++i) split_values<T, FORM, VF>(loaded.vc[i].w, vs[i], x.v[i]);
+      } else if (masked) {
         // Values of keys that do not count are zeros, and infinite or NaN ones, which a row that does not see them must not meet in a product, are taken out and
         // added to the rows that do see them.
         bool odd = false;
@@ -484,6 +534,31 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
       Tile x, y;
       request(x, t0, look_up(t0));
       int64_t next = look_up(min(t0 + 1, t1 - 1));
+      if constexpr (FORM != kPlain && split_ahead(DH, FORM) == 2) {
+        Tile z;
+        request(y, min(t0 + 1, t1 - 1), next);
+        next = look_up(min(t0 + 2, t1 - 1));
+#pragma unroll 1
+        for (int t = t0; t < t1; t += 3) {
+          request(z, min(t + 2, t1 - 1), next);
+          next = look_up(min(t + 3, t1 - 1));
+          __builtin_amdgcn_sched_barrier(0);
+          add(x, t);
+          __builtin_amdgcn_sched_barrier(0);
+          if (t + 1 >= t1) break;
+          request(x, min(t + 3, t1 - 1), next);
+          next = look_up(min(t + 4, t1 - 1));
+          __builtin_amdgcn_sched_barrier(0);
+          add(y, t + 1);
+          __builtin_amdgcn_sched_barrier(0);
+          if (t + 2 >= t1) break;
+          request(y, min(t + 4, t1 - 1), next);
+          next = look_up(min(t + 5, t1 - 1));
+          __builtin_amdgcn_sched_barrier(0);
+          add(z, t + 2);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else {
 #pragma unroll 1
       for (int t = t0; t < t1; t += 2) {
         request(y, min(t + 1, t1 - 1), next);
@@ -498,10 +573,11 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
         add(y, t + 1);
         __builtin_amdgcn_sched_barrier(0);
       }
+      }
     }
     l = split_sum(l);
     if (t0 == 0 && row_there && g == 0) {
-      const int last = t1 == s.tiles ? worker : (int)((tile + s.tiles - 1) / per);
+      const int last = t1 == s.tiles ? worker : (int)((tile + s.tiles - 1) / per) + (worker - stretch);
       ((int2 *)(parts + split_parts_floats(DH)))[(int64_t)(s.first + token) * a.n_q_heads + head] = int2{2 * worker + !begins, last};
     }
     // accumulator element e of product j: feature VF (4 g + e) + j of my row (plain fp32 with 128 features: 4 (4 g + e) + j % 4 of half j / 4)
