@@ -48,8 +48,13 @@ struct KvAttention {
   float *parts;
   int32_t form;               // of the pages: 0 as the element type, or a flame_kvq_form
   const char *k_scales, *v_scales;
-  const int32_t *group_offsets, *prefix_lens;   // shared histories (else NULL)
+  const int32_t *group_offsets, *prefix_lens;   // shared histories (else NULL); splits is 0 where their parts are of equal length
   int32_t n_groups;
+  int32_t budget;             // workgroups of row tiles over the histories that there is room for, a key head
+  int32_t split_blocks;       // workgroups of split attention over the sequences' own keys, in the same launch
+  int64_t part_rows;
+  int2 *cuts;                 // of up to 64 groups: where its parts begin, and how many a row tile has
+  float *own;
 };
 
 // How a call runs (kv_api.cpp): split kernel, or flash kernel with so many wavefronts per 32 rows and parts of the keys.
@@ -59,11 +64,13 @@ struct KvRoute {
   int64_t workspace;          // bytes
 };
 KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool paged, bool decode, int64_t capacity);
+KvRoute kvq_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool decode, int64_t capacity);   // over a quantised cache
 
 // The same for groups that share histories, and where the split part's workspace begins.
 struct KvSharedRoute {
-  int32_t wavefronts, splits;
-  int64_t split_at, workspace;
+  int32_t wavefronts, splits, budget;
+  int64_t slots, part_rows;                // row tiles (times parts) that there are at most, a key head; rows of parts
+  int64_t cuts_at, own_at, split_at, workspace;
 };
 KvSharedRoute kv_shared_route(const flame_kv_config &c, int32_t n_groups, int64_t n_rows, int64_t capacity);
 
@@ -77,9 +84,9 @@ hipError_t launch_kvq_read(const KvBatch &batch, const KvPages &pages, const KvS
 hipError_t launch_kvq_attention_f8(const KvAttention &a, int wavefronts, hipStream_t stream);
 hipError_t launch_kvq_attention_f4(const KvAttention &a, int wavefronts, hipStream_t stream);
 // shared histories (kv_shared.h)
-hipError_t launch_kv_shared_plain(const KvAttention &a, int wavefronts, void *split_workspace, hipStream_t stream);
-hipError_t launch_kv_shared_f8(const KvAttention &a, int wavefronts, void *split_workspace, hipStream_t stream);
-hipError_t launch_kv_shared_f4(const KvAttention &a, int wavefronts, void *split_workspace, hipStream_t stream);
+hipError_t launch_kv_shared_plain(const KvAttention &a, const KvSharedRoute &route, void *split_workspace, hipStream_t stream);
+hipError_t launch_kv_shared_f8(const KvAttention &a, const KvSharedRoute &route, void *split_workspace, hipStream_t stream);
+hipError_t launch_kv_shared_f4(const KvAttention &a, const KvSharedRoute &route, void *split_workspace, hipStream_t stream);
 hipError_t launch_kv_attention(const KvAttention &a, int wavefronts, hipStream_t stream);
 // few query rows: split over the keys (kv_split.hip)
 hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream);

@@ -27,6 +27,7 @@ constexpr int64_t kMaxRowHeads = (int64_t)1 << 25, kMaxSequenceHeads = ((int64_t
 constexpr int64_t kSmallCache = 1024;                          // tokens that a sequence has room for, up to which its keys are not split over the chip
 constexpr int64_t kMaxKeys = ((int64_t)1 << 31) - 65536;     // of a sequence: room for a tile's end behind them in 32 bits
 // Limits of kv_route, for the workspace of every call up to a size: rows times heads of an extend that is split, parts of a row tile's keys, and workgroups of a launch whose keys are cut.
+constexpr int64_t kFlashRows = 128, kSharedPlaces = 512;         // rows of a tile (kv_flash.h); workgroups over shared histories
 constexpr int64_t kSplitRowHeads = 16384, kMostParts = 64, kPartWorkgroups = 400;
 
 int64_t element(int32_t dtype) { return dtype == FLAME_KV_F32 ? 4 : 2; }
@@ -159,7 +160,9 @@ int attend_quantised(const flame_kv_config *cfg, const flame_kvq_cache *cache, c
   if (int rc = take_rows(cfg, out, &a.out)) return rc;
   if (int rc = take_pages(cfg, cache, &a.pages, &scales)) return rc;
   if (!kv_lens) return bad("kv_lens is NULL");
-  const int64_t need = workspace_bytes_for(*cfg, n_seqs, n_rows, offsets == nullptr);
+  const bool decode = offsets == nullptr;
+  const KvRoute route = kvq_route(*cfg, n_seqs, n_rows, decode, a.pages.capacity);
+  const int64_t need = std::max(kvq_route(*cfg, n_seqs, n_rows, decode, kMaxKeys).workspace, kvq_route(*cfg, n_seqs, n_rows, decode, kSmallCache).workspace);
   if (need > 0 && (!workspace || !aligned(workspace))) return bad("the workspace is NULL or not 16-byte aligned");
   if (workspace_bytes < need) return bad("the workspace is smaller than this call needs (flame_kv_workspace_bytes)", FLAME_GR_CAPACITY_EXCEEDED);
   a.batch = KvBatch{offsets, kv_lens, n_seqs, n_rows, faults};
@@ -167,19 +170,19 @@ int attend_quantised(const flame_kv_config *cfg, const flame_kvq_cache *cache, c
   a.form = scales.form;
   a.k_scales = scales.k;
   a.v_scales = scales.v;
-  const KvRoute route = kv_route(*cfg, n_seqs, n_rows, true, offsets == nullptr, a.pages.capacity);
   if (route.split) return done(launch_kvq_split(a, workspace, (hipStream_t)stream));
   a.splits = route.splits;
   a.parts = (float *)workspace;
   return done((a.form == FLAME_KVQ_F8 ? launch_kvq_attention_f8 : launch_kvq_attention_f4)(a, route.wavefronts, (hipStream_t)stream));
 }
 
-// What any flame_kv_shared of up to this many groups, sequences and rows may need: kv_shared_route's parts times rows and heads stay below the bound of workspace_bound (whose sequences
-// are the groups here), and there is a plane for the sequences' own keys and the split kernel's workspace.
+// What any flame_kv_shared of up to this many groups, sequences and rows may need.  Parts of equal length: row tiles are up to rows times heads over a tile's rows and a tile for each group and key head, or
+// kSharedPlaces of them, of up to 128 rows, and such a call has up to kPartWorkgroups tiles of 128 rows (and wavefronts, up to four, times as many smaller ones).  Others: as in workspace_bound, groups for sequences.
 int64_t shared_workspace_bound(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows) {
   if (n_seqs == 0 || n_rows == 0) return 0;
   const int64_t heads = n_rows * c.n_q_heads;
-  return (heads + std::max(heads, std::min(kMostParts * heads, (int64_t)1024 * 129))) * (c.head_dim + 2) * 4 + 16 + kv_split_workspace_bytes(c.head_dim, heads);
+  const int64_t parts = std::max({heads, std::min(kMostParts * heads, (int64_t)1024 * 129), std::max(kSharedPlaces, 4 * kPartWorkgroups) * kFlashRows});
+  return (heads + parts) * (c.head_dim + 2) * 4 + 64 * 8 + 48 + kv_split_workspace_bytes(c.head_dim, heads);
 }
 
 int check_groups(const flame_kv_config *c, int32_t n_groups, int32_t n_seqs, int64_t n_rows) {
@@ -205,7 +208,7 @@ int attend_shared(const flame_kv_config *cfg, const flame_kv_cache *cache, const
   if (int rc = plain ? take_pages(cfg, cache, &a.pages) : take_pages(cfg, quantised, &a.pages, &scales)) return rc;
   if (!kv_lens || !groups->prefix_lens || !groups->group_offsets) return bad("kv_lens, group_offsets or prefix_lens is NULL");
   const KvSharedRoute route = kv_shared_route(*cfg, groups->n_groups, n_rows, a.pages.capacity);
-  const int64_t need = kv_shared_route(*cfg, groups->n_groups, n_rows, kMaxKeys).workspace;
+  const int64_t need = std::max(kv_shared_route(*cfg, groups->n_groups, n_rows, kMaxKeys).workspace, kv_shared_route(*cfg, groups->n_groups, n_rows, 1).workspace);
   if (need > 0 && (!workspace || !aligned(workspace))) return bad("the workspace is NULL or not 16-byte aligned");
   if (workspace_bytes < need) return bad("the workspace is smaller than this call needs (flame_kv_shared_workspace_bytes)", FLAME_GR_CAPACITY_EXCEEDED);
   a.batch = KvBatch{offsets, kv_lens, n_seqs, n_rows, faults};
@@ -217,9 +220,13 @@ int attend_shared(const flame_kv_config *cfg, const flame_kv_cache *cache, const
   a.prefix_lens = groups->prefix_lens;
   a.n_groups = groups->n_groups;
   a.splits = route.splits;
+  a.budget = route.budget;
   a.parts = (float *)workspace;
+  a.part_rows = route.part_rows;
+  a.cuts = (int2 *)((char *)workspace + route.cuts_at);
+  a.own = (float *)((char *)workspace + route.own_at);
   const auto launch = plain ? launch_kv_shared_plain : a.form == FLAME_KVQ_F8 ? launch_kv_shared_f8 : launch_kv_shared_f4;
-  return done(launch(a, route.wavefronts, (char *)workspace + route.split_at, (hipStream_t)stream));
+  return done(launch(a, route, (char *)workspace + route.split_at, (hipStream_t)stream));
 }
 
 }  // namespace
@@ -228,7 +235,7 @@ namespace flame {
 
 // Decoding steps, and calls with few query rows over caches that may be long, split the keys over the chip; others run on row tiles, of which a launch of few has its keys cut
 // into parts.  The host knows rows and sequences, but of the keys only what the page table has room for.
-KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool paged, bool decode, int64_t capacity) {
+static KvRoute route_of(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool paged, bool decode, int64_t capacity, bool codes) {
   const bool f32 = c.dtype == FLAME_KV_F32;
   const int64_t group = c.n_q_heads / c.n_kv_heads, heads = n_rows * c.n_q_heads, rows = n_rows * group / std::max(n_seqs, 1);   // rows: of a sequence and key head
   // The split kernel reads the keys again for every 16 rows of a sequence and key head; up to there it reads them once, whatever the sequences' lengths, and carries no masked rows.
@@ -241,7 +248,12 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   // fp32: up to 32 rows: 2048 (16 x 4, 32/8, over 2048) 64 | 113, 16384 (64 x 8, 32/8, over 2048) 301 | 399; more: 512 (16 new, 32/8, over 4096) 36 | 55, 1024 (32 new, 32/8, over 4096) 49 | 91,
   //   (over 16384) 129 | 112, 2048 (64 new, 32/8, over 4096) 75 | 92, (over 16384) 235 | 168, 4096 (4 x 32, 32/8, over 4096) 137 | 100
   // Room for 512 tokens, bf16: 1024 (4 x 8, 32/8) 21 | 13
-  const int64_t few = f32 ? (rows <= 32 ? kSplitRowHeads : 1024) : rows > 32 ? 0 : rows > 16 ? 512 : n_seqs > 64 ? 8192 : 2048;
+  // Codes are half or a quarter of the bytes, for split attention more than for row tiles; us split | row tiles, f8 (f4), 16-bit rows:
+  //   up to 16 rows: 4096 (64 sequences x 2 new, 32/8 heads of 128, over 2048) 71 | 96 (51 | 88), 16384 (128 x 4) 148 | 176 (108 | 163), (256 x 2, over 1500) 174 | 303 (120 | 278),
+  //     12800 (400 x 4, 8/2 of 64, over 1100) 68 | 73 (59 | 60)
+  //   up to 32: 1024 (4 x 8, 32/8, over 4096) 26 | 26 (24 | 26), (over 16384) 54 | 70 (44 | 59), 8192 (32 x 8, over 2048) 69 | 76 (55 | 66), 2048 (32 x 8, 8/2 of 64, over 8192) 38 | 39 (34 | 32);
+  //   more: 384 (12 new, 32/8, over 16384) 37 | 34 (31 | 33), 4096 (128 new) 48 | 32
+  const int64_t few = f32 ? (rows <= 32 ? kSplitRowHeads : 1024) : rows > 32 ? 0 : codes ? kSplitRowHeads : rows > 16 ? 512 : n_seqs > 64 ? 8192 : 2048;
   if (decode || (paged && capacity > kSmallCache && heads <= few)) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim, heads)};
   // Four or two wavefronts share 32 rows where that many workgroups of one wavefront per 32 rows leave places of the chip empty, or all are placed at
   // once and wait for the longest.  us with one | two | four, at that many workgroups
@@ -274,17 +286,36 @@ KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool 
   return r;
 }
 
+KvRoute kv_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool paged, bool decode, int64_t capacity) { return route_of(c, n_seqs, n_rows, paged, decode, capacity, false); }
+KvRoute kvq_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool decode, int64_t capacity) { return route_of(c, n_seqs, n_rows, true, decode, capacity, true); }
+
 // The histories' rows are those of whole groups.
 KvSharedRoute kv_shared_route(const flame_kv_config &c, int32_t n_groups, int64_t n_rows, int64_t capacity) {
   const bool wide = c.dtype == FLAME_KV_F32 && c.head_dim == 128;
   const int64_t group = c.n_q_heads / c.n_kv_heads, heads = n_rows * c.n_q_heads, rows = n_rows * group / std::max(n_groups, 1);
-  const int32_t kp = rows <= 32 && !wide ? 4 : rows <= 64 ? 2 : 1;
-  KvSharedRoute r{kp, 1, 0, 0};
-  if ((n_rows * group / 128 + n_groups) * c.n_kv_heads <= kPartWorkgroups && capacity >= kSmallCache) {
-    const int64_t likely = std::max(n_groups * ((rows * kp + 127) / 128) * c.n_kv_heads, (int64_t)1);
-    r.splits = (int32_t)std::max((int64_t)1, std::min({(likely > 256 ? 1024 : 512) / likely, std::min(capacity / 256, std::max((int64_t)32, capacity / 512)), kMostParts}));
+  KvSharedRoute r{};
+  r.wavefronts = rows <= 32 && !wide ? 4 : rows <= 64 ? 2 : 1;
+  r.splits = 1;
+  const int64_t tile = kFlashRows / r.wavefronts;
+  r.slots = n_rows * group / tile + n_groups;
+  r.part_rows = n_groups > 0 ? heads : 0;
+  if (n_groups > 0 && (n_rows * group / 128 + n_groups) * c.n_kv_heads <= kPartWorkgroups && capacity >= kSmallCache) {
+    if (n_groups <= 64) {
+      // parts of equal length, for the chip's places
+      r.splits = 0;
+      r.budget = (int32_t)std::max((int64_t)1, kSharedPlaces / c.n_kv_heads);
+      r.slots = std::max(r.slots, (int64_t)r.budget);
+      r.part_rows = r.slots * c.n_kv_heads * tile;
+    } else {
+      const int64_t likely = std::max(n_groups * ((rows * r.wavefronts + 127) / 128) * c.n_kv_heads, (int64_t)1);
+      r.splits = (int32_t)std::max((int64_t)1, std::min({(likely > 256 ? 1024 : 512) / likely, std::min(capacity / 256, std::max((int64_t)32, capacity / 512)), kMostParts}));
+      r.part_rows = r.splits * heads;
+    }
   }
-  r.split_at = ((r.splits + 1) * heads * (c.head_dim + 2) * 4 + 15) / 16 * 16;
+  const auto up = [](int64_t n) { return (n + 15) / 16 * 16; };
+  r.cuts_at = up(r.part_rows * (c.head_dim + 2) * 4);
+  r.own_at = r.cuts_at + 64 * 8;
+  r.split_at = up(r.own_at + heads * (c.head_dim + 2) * 4);
   r.workspace = r.split_at + kv_split_workspace_bytes(c.head_dim, heads);
   return r;
 }

@@ -8,7 +8,7 @@ hipError_t launch_kv_attention(const KvAttention &a, int wavefronts, hipStream_t
   flash_with_shape(a, wavefronts, [&](auto t, auto width, auto kp) {
     using T = decltype(t);
     constexpr int DH = decltype(width)::value, KP = decltype(kp)::value;
-    e = a.pages.table ? launch_flash<T, DH, true, KP, kPlain, false>(a, stream) : launch_flash<T, DH, false, KP, kPlain, false>(a, stream);
+    e = a.pages.table ? launch_flash<T, DH, true, KP, kPlain>(a, stream) : launch_flash<T, DH, false, KP, kPlain>(a, stream);
   });
   return e;
 }

@@ -73,10 +73,13 @@ template <typename T> __device__ __forceinline__ uint32_t only_finite(uint32_t w
   return ((w & E) == E ? 0u : w & 0xffffu) | ((w >> 16 & E) == E ? 0u : w & 0xffff0000u);
 }
 
-// Parts of rows whose keys were cut, in the workspace: of every part and output row the sums [planes][rows][features], and behind them the maxima and weights [planes][rows].  Planes are those of the
-// row tiles' parts, and with shared histories one more, for the sequences' own keys.
+// Parts of rows whose keys were cut, in the workspace: of every part and output row the sums [planes][rows][features], and behind them the maxima and weights [planes][rows].
 __device__ __forceinline__ int64_t kv_part_row(const KvAttention &a, int plane, int64_t row) { return plane * a.batch.n_rows * a.n_q_heads + row; }
 __device__ __forceinline__ float2 *kv_part_state(const KvAttention &a, int planes) { return (float2 *)(a.parts + planes * a.batch.n_rows * a.n_q_heads * a.head_dim); }
+
+// With shared histories: the parts of the histories, whose states stand behind a.part_rows of them, and the results over the sequences' own keys, a row each.
+__device__ __forceinline__ float2 *kv_shared_state(const KvAttention &a) { return (float2 *)(a.parts + a.part_rows * a.head_dim); }
+__device__ __forceinline__ float2 *kv_own_state(const KvAttention &a) { return (float2 *)(a.own + a.batch.n_rows * a.n_q_heads * a.head_dim); }
 
 // Softmax weights are 2^(logit - reference), and `above` is what log2 of a weight may come to.  fp16 weights would be zeros from 2^-25 on, thousands of which can make up a row's result
 // beside one of 1; they are held as high as its range has room (up to 2^15), by a reference that is as much lower, in numerator and denominator alike.  Others need no such place.

@@ -141,8 +141,42 @@ __device__ __forceinline__ int flash_shared_seen(const KvAttention &a, const Fla
   return (int)max((int64_t)0, min(sees, (int64_t)min(history, kv_clip(a.prefix_lens[b], a.pages.capacity))));
 }
 
+// How the keys of shared histories are cut where there is room for `budget` workgroups a key head: lane g holds group g (of up to 64), whose `tiles` row tiles have `keys` key tiles each.  All parts have the same
+// number of key tiles, the least (of at least kSharedTiles) with which they are no more than the budget; the last one of a row tile may be shorter.
+constexpr int kSharedTiles = 2;
+struct FlashCut {
+  int parts, before;     // of a row tile of the lane's group; slots of the groups ahead of it
+  int chunk;
+};
+__device__ __forceinline__ int flash_wave_sum(int v) {
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) v += __shfl_xor(v, i);
+  return v;
+}
+__device__ __forceinline__ FlashCut flash_cut(int tiles, int keys, int budget, int lane) {
+  if (keys == 0) tiles = 0;
+  const int work = flash_wave_sum((int)min((int64_t)tiles * keys, (int64_t)1 << 24)), rows = flash_wave_sum(tiles);
+  FlashCut c{0, 0, max(kSharedTiles, (work + budget - 1) / max(budget, 1))};
+  // (each step adds a sixteenth: from the least that could do to a part for each row tile there are fewer than 200)
+  for (;;) {
+    c.parts = tiles ? (keys + c.chunk - 1) / c.chunk : 0;
+    const int all = flash_wave_sum(tiles * c.parts);
+    if (all <= budget || all == rows) break;
+    c.chunk += max(1, c.chunk / 16);
+  }
+  int sums = tiles * c.parts;
+#pragma unroll
+  for (int i = 1; i < 64; i <<= 1) {
+    const int other = __shfl_up(sums, i);
+    sums += lane >= i ? other : 0;
+  }
+  c.before = sums - tiles * c.parts;
+  return c;
+}
+
+// (kv_shared.h runs this beside split attention in one launch: `block` of `blocks` is its own.)
 template <typename T, int DH, bool PAGED, int KP, int FORM, bool SHARED>
-__global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash_kernel(KvAttention a) {
+__device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_block, unsigned blocks) {
   static_assert(PAGED || (FORM == kPlain && !SHARED), "codes and histories lie in pages");
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int QT = kFlashRows / KP;                             // query rows of a workgroup
@@ -161,7 +195,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   const int group = a.n_q_heads / a.n_kv_heads;
 
   // Which tile.  Tiles with most keys go first: the sequences by their number of keys, and each from its end.
-  if (!SHARED && blockIdx.x == 0 && a.batch.faults)
+  if (!SHARED && my_block == 0 && a.batch.faults)
     for (int b = threadIdx.x; b < a.batch.n_seqs; b += 256) {
       const int64_t first = a.batch.offsets[b], end = a.batch.offsets[b + 1];
       kv_report_offsets(first, end, a.batch.n_rows, a.batch.faults);
@@ -175,14 +209,17 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
     }
   // Of a compute unit's workgroups, one is of the first 256 and one of the next: those go the other way round, so that a long one has a short one beside it
   // (4 prompts of 2048, 8/2 heads of 64: 50 -> 40 us, fp32 4 of 1024, 16 heads of 32: 69 -> 60; launches of many more are as before).
-  unsigned block = blockIdx.x;
-  if (flash_workgroups<T, DH, KP>() >= 2) {
-    const unsigned placed = min(gridDim.x, 512u);
+  unsigned block = my_block;
+  if (!SHARED && flash_workgroups<T, DH, KP>() >= 2) {
+    const unsigned placed = min(blocks, 512u);
     if (block >= 256 && block < placed) block = 256 + placed - 1 - block;
   }
   const int kvh = block % a.n_kv_heads;
-  const int64_t slot = block / a.n_kv_heads / a.splits;
-  const int split = block / a.n_kv_heads % a.splits;
+  const bool balanced = SHARED && a.splits == 0;                  // (see flash_cut)
+  const int splits = SHARED ? max(a.splits, 1) : a.splits;
+  const int64_t slot = block / a.n_kv_heads / splits;
+  int split = block / a.n_kv_heads % splits;
+  FlashCut even{1, 0, 0};
   int seq;
   int64_t tile, first, end;                                       // tile: counted from the sequence's end
   int kv_len = 0;
@@ -209,6 +246,12 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
     const uint64_t wrong = __builtin_amdgcn_ballot_w64(none || kv_wrong_offsets(b, e));
     if (wrong && lane >= __builtin_ctzll(wrong)) tiles = 0;
     int before = 0;
+    if (balanced) {
+      even = flash_cut((int)tiles, (max(keys, 0) + KW - 1) / KW, a.budget, lane);
+      if (my_block == 0 && threadIdx.x < 64) a.cuts[lane] = int2{even.before, even.parts};
+      before = even.before;
+      tiles *= even.parts;
+    } else
     for (int j = 0; j < n_spans; ++j) {
       const int other = __builtin_amdgcn_readlane(keys, j);
       before += other > keys || (other == keys && j < lane) ? __builtin_amdgcn_readlane((int)tiles, j) : 0;
@@ -217,12 +260,17 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
     if (!mine) return;
     seq = __builtin_ctzll(mine);
     tile = slot - __builtin_amdgcn_readlane(before, seq);
+    if (balanced) {
+      even.parts = __builtin_amdgcn_readlane(even.parts, seq);
+      split = (int)tile % even.parts;
+      tile = (int)tile / even.parts;
+    }
     first = __builtin_amdgcn_readlane(b, seq);
     end = __builtin_amdgcn_readlane(e, seq);
     if (PAGED) kv_len = __builtin_amdgcn_readlane(keys, seq);
   } else {
     // Those of sequence b begin at slot offsets[b] * G / QT + b, where there is room for them whatever the lengths; the last sequence goes first.
-    const int64_t back_slot = gridDim.x / a.n_kv_heads / a.splits - 1 - slot;
+    const int64_t back_slot = blocks / a.n_kv_heads / splits - 1 - slot;
     int lo = 0, n = n_spans;                                      // the last sequence whose slots begin at or before this one
     while (n > 1) {
       const int step = (n + 63) / 64;
@@ -258,7 +306,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   const int rows = (int)max((int64_t)0, min(end, a.batch.n_rows) - first) * group;
   const int row_tiles = (rows + QT - 1) / QT;
   if (tile < 0 || tile >= row_tiles) return;
-  const int row0 = (row_tiles - 1 - (int)tile) * QT;
+  const int row0 = SHARED ? (int)tile * QT : (row_tiles - 1 - (int)tile) * QT;
 
   int n;
   const char *kp, *vp;
@@ -283,7 +331,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   auto seen_by = [&](int row) { return (int)max((int64_t)0, back + row / group + 1); };
   const int n_seen = SHARED ? n : seen_by(min(row0 + QT, rows) - 1);
   // the workgroup's tiles: all, or a part of them
-  const FlashParts cut = flash_parts<KW>(n_seen, a.splits);
+  const FlashParts cut = balanced ? FlashParts{even.parts, even.chunk} : flash_parts<KW>(n_seen, splits);
   if (split >= cut.parts || (SHARED && n == 0)) return;
   const int t_begin = split * cut.tiles, n_tiles = min(cut.tiles, (n_seen + KW - 1) / KW - t_begin), key0 = t_begin * KW;
   const int part = KP == 1 ? 0 : wave % KP, wave_row = row0 + wave / KP * 32;
@@ -693,9 +741,9 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
       }
       const int tk = row / group, h = kvh * group + row - tk * group;
       if (SHARED || cut.parts > 1) {
-        const int64_t to = kv_part_row(a, split, (first + tk) * a.n_q_heads + h);
+        const int64_t to = balanced ? (slot * a.n_kv_heads + kvh) * QT + r : kv_part_row(a, split, (first + tk) * a.n_q_heads + h);
         *(f32x4 *)(a.parts + to * DH + f) = x;
-        if (f == 0) kv_part_state(a, SHARED ? a.splits + 1 : a.splits)[to] = float2{top, sum};
+        if (f == 0) (SHARED ? kv_shared_state(a) : kv_part_state(a, a.splits))[to] = float2{top, sum};
         continue;
       }
       const float inv = top == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
@@ -710,7 +758,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
   if (SHARED || cut.parts > 1) {
     if (wave_row + l32 >= rows) return;
     const int row = wave_row + l32, tk = row / group;
-    const int64_t to = kv_part_row(a, split, (first + tk) * a.n_q_heads + kvh * group + row - tk * group);
+    const int64_t to = balanced ? (slot * a.n_kv_heads + kvh) * QT + row - row0 : kv_part_row(a, split, (first + tk) * a.n_q_heads + kvh * group + row - tk * group);
     float *po = a.parts + to * DH;
     if constexpr (F32) {
 #pragma unroll
@@ -726,7 +774,7 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
 #pragma unroll
         for (int i = 0; i < 4; ++i) *(f32x4 *)(po + 32 * b + 8 * i + 4 * lh) = f32x4{o[b][4 * i], o[b][4 * i + 1], o[b][4 * i + 2], o[b][4 * i + 3]};
     }
-    if (lh == 0) kv_part_state(a, SHARED ? a.splits + 1 : a.splits)[to] = float2{m, l};
+    if (lh == 0) (SHARED ? kv_shared_state(a) : kv_part_state(a, a.splits))[to] = float2{m, l};
     return;
   }
   const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
@@ -764,6 +812,11 @@ __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash
       *(word4 *)(a.out.p + (first + tk) * a.out.row + h * a.out.head + chunk * 16) = *(const word4 *)(patch + r * RB + ((chunk ^ (r & (CH - 1))) << 4));
     }
   }
+}
+
+template <typename T, int DH, bool PAGED, int KP, int FORM>
+__global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_flash_kernel(KvAttention a) {
+  flash_rows<T, DH, PAGED, KP, FORM, false>(a, blockIdx.x, gridDim.x);
 }
 
 // Adds up the parts of rows whose keys were cut, in the order of the keys.  DH / 4 lanes a head, and a workgroup 256 / (DH / 4) heads of a token, so that all loads of a lane are in
@@ -811,15 +864,14 @@ __global__ __launch_bounds__(256) void kv_flash_join_kernel(KvAttention a) {
   *(out4 *)(a.out.p + q_row * a.out.row + head * a.out.head + f * sizeof(T)) = y;
 }
 
-template <typename T, int DH, bool PAGED, int KP, int FORM, bool SHARED> hipError_t launch_flash(const KvAttention &a, hipStream_t stream) {
+template <typename T, int DH, bool PAGED, int KP, int FORM> hipError_t launch_flash(const KvAttention &a, hipStream_t stream) {
   static std::atomic<uint64_t> raised{0};
   constexpr int kBytes = flash_lds_bytes<T, DH, KP>();
-  const hipError_t e = raise_lds_limit(reinterpret_cast<const void *>(&kv_flash_kernel<T, DH, PAGED, KP, FORM, SHARED>), kBytes, raised);
+  const hipError_t e = raise_lds_limit(reinterpret_cast<const void *>(&kv_flash_kernel<T, DH, PAGED, KP, FORM>), kBytes, raised);
   if (e != hipSuccess) return e;
-  const int64_t slots = a.batch.n_rows * (a.n_q_heads / a.n_kv_heads) / (kFlashRows / KP) + (SHARED ? a.n_groups : a.batch.n_seqs);
-  kv_flash_kernel<T, DH, PAGED, KP, FORM, SHARED><<<(unsigned)(slots * a.n_kv_heads * a.splits), 256, kBytes, stream>>>(a);
-  if constexpr (!SHARED)
-    if (a.splits > 1) kv_flash_join_kernel<T, DH, KP><<<(unsigned)(a.batch.n_rows * ((a.n_q_heads * (DH / 4) + 255) / 256)), 256, 0, stream>>>(a);
+  const int64_t slots = a.batch.n_rows * (a.n_q_heads / a.n_kv_heads) / (kFlashRows / KP) + a.batch.n_seqs;
+  kv_flash_kernel<T, DH, PAGED, KP, FORM><<<(unsigned)(slots * a.n_kv_heads * a.splits), 256, kBytes, stream>>>(a);
+  if (a.splits > 1) kv_flash_join_kernel<T, DH, KP><<<(unsigned)(a.batch.n_rows * ((a.n_q_heads * (DH / 4) + 255) / 256)), 256, 0, stream>>>(a);
   return hipGetLastError();
 }
 

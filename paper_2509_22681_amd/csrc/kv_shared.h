@@ -12,9 +12,16 @@ namespace flame {
 namespace {
 
 // Bound by latency and by the planes, which it reads once.  DH / 4 lanes a head, and a workgroup 256 / (DH / 4) heads of a row.
+template <typename T, int DH, int KP, int FORM>
+__global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_shared_kernel(KvAttention a, float *__restrict__ split_parts) {
+  const unsigned tiles = gridDim.x - a.split_blocks;
+  if (blockIdx.x < tiles) flash_rows<T, DH, true, KP, FORM, true>(a, blockIdx.x, tiles);
+  else split_units<T, DH, FORM, true>(a, split_parts, blockIdx.x - tiles, a.split_blocks * 4);
+}
+
 template <typename T, int DH, int KP>
 __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, const float *__restrict__ split_parts) {
-  constexpr int KW = KP * key_block<T, DH, KP>();
+  constexpr int KW = KP * key_block<T, DH, KP>(), QT = kFlashRows / KP;
   constexpr int H = 256 / (DH / 4);
   const int lane = threadIdx.x & 63;
   if (blockIdx.x == 0 && a.batch.faults) {
@@ -44,18 +51,30 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, cons
   }
   // parts of the history
   int parts = 0;
+  int64_t part_at = 0, step = a.batch.n_rows * a.n_q_heads;       // the first one's row, and from one to the next
+  const int64_t from = q_row * a.n_q_heads + head;
+  const int group = a.n_q_heads / a.n_kv_heads, kvh = head / group;
   const int g = kv_find_sequence(a.group_offsets, a.n_groups, seq, lane);
   if (g < a.n_groups) {
     const int b0 = a.group_offsets[g];
     if (b0 >= 0 && b0 <= seq) {
       const int history = kv_clip(a.prefix_lens[b0], a.pages.capacity);
-      if (history > 0) parts = flash_parts<KW>(history, a.splits).parts;
+      if (history > 0 && a.splits == 0) {
+        const int64_t group_first = a.batch.offsets ? a.batch.offsets[b0] : b0;
+        const int2 cut = a.cuts[g];
+        const int row = (int)((q_row - group_first) * group) + head % group;
+        parts = cut.y;
+        part_at = ((cut.x + (int64_t)(row / QT) * parts) * a.n_kv_heads + kvh) * QT + row % QT;
+        step = (int64_t)a.n_kv_heads * QT;
+      } else if (history > 0) {
+        parts = flash_parts<KW>(history, a.splits).parts;
+        part_at = from;
+      }
     }
   }
   if (head >= a.n_q_heads) return;
-  const int64_t step = a.batch.n_rows * a.n_q_heads, from = q_row * a.n_q_heads + head;
-  const float2 *state = kv_part_state(a, a.splits + 1) + from;
-  const float *sums = a.parts + from * DH + f;
+  const float2 *state = kv_shared_state(a) + part_at;
+  const float *sums = a.parts + part_at * DH + f;
   float m = -INFINITY, l = 0.f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
   const auto add = [&](float mw, float lw, f32x4 ow) {
@@ -66,7 +85,7 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, cons
     for (int i = 0; i < 4; ++i) o[i] = o[i] * keep + ow[i] * take;
     m = m_new;
   };
-#pragma unroll 4
+#pragma unroll 8
   for (int p = 0; p < parts; ++p) {
     const float2 ml = state[p * step];
     add(ml.x, ml.y, *(const f32x4 *)(sums + p * step * DH));
@@ -74,14 +93,14 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, cons
   // the sequence's own keys: one plane, or parts of wavefronts
   const int2 of = ((const int2 *)(split_parts + split_parts_floats(DH)))[from];
   if (of.x >= 0 && of.x >> 1 < of.y && of.y < split_workers(DH)) {
-    const int group = a.n_q_heads / a.n_kv_heads, r = (int)(((q_row - first) * group + head % group) % kRows);
+    const int r = (int)(((q_row - first) * group + head % group) % kRows);
     for (int w = of.x >> 1; w <= of.y; ++w) {
       const float *part = split_parts + ((int64_t)w * 2 + (w == of.x >> 1 ? of.x & 1 : 0)) * split_part_floats(DH);
       add(part[r], part[kRows + r], *(const f32x4 *)(part + 2 * kRows + r * DH + f));
     }
   } else {
-    const float2 ml = state[a.splits * step];
-    add(ml.x, ml.y, *(const f32x4 *)(sums + a.splits * step * DH));
+    const float2 ml = kv_own_state(a)[from];
+    add(ml.x, ml.y, *(const f32x4 *)(a.own + from * DH + f));
   }
   const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
   typedef T out4 __attribute__((ext_vector_type(4)));
@@ -91,16 +110,18 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, cons
   *(out4 *)(a.out.p + q_row * a.out.row + head * a.out.head + f * sizeof(T)) = y;
 }
 
-template <int FORM> hipError_t launch_shared(const KvAttention &a, int wavefronts, void *split_workspace, hipStream_t stream) {
+template <int FORM> hipError_t launch_shared(const KvAttention &call, const KvSharedRoute &route, void *split_workspace, hipStream_t stream) {
   hipError_t e = hipErrorInvalidValue;
-  flash_with_shape(a, wavefronts, [&](auto t, auto width, auto kp) {
+  flash_with_shape(call, route.wavefronts, [&](auto t, auto width, auto kp) {
     using T = decltype(t);
-    constexpr int DH = decltype(width)::value, KP = decltype(kp)::value;
-    if (a.n_groups > 0) {
-      e = launch_flash<T, DH, true, KP, FORM, true>(a, stream);
-      if (e != hipSuccess) return;
-    }
-    kv_split_kernel<T, DH, FORM, true><<<split_workers(DH) / 4, 256, 0, stream>>>(a, (float *)split_workspace);
+    constexpr int DH = decltype(width)::value, KP = decltype(kp)::value, kBytes = flash_lds_bytes<T, DH, KP>();
+    static std::atomic<uint64_t> raised{0};
+    e = raise_lds_limit(reinterpret_cast<const void *>(&kv_shared_kernel<T, DH, KP, FORM>), kBytes, raised);
+    if (e != hipSuccess) return;
+    KvAttention a = call;
+    a.split_blocks = split_workers(DH) / 4;
+    const int64_t tiles = a.n_groups ? route.slots * a.n_kv_heads * std::max(a.splits, 1) : 0;
+    kv_shared_kernel<T, DH, KP, FORM><<<(unsigned)(a.split_blocks + tiles), 256, kBytes, stream>>>(a, (float *)split_workspace);
     kv_shared_join_kernel<T, DH, KP><<<(unsigned)(a.batch.n_rows * ((a.n_q_heads * (DH / 4) + 255) / 256)), 256, 0, stream>>>(a, (const float *)split_workspace);
     e = hipGetLastError();
   });

@@ -3,6 +3,6 @@
 
 namespace flame {
 
-hipError_t launch_kv_shared_f8(const KvAttention &a, int wavefronts, void *split_workspace, hipStream_t stream) { return launch_shared<kF8>(a, wavefronts, split_workspace, stream); }
+hipError_t launch_kv_shared_f8(const KvAttention &a, const KvSharedRoute &route, void *split_workspace, hipStream_t stream) { return launch_shared<kF8>(a, route, split_workspace, stream); }
 
 }  // namespace flame

@@ -129,13 +129,13 @@ struct SplitPlace {
   SplitSeq mine;      // the lane's sequence, of up to 64
 };
 
-template <int KT, bool SHARED, typename F> __device__ __forceinline__ SplitPlace split_find(const KvAttention &a, int lane, int heads, F target) {
+template <int KT, bool SHARED, typename F> __device__ __forceinline__ SplitPlace split_find(const KvAttention &a, int lane, int heads, bool reports, F target) {
   SplitPlace p{0, 0, a.batch.n_seqs, SplitSeq{}};
   int lo = 0, n = a.batch.n_seqs;
   int64_t base = 0, at = 0;
   for (bool top = true;; top = false) {
     // lane i: the tiles of `chunk` sequences from lo + i chunk on, of one sequence in the end
-    const bool report = top && blockIdx.x == 0 && threadIdx.x < 64;
+    const bool report = top && reports && threadIdx.x < 64;
     int64_t mine = 0;
     int chunk = 1;
     if (n <= 64) {
@@ -219,8 +219,9 @@ template <> struct Matrix16<half_t> {
   static __device__ __forceinline__ f32x4 mul(frag x, frag y, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(x, y, c, 0, 0, 0); }
 };
 
+// (kv_shared.h runs this beside row tiles in one launch: block `my_block` of its own, `workers` wavefronts in all.)
 template <typename T, int DH, int FORM, bool SHARED>
-__global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAttention a, float *__restrict__ parts) {
+__device__ __forceinline__ void split_units(const KvAttention &a, float *__restrict__ parts, unsigned my_block, int workers) {
   typedef SplitShape<T, DH, FORM> S;
   constexpr int KT = S::KT, VF = S::VF;
   constexpr bool F32 = S::F32;
@@ -237,11 +238,11 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
   // Codes of a token's heads lie side by side where its page is laid out token by token, several heads to a line of the caches, and so do scales.  So of codes, up to four wavefronts of a workgroup take the
   // same tiles of neighbouring heads: `together` of them share a stretch of the line, which is shorter by as much.  Storage for parts goes by head first, so that a head's parts are neighbours.
   const int together = FORM == kPlain ? 1 : a.n_kv_heads % 4 == 0 ? 4 : a.n_kv_heads % 2 == 0 ? 2 : 1;
-  const int stretches = split_workers(DH) / together, stretch = FORM == kPlain ? blockIdx.x * 4 + wave : blockIdx.x * (4 / together) + wave / together;
+  const int stretches = workers / together, stretch = FORM == kPlain ? my_block * 4 + wave : my_block * (4 / together) + wave / together;
   const int my_head = FORM == kPlain ? 0 : wave % together, worker = FORM == kPlain ? stretch : my_head * stretches + stretch;
   const int heads = FORM == kPlain ? a.n_kv_heads : a.n_kv_heads / together;
   int64_t per = 0;
-  SplitPlace place = split_find<KT, SHARED>(a, lane, heads, [&](int64_t total) {
+  SplitPlace place = split_find<KT, SHARED>(a, lane, heads, my_block == 0, [&](int64_t total) {
     per = (total + stretches - 1) / stretches;
     return (int64_t)stretch * per;
   });
@@ -584,9 +585,9 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
     auto feature = [&](int e, int j) { return VB == 32 && FORM == kPlain ? 64 * (j >> 2) + 4 * (4 * g + e) + (j & 3) : VF * (4 * g + e) + j; };
     if (SHARED && t0 == 0 && t1 == s.tiles) {
       if (row_there) {
-        const int64_t to = kv_part_row(a, a.splits, (int64_t)(s.first + token) * a.n_q_heads + head);
-        if (g == 0) kv_part_state(a, a.splits + 1)[to] = float2{m, l};
-        float *sums = a.parts + to * DH;
+        const int64_t to = (int64_t)(s.first + token) * a.n_q_heads + head;
+        if (g == 0) kv_own_state(a)[to] = float2{m, l};
+        float *sums = a.own + to * DH;
 #pragma unroll
         for (int e = 0; e < 4; ++e)
 #pragma unroll
@@ -617,6 +618,11 @@ __global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAt
     tile += t1 - t0;
     begins = false;
   }
+}
+
+template <typename T, int DH, int FORM>
+__global__ __launch_bounds__(256, split_occupancy(DH)) void kv_split_kernel(KvAttention a, float *__restrict__ parts) {
+  split_units<T, DH, FORM, false>(a, parts, blockIdx.x, split_workers(DH));
 }
 
 // Adds up the parts of the query rows and heads whose units were cut; a workgroup looks at `rows` of them.  Bound by latency (4 to 8 us): DH / 4 lanes share a part, so that
@@ -694,7 +700,7 @@ template <int FORM> hipError_t launch_split(const KvAttention &a, void *workspac
     using T = decltype(t);
     kv_with_width(a.head_dim, [&](auto width) {
       constexpr int DH = decltype(width)::value;
-      kv_split_kernel<T, DH, FORM, false><<<split_workers(DH) / 4, 256, 0, stream>>>(a, (float *)workspace);
+      kv_split_kernel<T, DH, FORM><<<split_workers(DH) / 4, 256, 0, stream>>>(a, (float *)workspace);
       kv_join_kernel<T, DH><<<(unsigned)((joins + rows - 1) / rows), 256, 0, stream>>>(a, (const float *)workspace, rows);
     });
   });
