@@ -33,8 +33,6 @@ namespace {
 // memory speed all the same.
 constexpr int split_occupancy(int dh) { return dh == 128 ? 2 : dh == 64 ? 3 : 4; }
 constexpr int split_workers(int dh) { return 1024 * split_occupancy(dh); }
-// Tiles of codes that a wavefront has requested ahead of the one at work.
-constexpr int split_ahead(int dh, int form) { return 1; }
 constexpr int kRows = 16;           // query rows of a unit
 
 template <typename T, int DH, int FORM> struct SplitShape {
@@ -535,31 +533,6 @@ __device__ __forceinline__ void split_units(const KvAttention &a, float *__restr
       Tile x, y;
       request(x, t0, look_up(t0));
       int64_t next = look_up(min(t0 + 1, t1 - 1));
-      if constexpr (FORM != kPlain && split_ahead(DH, FORM) == 2) {
-        Tile z;
-        request(y, min(t0 + 1, t1 - 1), next);
-        next = look_up(min(t0 + 2, t1 - 1));
-#pragma unroll 1
-        for (int t = t0; t < t1; t += 3) {
-          request(z, min(t + 2, t1 - 1), next);
-          next = look_up(min(t + 3, t1 - 1));
-          __builtin_amdgcn_sched_barrier(0);
-          add(x, t);
-          __builtin_amdgcn_sched_barrier(0);
-          if (t + 1 >= t1) break;
-          request(x, min(t + 3, t1 - 1), next);
-          next = look_up(min(t + 4, t1 - 1));
-          __builtin_amdgcn_sched_barrier(0);
-          add(y, t + 1);
-          __builtin_amdgcn_sched_barrier(0);
-          if (t + 2 >= t1) break;
-          request(y, min(t + 4, t1 - 1), next);
-          next = look_up(min(t + 5, t1 - 1));
-          __builtin_amdgcn_sched_barrier(0);
-          add(z, t + 2);
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      } else {
 #pragma unroll 1
       for (int t = t0; t < t1; t += 2) {
         request(y, min(t + 1, t1 - 1), next);
@@ -573,7 +546,6 @@ __device__ __forceinline__ void split_units(const KvAttention &a, float *__restr
         __builtin_amdgcn_sched_barrier(0);
         add(y, t + 1);
         __builtin_amdgcn_sched_barrier(0);
-      }
       }
     }
     l = split_sum(l);
