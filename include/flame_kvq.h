@@ -26,7 +26,7 @@ extern "C" {
 
 typedef enum { FLAME_KVQ_F8 = 1, FLAME_KVQ_F4 = 2 } flame_kvq_form;
 
-/* As flame_kv_cache, with strides in BYTES of codes, each a multiple of what a head's row takes (head_dim bytes in F8, head_dim / 2 in F4), pools 16-byte aligned.  Features 2j and 2j + 1
+/* As flame_kv_cache, with strides in BYTES of codes, not negative, each a multiple of what a head's row takes (head_dim bytes in F8, head_dim / 2 in F4), pools 16-byte aligned.  Features 2j and 2j + 1
  * are the lower and upper half of byte j in F4.  The scale of the 32 features whose codes begin at byte x of k is byte x / 32 (F8) or x / 16 (F4) of k_scales, e + 127; v alike.
  * Scales are 4-byte aligned. */
 typedef struct {
@@ -40,7 +40,7 @@ typedef struct {
   int32_t pages_per_seq;
 } flame_kvq_cache;
 
-/* flame_kv_append into such a cache.  The same call gives the same bits. */
+/* flame_kv_append into such a cache.  The same call gives the same bits.  Of two new tokens in one slot every code and every scale there is one or the other's, and not always of the same one. */
 int flame_kvq_append(const flame_kv_config *cfg, const flame_kvq_cache *cache, const flame_kv_rows *k, const flame_kv_rows *v, const flame_kv_rows *q, const flame_kv_rows *q_out,
                      const flame_kv_rotation *rotation, const int32_t *offsets, const int32_t *kv_lens, int32_t n_seqs, int64_t n_tokens, int32_t *faults, void *stream);
 

@@ -54,6 +54,8 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, cons
   int64_t part_at = 0, step = a.batch.n_rows * a.n_q_heads;       // the first one's row, and from one to the next
   const int64_t from = q_row * a.n_q_heads + head;
   const int group = a.n_q_heads / a.n_kv_heads, kvh = head / group;
+  int2 of = {0, 0};
+  if (head < a.n_q_heads) of = ((const int2 *)(split_parts + split_parts_floats(DH)))[from];
   const int g = kv_find_sequence(a.group_offsets, a.n_groups, seq, lane);
   if (g < a.n_groups) {
     const int b0 = a.group_offsets[g];
@@ -62,10 +64,12 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, cons
       if (history > 0 && a.splits == 0) {
         const int64_t group_first = a.batch.offsets ? a.batch.offsets[b0] : b0;
         const int2 cut = a.cuts[g];
-        const int row = (int)((q_row - group_first) * group) + head % group;
+        const int64_t row = (q_row - group_first) * group + head % group;
         parts = cut.y;
-        part_at = ((cut.x + (int64_t)(row / QT) * parts) * a.n_kv_heads + kvh) * QT + row % QT;
+        part_at = ((cut.x + row / QT * parts) * a.n_kv_heads + kvh) * QT + row % QT;
         step = (int64_t)a.n_kv_heads * QT;
+        // (offsets of more than 64 sequences that are none may claim other rows than were counted)
+        if (row < 0 || parts < 0 || part_at + (parts - 1) * step >= a.part_rows) parts = 0;
       } else if (history > 0) {
         parts = flash_parts<KW>(history, a.splits).parts;
         part_at = from;
@@ -91,7 +95,6 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, cons
     add(ml.x, ml.y, *(const f32x4 *)(sums + p * step * DH));
   }
   // the sequence's own keys: one plane, or parts of wavefronts
-  const int2 of = ((const int2 *)(split_parts + split_parts_floats(DH)))[from];
   if (of.x >= 0 && of.x >> 1 < of.y && of.y < split_workers(DH)) {
     const int r = (int)(((q_row - first) * group + head % group) % kRows);
     for (int w = of.x >> 1; w <= of.y; ++w) {

@@ -580,3 +580,210 @@ def test_two_calls_at_once(B, form):  # noqa: F811
             call(B, c, "shared", q, *args, o, ws, stream=s)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+# ---------------------------------------------------------------------------------------------- what else the calls allow
+@pytest.mark.parametrize("form", [None, "f8", "f4"])
+@pytest.mark.parametrize("dtype,hq,hkv,dim", [("bf16", 2, 1, 64), ("f16", 4, 4, 32), ("f32", 3, 1, 32)])
+def test_shared_of_more_groups_than_lanes_over_long_histories(B, form, dtype, hq, hkv, dim):  # noqa: F811
+    """Seventy groups whose histories are cut into parts (not of equal length: that takes a lane for each group)."""
+    import torch
+    gen = generator(70 + dim)
+    groups = [(900 + 17 * g, [(901 + 17 * g + 3 * i, 1 + (g + i) % 2, None) for i in range(1 + g % 3)]) for g in range(70)]
+    c, lens, new, prefix, lists, first = shared_case(B, gen, form, dtype, hq, hkv, dim, groups, page=64, tokens=4096)
+    q = rand(gen, dtype, sum(new), hq, dim)
+    out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+    ws = shared_workspace(B, c.cfg, 70, len(lens), sum(new))
+    call(B, c, "shared", q, ints(offsets(new)), ints(lens), ints(first), ints(prefix), out, ws, faults=faults)
+    assert int(faults[0]) == 0
+    check_shared(B, c, q, out, lens, new, prefix, lists[::9] + lists[-1:], dtype, False)
+
+
+@pytest.mark.parametrize("form", FORMS)
+def test_pools_beyond_32_bits(B, form):  # noqa: F811
+    """Pages that begin 3 GiB apart: append, read, extend, decode and shared attention."""
+    import torch
+    gen, page, far, dim = generator(41), 16, 3 << 30, 64
+    row = dim if form == "f8" else dim // 2
+    cfg = B.make_kv_config("bf16", 4, 2, dim)
+    pools, scales = [torch.empty(2 * far + page * 2 * row, dtype=torch.uint8, device=DEV) for _ in range(2)], []
+    unit = 32 if form == "f8" else 16
+    views = [p.as_strided((3, page, 2, row), (far, 2 * row, row, 1)) for p in pools]
+    for _ in range(2):
+        s = torch.empty(2 * far // unit + page * 4, dtype=torch.uint8, device=DEV)
+        scales.append(s.as_strided((3, page, 2, 2), (far // unit, 2 * row // unit, row // unit, 1)))
+    cache = B.pack_kvq_cache(cfg, form, *views, *scales, ints([[2, 0, 1], [2, 1, 0]]))
+    k, v, q = rand(gen, "bf16", 40, 2, dim), rand(gen, "bf16", 40, 2, dim), rand(gen, "bf16", 40, 4, dim)
+    B.flame_kvq_append(cfg, cache, k, v, ints([0, 40]), ints([40]))
+    rk, rv = torch.empty_like(k), torch.empty_like(v)
+    B.flame_kvq_read(cfg, cache, ints([0, 40]), ints([40]), rk, rv)
+    assert np.array_equal(host(rk), kv_oracle.quantise(host(k), form, "bf16")[2]) and np.array_equal(host(rv), kv_oracle.quantise(host(v), form, "bf16")[2])
+    out = torch.empty_like(q)
+    B.flame_kvq_extend(cfg, cache, q, ints([0, 40]), ints([40]), out, workspace_for(B, cfg, 1, 40))
+    check_attention(host(out), host(q), host(rk), host(rv), "bf16")
+    single = torch.empty_like(q[:1])
+    B.flame_kvq_decode(cfg, cache, q[:1], ints([40]), single, workspace_for(B, cfg, 1))
+    check_attention(host(single), host(q[:1]), host(rk), host(rv), "bf16")
+    two = torch.empty_like(q[:2])                                       # the second leaves the first one's page 2 for page 1, which holds tokens 32..39
+    B.flame_kvq_shared(cfg, cache, q[:2], None, ints([40, 24]), ints([0, 2]), ints([16, 16]), two, shared_workspace(B, cfg, 1, 2))
+    check_attention(host(two[:1]), host(q[:1]), host(rk), host(rv), "bf16")
+    rows = list(range(16)) + list(range(32, 40))
+    check_attention(host(two[1:]), host(q[1:2]), host(rk)[rows], host(rv)[rows], "bf16")
+
+
+@pytest.mark.parametrize("form", [None, "f8"])
+@pytest.mark.parametrize("n_seqs", [5, 90])
+def test_padded_batches_and_wrong_offsets(B, form, n_seqs):  # noqa: F811
+    """Rows ahead of the first sequence and behind the last are left as they are; offsets that are none make no access out of range and are reported, and of up to 64 sequences those before them
+    have their results, by every call."""
+    import torch
+    gen = generator(n_seqs)
+    groups = [(70, [(71 + i, 1 + i % 3, None) for i in range(2)]), (40, [(45 + i, 2, None) for i in range(n_seqs - 2)])]
+    c, lens, new, prefix, lists, first = shared_case(B, gen, form, "bf16", 4, 2, 64, groups, tokens=2048)
+    off = 3 + offsets(new)
+    n = int(off[-1]) + 4
+    q = rand(gen, "bf16", n, 4, 64)
+    pools = c.pools()
+
+    def run(off):
+        out, faults = torch.full_like(q, 7.0), torch.zeros(1, dtype=torch.int32, device=DEV)
+        call(B, c, "shared", q, ints(off), ints(lens), ints(first), ints(prefix), out, shared_workspace(B, c.cfg, 2, n_seqs, n), faults=faults)
+        return out, int(faults[0])
+
+    def check(out, off, b):
+        s = slice(off[b], off[b + 1])
+        check_attention(host(out[s]), host(q[s]), *c.rows(b, lens[b], prefix[b], 0 if b < 2 else 2, pools), "bf16", what=b)
+
+    out, fault = run(off)
+    assert fault == 0 and bool((out[:3] == 7.0).all()) and bool((out[-4:] == 7.0).all())
+    for b in (0, 1, 2, n_seqs - 1):
+        check(out, off, b)
+    for at, value in ((3, 4), (3, -1), (n_seqs, 1 << 30), (1, -(1 << 31)), (n_seqs, -7), (0, -2), (2, 1 << 30)):
+        wrong = off.copy()
+        wrong[at] = value
+        out, fault = run(wrong)
+        assert fault & 4, (at, value)
+        if n_seqs <= 64:
+            bad = next((b for b in range(n_seqs) if wrong[b] < 0 or wrong[b + 1] < wrong[b]), n_seqs)
+            for b in range(bad):
+                if wrong[b + 1] <= n:
+                    check(out, wrong, b) if wrong[b + 1] - wrong[b] == new[b] else None
+            after = int(max(wrong[:bad + 1].max(), 0)) if bad else 0
+            assert bool((out[after:] == 7.0).all()), (at, value)
+    if form == "f8":
+        rk, rv = (torch.full((n, 2, 64), 7.0, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+        B.flame_kvq_read(c.cfg, c.packed, ints(off), ints(np.minimum(lens, 16)), rk, rv)
+        assert bool((rk[:3] == 7.0).all()) and bool((rk[-4:] == 7.0).all())
+        for b in (0, 2):                                                # (of groups' first sequences the rows of the table name the first tokens too)
+            page = c.table_host[b, 0]
+            t = np.arange(min(lens[b], 16) - new[b], min(lens[b], 16))
+            assert np.array_equal(host(rk)[off[b]:off[b + 1]], pools[0][page, t])
+
+
+def test_append_far_positions(B):  # noqa: F811
+    """A cache that spans 2^31 - 2^16 positions over a few pages: keys and queries there, by the same angles as in the cache of the element type."""
+    import torch
+    gen, page, width = generator(51), 65536, 32767
+    cfg = B.make_kv_config("f32", 2, 1, 64)
+    pool = B.make_kvq_pool(cfg, "f8", 2, page)
+    cache = B.pack_kvq_cache(cfg, "f8", *pool, torch.ones(2, width, dtype=torch.int32, device=DEV))
+    lens = np.array([page * width, (1 << 30) + 12345], np.int64)
+    q, k = rand(gen, "f32", 4, 2, 64), rand(gen, "f32", 4, 1, 64)
+    f = B.flame_kv_rotation_frequencies(64)
+    out = torch.empty_like(q)
+    B.flame_kvq_append(cfg, cache, k, k, ints([0, 2, 4]), ints(lens), q=q, q_out=out, rotation=B.make_kv_rotation(f))
+    plain = B.pack_kv_cache(cfg, torch.zeros(2, page, 1, 64, device=DEV), torch.zeros(2, page, 1, 64, device=DEV), torch.ones(2, width, dtype=torch.int32, device=DEV))
+    want = torch.empty_like(q)
+    B.flame_kv_append(cfg, plain, k, k, ints([0, 2, 4]), ints(lens), q=q, q_out=want, rotation=B.make_kv_rotation(f))
+    position = np.concatenate([[x - 2, x - 1] for x in lens])
+    turned = kv_oracle.rotate(host(q), position, f, False)
+    assert np.abs(host(out) - turned).max() <= 2.0 ** -24 * np.abs(turned).max() + 2 * np.abs(host(q)).max() * 2.0 ** -21
+    assert np.abs(host(out) - host(want)).max() <= 2 * (2.0 ** -24 * np.abs(turned).max() + 2 * np.abs(host(q)).max() * 2.0 ** -21)
+    back_k, back_v = torch.empty_like(k), torch.empty_like(k)
+    B.flame_kvq_read(cfg, cache, ints([0, 2, 4]), ints(lens), back_k, back_v)
+    assert np.array_equal(host(back_v), kv_oracle.quantise(host(k), "f8", "f32")[2])
+    key = kv_oracle.rotate(host(k), position, f, False)
+    assert (np.abs(host(back_k) - key) <= 2.0 ** -4 * np.abs(key) + 2.0 ** -9 * np.abs(key).max() / 464 + 2 * np.abs(host(k)).max() * 2.0 ** -21 * (1 + 2.0 ** -4)).all()
+
+
+def test_two_graphs_with_one_workspace(B):  # noqa: F811
+    """Graphs of a shared and of a decoding call that use the same workspace, replayed in turn with eager calls between them, lengths changing on the device."""
+    import torch
+    gen = generator(61)
+    c, lens, new, prefix, lists, first = shared_case(B, gen, "f8", "bf16", 8, 2, 64, [(1500, [(1501 + 9 * i, 1, None) for i in range(6)])], tokens=2048)
+    q, one = rand(gen, "bf16", 6, 8, 64), rand(gen, "bf16", 1, 8, 64)
+    ws = shared_workspace(B, c.cfg, 1, 6)
+    assert ws.numel() >= B.flame_kv_workspace_bytes(c.cfg, 1)
+    lens_t, first_t, prefix_t = ints(lens), ints(first), ints(prefix)
+    out, single = torch.empty_like(q), torch.empty_like(one)
+
+    def both():
+        call(B, c, "shared", q, None, lens_t, first_t, prefix_t, out, ws)
+
+    def decode():
+        B.flame_kvq_decode(c.cfg, c.packed, one, lens_t[:1], single, ws)
+
+    both(), decode()
+    graphs = []
+    for f in (both, decode):
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            f()
+        graphs.append(g)
+    for i in range(4):
+        now = [n - 5 * i for n in lens]
+        lens_t.copy_(ints(now))
+        prefix_t.copy_(ints([max(0, p - 300 * i) if b else p for b, p in enumerate(prefix)]))
+        q.copy_(rand(gen, "bf16", 6, 8, 64)), one.copy_(rand(gen, "bf16", 1, 8, 64))
+        graphs[0].replay(), graphs[1].replay()
+        torch.cuda.synchronize()
+        got, alone = out.clone(), single.clone()
+        ws.fill_(255), out.zero_(), single.zero_()
+        both(), decode()
+        torch.cuda.synchronize()
+        assert torch.equal(out, got) and torch.equal(single, alone)
+        pools = c.pools()
+        check_attention(host(alone), host(one), *c.rows(0, now[0], pools=pools), "bf16", what=i)
+        if i == 0:
+            for b in range(6):
+                check_attention(host(got[b:b + 1]), host(q[b:b + 1]), *c.rows(b, now[b], prefix[b], 0, pools), "bf16", what=(i, b))
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+@pytest.mark.parametrize("shared", [False, True])
+def test_few_rows_do_not_feel_what_they_do_not_see(B, form, dtype, dim, shared):  # noqa: F811
+    """A few new rows over a cache with room for many tokens (split over the keys): a NaN block among the newest tokens is seen by the rows from its token on, in its 32 features of the values."""
+    import torch
+    gen = generator(5 + dim)
+    lens, new = [200, 90, 12], [11, 3, 12]
+    c = Cache(B, gen, form, dtype, 4, 2, dim, lens, 16, tokens=4096)
+    off = ints(offsets(new))
+    q = rand(gen, dtype, 26, 4, dim)
+    clean, dirty = torch.empty_like(q), torch.empty_like(q)
+
+    def run(out):
+        if shared:
+            B.flame_kvq_shared(c.cfg, c.packed, q, off, ints(lens), ints([0, 1, 2, 3]), ints([150, 40, 0]), out, shared_workspace(B, c.cfg, 3, 3, 26))
+        else:
+            B.flame_kvq_extend(c.cfg, c.packed, q, off, ints(lens), out, workspace_for(B, c.cfg, 3, 26))
+
+    run(clean)
+    pools = c.pools()
+    for b, (n, m) in enumerate(zip(lens, new)):
+        s = slice(sum(new[:b]), sum(new[:b + 1]))
+        check_attention(host(clean[s]), host(q[s]), *c.rows(b, n, pools=pools), dtype, what=b)
+    for at in (189, 190, 195, 199):
+        page, slot, row = c.table_host[0, at // 16], at % 16, at - 189
+        for block in range(dim // 32):
+            for scales, where in ((c.vs, "v"), (c.ks, "k")):
+                was = int(scales[page, slot, 1, block])
+                scales[page, slot, 1, block] = 255
+                run(dirty)
+                scales[page, slot, 1, block] = was
+                assert torch.equal(dirty[:row], clean[:row]) and torch.equal(dirty[11:], clean[11:]) and torch.equal(dirty[:, :2], clean[:, :2]), (at, where)
+                mine = slice(32 * block, 32 * block + 32) if where == "v" else slice(0, dim)
+                assert bool(dirty[row:11, 2:, mine].isnan().all())
+                others = [i for i in range(dim) if not mine.start <= i < mine.stop]
+                assert torch.equal(dirty[:, :, others], clean[:, :, others])

@@ -152,3 +152,52 @@ def test_unpacked_codes():
     assert np.array_equal(kv_oracle.unpack(pool, "f8"), pool)
     codes = kv_oracle.unpack(pool, "f4")
     assert codes.shape == (1, 512) and (codes[0, 0::2] == np.arange(256) % 16).all() and (codes[0, 1::2] == np.arange(256) // 16).all()
+
+
+class Route(C.Structure):
+    _fields_ = [("split", C.c_bool), ("wavefronts", C.c_int32), ("splits", C.c_int32), ("workspace", C.c_int64)]
+
+
+class SharedRoute(C.Structure):
+    _fields_ = [("wavefronts", C.c_int32), ("splits", C.c_int32), ("budget", C.c_int32), ("slots", C.c_int64), ("part_rows", C.c_int64), ("cuts_at", C.c_int64), ("own_at", C.c_int64),
+                ("split_at", C.c_int64), ("workspace", C.c_int64)]
+
+
+# KvRoute kvq_route(const flame_kv_config &, int32_t n_seqs, int64_t n_rows, bool decode, int64_t capacity) and
+# KvSharedRoute kv_shared_route(const flame_kv_config &, int32_t n_groups, int64_t n_rows, int64_t capacity) of csrc/kv.h
+kvq_route = B._lib["_ZN5flame9kvq_routeERK15flame_kv_configilbl"]
+kvq_route.restype, kvq_route.argtypes = Route, [C.POINTER(B.flame_kv_config), C.c_int32, C.c_int64, C.c_bool, C.c_int64]
+kv_shared_route = B._lib["_ZN5flame15kv_shared_routeERK15flame_kv_configill"]
+kv_shared_route.restype, kv_shared_route.argtypes = SharedRoute, [C.POINTER(B.flame_kv_config), C.c_int32, C.c_int64, C.c_int64]
+ROOM = [1, 1023, 1024, 1025, 5000, 16384, 1 << 20, (1 << 31) - 65536]
+SHAPES = [("bf16", 32, 8, 128), ("f16", 8, 2, 64), ("f32", 32, 8, 128), ("bf16", 1, 1, 32), ("f32", 6, 2, 64), ("f16", 40, 1, 32), ("bf16", 400, 400, 64), ("f32", 4096, 1, 128)]
+
+
+@pytest.mark.parametrize("dtype,hq,hkv,dim", SHAPES)
+def test_a_workspace_serves_every_smaller_batch(dtype, hq, hkv, dim):
+    cfg, rng = B.make_kv_config(dtype, hq, hkv, dim), np.random.default_rng(hq)
+    most = [min(1 << 22, ((1 << 23) - 1) // hq), min((1 << 25) // hq, (1 << 24) - 1)]
+    counts = [sorted({min(n, m) for n in [1, 2, 5, 8, 16, 33, 64, 65, 128, 129, 200, 400, 401, 1000, 4096, 1 << 17, m] + rng.integers(1, 3000, 8).tolist()}) for m in most]
+    needed, held, shared = {}, {}, {}
+    for s in counts[0]:
+        for t in counts[1]:
+            needed[s, t] = max(kvq_route(cfg, s, t, False, c).workspace for c in ROOM)
+            held[s, t] = B.flame_kv_workspace_bytes(cfg, s, t)
+    for t in counts[1]:
+        shared[t] = 0
+        for g in [0] + counts[0]:
+            for c in ROOM:
+                r = kv_shared_route(cfg, g, t, c)
+                rows = 128 // r.wavefronts
+                assert r.slots * hkv * max(r.splits, 1) < 1 << 32 and r.part_rows >= (0 if g == 0 else t * hq)
+                # the parts that the row tiles may leave: of equal length as many as there are slots, else a plane for each of `splits`
+                if g:
+                    assert r.part_rows >= (r.slots * hkv * rows if r.splits == 0 else r.splits * t * hq)
+                    assert r.slots >= t * (hq // hkv) // rows + g and (r.splits or (g <= 64 and 1 <= r.budget <= r.slots))
+                assert r.cuts_at >= r.part_rows * (dim + 2) * 4 and r.own_at >= r.cuts_at + 512 and r.split_at >= r.own_at + t * hq * (dim + 2) * 4 and r.split_at % 16 == r.own_at % 16 == 0
+                shared[t] = max(shared[t], r.workspace)
+    for s_most in counts[0]:
+        for t_most in counts[1]:
+            assert held[s_most, t_most] >= max(needed[s, t] for s, t in needed if s <= s_most and t <= t_most), (s_most, t_most)
+    for t_most in counts[1]:
+        assert B.flame_kv_shared_workspace_bytes(cfg, 1, 1, t_most) >= max(n for t, n in shared.items() if t <= t_most), t_most
