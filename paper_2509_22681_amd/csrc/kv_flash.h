@@ -148,12 +148,18 @@ struct FlashCut {
   int parts, before;     // of a row tile of the lane's group; slots of the groups ahead of it
   int chunk;
 };
-__device__ __forceinline__ int flash_wave_sum(int v) {
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) v += __shfl_xor(v, i);
+template <int CTRL, int ROWS = 0xf> __device__ __forceinline__ int flash_dpp(int v) { return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false); }
+__device__ __forceinline__ int flash_scan(int v) {               // inclusive sums over the wavefront
+  v += flash_dpp<0x111>(v);                                      // row_shr:1, 2, 4, 8
+  v += flash_dpp<0x112>(v);
+  v += flash_dpp<0x114>(v);
+  v += flash_dpp<0x118>(v);
+  v += flash_dpp<0x142, 0xa>(v);                                 // the last lane of a row to the next row
+  v += flash_dpp<0x143, 0xc>(v);                                 // lane 31 to the upper half
   return v;
 }
-__device__ __forceinline__ FlashCut flash_cut(int tiles, int keys, int budget, int lane) {
+__device__ __forceinline__ int flash_wave_sum(int v) { return __builtin_amdgcn_readlane(flash_scan(v), 63); }
+__device__ __forceinline__ FlashCut flash_cut(int tiles, int keys, int budget) {
   if (keys == 0) tiles = 0;
   const int work = flash_wave_sum((int)min((int64_t)tiles * keys, (int64_t)1 << 24)), rows = flash_wave_sum(tiles);
   FlashCut c{0, 0, max(kSharedTiles, (work + budget - 1) / max(budget, 1))};
@@ -164,13 +170,7 @@ __device__ __forceinline__ FlashCut flash_cut(int tiles, int keys, int budget, i
     if (all <= budget || all == rows) break;
     c.chunk += max(1, c.chunk / 16);
   }
-  int sums = tiles * c.parts;
-#pragma unroll
-  for (int i = 1; i < 64; i <<= 1) {
-    const int other = __shfl_up(sums, i);
-    sums += lane >= i ? other : 0;
-  }
-  c.before = sums - tiles * c.parts;
+  c.before = flash_scan(tiles * c.parts) - tiles * c.parts;
   return c;
 }
 
@@ -247,7 +247,7 @@ __device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_blo
     if (wrong && lane >= __builtin_ctzll(wrong)) tiles = 0;
     int before = 0;
     if (balanced) {
-      even = flash_cut((int)tiles, (max(keys, 0) + KW - 1) / KW, a.budget, lane);
+      even = flash_cut((int)tiles, (max(keys, 0) + KW - 1) / KW, a.budget);
       if (my_block == 0 && threadIdx.x < 64) a.cuts[lane] = int2{even.before, even.parts};
       before = even.before;
       tiles *= even.parts;
@@ -342,14 +342,18 @@ __device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_blo
     const FlashGroup s = flash_group(a, seq, n_seqs);
     table = a.pages.table + s.b0 * a.pages.table_stride;
     sees = flash_shared_seen(a, s, first + my_row() / group, n);
-    wave_least = wave_most = sees;
-#pragma unroll
-    for (int i = 1; i < 32; i <<= 1) {
-      wave_least = min(wave_least, __shfl_xor(wave_least, i));
-      wave_most = max(wave_most, __shfl_xor(wave_most, i));
-    }
-    wave_least = active ? __builtin_amdgcn_readfirstlane(wave_least) : 0;
-    wave_most = active ? __builtin_amdgcn_readfirstlane(wave_most) : 0;
+    // over the 32 rows, which both halves of the wavefront have: rotations within 16 lanes, and the two rows of lanes
+    int least = sees, most = sees;
+    least = min(least, flash_dpp<0x121>(least));
+    most = max(most, flash_dpp<0x121>(most));
+    least = min(least, flash_dpp<0x122>(least));
+    most = max(most, flash_dpp<0x122>(most));
+    least = min(least, flash_dpp<0x124>(least));
+    most = max(most, flash_dpp<0x124>(most));
+    least = min(least, flash_dpp<0x128>(least));
+    most = max(most, flash_dpp<0x128>(most));
+    wave_least = active ? min(__builtin_amdgcn_readlane(least, 0), __builtin_amdgcn_readlane(least, 16)) : 0;
+    wave_most = active ? max(__builtin_amdgcn_readlane(most, 0), __builtin_amdgcn_readlane(most, 16)) : 0;
   } else {
     sees = seen_by(my_row());
     wave_least = active ? seen_by(wave_row) : 0;

@@ -110,8 +110,8 @@ __device__ __forceinline__ Token find_tokens(const KvBatch &batch, const KvPages
   bool open = lane < count && row < batch.n_rows;
   int seq = 0;
   int64_t first = 0, end = 0;
-  // From the first token's sequence on, a lane holds one sequence of 64: lane i looks among them for the first one that ends behind its token, ahead of offsets that are none.
-  for (int s0 = kv_find_sequence(batch.offsets, batch.n_seqs, row0, lane); s0 < batch.n_seqs; s0 += 64) {
+  // From the first token's sequence on (of up to 64 from the first one), a lane holds one sequence of 64: lane i looks among them for the first one that ends behind its token, ahead of offsets that are none.
+  for (int s0 = batch.n_seqs <= 64 ? 0 : kv_find_sequence(batch.offsets, batch.n_seqs, row0, lane); s0 < batch.n_seqs; s0 += 64) {
     int b = 0, e = 0;
     if (s0 + lane < batch.n_seqs) {
       b = batch.offsets[s0 + lane];
