@@ -142,8 +142,10 @@ __device__ __forceinline__ int flash_shared_seen(const KvAttention &a, const Fla
 }
 
 // How the keys of shared histories are cut where there is room for `budget` workgroups a key head: lane g holds group g (of up to 64), whose `tiles` row tiles have `keys` key tiles each.  All parts have the same
-// number of key tiles, the least (of at least kSharedTiles) with which they are no more than the budget; the last one of a row tile may be shorter.
-constexpr int kSharedTiles = 2;
+// number of key tiles, the least (of at least kSharedTiles) with which they are no more than the budget; the last one of a row tile may be shorter.  Half the budget does where parts would be of less than
+// `long_part` key tiles: one workgroup on a compute unit reads as fast as two, and leaves half as many parts.  us with 512 | 256 workgroups, bf16, 32/8 heads of 128, single tokens: 16 sequences over 16384
+// shared tokens 43 | 33, 32 over 8000 41 | 29, 128 over 32000 124 | 162; 400, 16/16 heads of 32, in 4 groups over 4000-10000 51 | 66
+constexpr int kSharedTiles = 2, kLongPart = 8;
 struct FlashCut {
   int parts, before;     // of a row tile of the lane's group; slots of the groups ahead of it
   int chunk;
@@ -159,9 +161,10 @@ __device__ __forceinline__ int flash_scan(int v) {               // inclusive su
   return v;
 }
 __device__ __forceinline__ int flash_wave_sum(int v) { return __builtin_amdgcn_readlane(flash_scan(v), 63); }
-__device__ __forceinline__ FlashCut flash_cut(int tiles, int keys, int budget) {
+__device__ __forceinline__ FlashCut flash_cut(int tiles, int keys, int budget, int long_part) {
   if (keys == 0) tiles = 0;
   const int work = flash_wave_sum((int)min((int64_t)tiles * keys, (int64_t)1 << 24)), rows = flash_wave_sum(tiles);
+  budget = max((budget + 1) / 2, min(budget, work / long_part));
   FlashCut c{0, 0, max(kSharedTiles, (work + budget - 1) / max(budget, 1))};
   // (each step adds a sixteenth: from the least that could do to a part for each row tile there are fewer than 200)
   for (;;) {
@@ -247,7 +250,7 @@ __device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_blo
     if (wrong && lane >= __builtin_ctzll(wrong)) tiles = 0;
     int before = 0;
     if (balanced) {
-      even = flash_cut((int)tiles, (max(keys, 0) + KW - 1) / KW, a.budget);
+      even = flash_cut((int)tiles, (max(keys, 0) + KW - 1) / KW, a.budget, kLongPart * KP);
       if (my_block == 0 && threadIdx.x < 64) a.cuts[lane] = int2{even.before, even.parts};
       before = even.before;
       tiles *= even.parts;
