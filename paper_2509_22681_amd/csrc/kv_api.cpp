@@ -291,10 +291,11 @@ KvRoute kvq_route(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows, bool
 
 // The histories' rows are those of whole groups.
 KvSharedRoute kv_shared_route(const flame_kv_config &c, int32_t n_groups, int64_t n_rows, int64_t capacity) {
-  const bool wide = c.dtype == FLAME_KV_F32 && c.head_dim == 128;
   const int64_t group = c.n_q_heads / c.n_kv_heads, heads = n_rows * c.n_q_heads, rows = n_rows * group / std::max(n_groups, 1);
   KvSharedRoute r{};
-  r.wavefronts = rows <= 32 && !wide ? 4 : rows <= 64 ? 2 : 1;
+  // Wavefronts that share 32 rows.  Four of 128 features fill a compute unit's LDS with one workgroup: us with four | two, bf16 (f8), 32/8 heads: 8 sequences over 16384 shared tokens 39 | 31 (35 | 29), 4 groups of
+  // 4 over 4000-8000 47 | 46 (39 | 36).  Two | one for 64 rows: 16 over 16384 34 | 35 (31 | 33), 8 groups of 12 over 2000-12000 112 | 118
+  r.wavefronts = rows <= 32 && c.head_dim < 128 ? 4 : rows <= 64 ? 2 : 1;
   r.splits = 1;
   const int64_t tile = kFlashRows / r.wavefronts;
   r.slots = n_rows * group / tile + n_groups;

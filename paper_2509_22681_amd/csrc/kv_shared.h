@@ -118,6 +118,7 @@ template <int FORM> hipError_t launch_shared(const KvAttention &call, const KvSh
   flash_with_shape(call, route.wavefronts, [&](auto t, auto width, auto kp) {
     using T = decltype(t);
     constexpr int DH = decltype(width)::value, KP = decltype(kp)::value, kBytes = flash_lds_bytes<T, DH, KP>();
+    if constexpr (DH < 128 || KP < 4) {                           // (kv_shared_route)
     static std::atomic<uint64_t> raised{0};
     e = raise_lds_limit(reinterpret_cast<const void *>(&kv_shared_kernel<T, DH, KP, FORM>), kBytes, raised);
     if (e != hipSuccess) return;
@@ -127,6 +128,7 @@ template <int FORM> hipError_t launch_shared(const KvAttention &call, const KvSh
     kv_shared_kernel<T, DH, KP, FORM><<<(unsigned)(a.split_blocks + tiles), 256, kBytes, stream>>>(a, (float *)split_workspace);
     kv_shared_join_kernel<T, DH, KP><<<(unsigned)(a.batch.n_rows * ((a.n_q_heads * (DH / 4) + 255) / 256)), 256, 0, stream>>>(a, (const float *)split_workspace);
     e = hipGetLastError();
+    }
   });
   return e;
 }
