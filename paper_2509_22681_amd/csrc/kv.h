@@ -88,7 +88,7 @@ hipError_t launch_kv_shared_plain(const KvAttention &a, const KvSharedRoute &rou
 hipError_t launch_kv_shared_f8(const KvAttention &a, const KvSharedRoute &route, void *split_workspace, hipStream_t stream);
 hipError_t launch_kv_shared_f4(const KvAttention &a, const KvSharedRoute &route, void *split_workspace, hipStream_t stream);
 hipError_t launch_kv_attention(const KvAttention &a, int wavefronts, hipStream_t stream);
-// few query rows: split over the keys (kv_split.hip)
+// few query rows: split over the keys (kv_split.h)
 hipError_t launch_kv_split(const KvAttention &a, void *workspace, hipStream_t stream);
 hipError_t launch_kvq_split(const KvAttention &a, void *workspace, hipStream_t stream);
 int64_t kv_split_workspace_bytes(int32_t head_dim, int64_t rows);   // rows times heads

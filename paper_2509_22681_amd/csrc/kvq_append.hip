@@ -166,8 +166,8 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_append_kernel(KvBatch batch, 
   const int per_row = head_dim / 8, shift = per_row == 4 ? 2 : per_row == 8 ? 3 : 4;      // lanes of a row
   const int at = lane & (per_row - 1), rows = 64 / per_row;
   const int there = t.there, below = t.position < 0;
-  // rows (token, head) of keys and values, then of queries
-  for (int r = 0; r < count * n_kv; r += rows) {
+  // rows (token, head) of keys and values, then of queries; the grid's second dimension shares them
+  for (int r = rows * blockIdx.y; r < count * n_kv; r += rows * gridDim.y) {
     const int mine = r + (lane >> shift), i = mine / n_kv, h = mine - i * n_kv;
     const int64_t page_at = of_lane(t.at, i & 63);
     if (i >= count || page_at < 0) continue;
@@ -180,7 +180,7 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_append_kernel(KvBatch batch, 
   }
   if (!q.p) return;
   // (a row's lanes are of one wavefront, which loads all of them before it stores any: q_out may be q)
-  for (int r = 0; r < count * n_q; r += rows) {
+  for (int r = rows * blockIdx.y; r < count * n_q; r += rows * gridDim.y) {
     const int mine = r + (lane >> shift), i = mine / n_q, h = mine - i * n_q;
     const bool go = __shfl(there, i & 63) && !__shfl(below, i & 63) && i < count;
     if (!go) continue;
@@ -268,10 +268,10 @@ template <typename F> void with_stored(int32_t dtype, int32_t form, int64_t byte
   });
 }
 
-// Tokens of a wavefront: as many as give its lanes `rounds` rows' pieces each, but not so many that few wavefronts are left.
+// Tokens of a wavefront: as many as give its lanes `rounds` rows' pieces each, but not so many that few wavefronts are left (one token each of 48 sequences, 8/2 heads of 64: 8.8 us by wavefronts of four).
 int tokens_of(int64_t n_rows, int lanes_of_token, int rounds, int most) {
   int count = 1;
-  while (count < most && (count * lanes_of_token < 64 || (count * lanes_of_token < 64 * rounds && n_rows / (2 * count) >= 4096))) count *= 2;
+  while (count < most && count * lanes_of_token < 64 * rounds && n_rows / (2 * count) >= (count * lanes_of_token < 64 ? 1024 : 4096)) count *= 2;
   return count;
 }
 unsigned blocks_of(const KvBatch &batch, int count) { return (unsigned)((batch.n_rows + count * kWaves - 1) / (count * kWaves)); }
@@ -281,9 +281,12 @@ unsigned blocks_of(const KvBatch &batch, int count) { return (unsigned)((batch.n
 hipError_t launch_kvq_append(const KvBatch &batch, const KvPages &pages, const KvScales &scales, const KvRows &k, const KvRows &v, const KvRows *q, const KvRows *q_out,
                              const KvRotation &rotation, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, hipStream_t stream) {
   const int count = tokens_of(batch.n_rows, n_kv_heads * head_dim / 8, 1, kAppendTokens);
+  // Few tokens: several wavefronts share the heads of theirs, up to one for each 64 lanes' worth of queries (one token each of 256 sequences, 32/8 heads of 128: 13.2 us with one).
+  int share = 1;
+  while (share * 2 * (64 / (head_dim / 8)) <= count * n_q_heads && batch.n_rows / count * share < 4096) share *= 2;
   const int64_t bytes = batch.n_rows * n_q_heads * head_dim * (dtype == FLAME_KV_F32 ? 4 : 2);
   with_stored(dtype, scales.form, bytes, [&](auto t, auto form, auto past) {
-    kvq_append_kernel<decltype(t), decltype(form)::value, decltype(past)::value><<<blocks_of(batch, count), 64 * kWaves, 0, stream>>>(batch, pages, scales, k, v, q ? *q : KvRows{}, q ? *q_out : KvRows{}, rotation,
+    kvq_append_kernel<decltype(t), decltype(form)::value, decltype(past)::value><<<dim3(blocks_of(batch, count), share), 64 * kWaves, 0, stream>>>(batch, pages, scales, k, v, q ? *q : KvRows{}, q ? *q_out : KvRows{}, rotation,
                                                                                                            n_q_heads, n_kv_heads, head_dim, count);
   });
   return hipGetLastError();
