@@ -24,7 +24,7 @@
 //
 // Over a cache of 8 or 4 bits a thread loads the codes of 16 features at a time into registers, a tile ahead, and when the products of this tile are done it makes the next one's LDS rows of
 // them: what follows is the same.  With shared histories (SHARED) a group of sequences is one sequence, whose rows are those of all of them and whose keys are the history; each row
-// sees as far as its own sequence and position let it, and all results are parts, which kv_shared.hip joins with those of the sequences' own keys.
+// sees as far as its own sequence and position let it, and all results are parts, which kv_shared.h joins with those of the sequences' own keys.
 #pragma once
 #include "kernels.h"
 #include "kv_codec.h"
@@ -98,6 +98,7 @@ template <int KW> __device__ __forceinline__ FlashParts flash_parts(int n_seen, 
   }
   return p;
 }
+
 // Which sequences of the batch have rows: all, or of up to 64 those before the first offsets that are none.
 __device__ __forceinline__ int flash_sequences(const KvAttention &a, int lane) {
   if (!a.batch.offsets || a.batch.n_seqs > 64) return a.batch.n_seqs;
@@ -224,7 +225,7 @@ __device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_blo
   int split = block / a.n_kv_heads % splits;
   FlashCut even{1, 0, 0};
   int seq;
-  int64_t tile, first, end;                                       // tile: counted from the sequence's end
+  int64_t tile, first, end;                                       // tile: counted from the sequence's end (a group's: from its first row)
   int kv_len = 0;
   const int n_spans = SHARED ? a.n_groups : a.batch.n_seqs, n_seqs = SHARED ? flash_sequences(a, lane) : 0;
   if (n_spans <= 64) {
@@ -254,10 +255,11 @@ __device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_blo
       if (my_block == 0 && threadIdx.x < 64) a.cuts[lane] = int2{even.before, even.parts};
       before = even.before;
       tiles *= even.parts;
-    } else
-    for (int j = 0; j < n_spans; ++j) {
-      const int other = __builtin_amdgcn_readlane(keys, j);
-      before += other > keys || (other == keys && j < lane) ? __builtin_amdgcn_readlane((int)tiles, j) : 0;
+    } else {
+      for (int j = 0; j < n_spans; ++j) {
+        const int other = __builtin_amdgcn_readlane(keys, j);
+        before += other > keys || (other == keys && j < lane) ? __builtin_amdgcn_readlane((int)tiles, j) : 0;
+      }
     }
     const uint64_t mine = __builtin_amdgcn_ballot_w64(slot >= before && slot < before + tiles);
     if (!mine) return;

@@ -107,7 +107,8 @@ __device__ __forceinline__ Token find_tokens(const KvBatch &batch, const KvPages
   Token t{0, -1, false};
   if (row0 >= batch.n_rows) return t;
   const int64_t row = row0 + lane;
-  bool open = lane < count && row < batch.n_rows;
+  // (behind the last sequence there is nothing to look for; of up to 64, which are looked at once, offsets that are none may lie behind those that have rows)
+  bool open = lane < count && row < batch.n_rows && (batch.n_seqs <= 64 || row < batch.offsets[batch.n_seqs]);
   int seq = 0;
   int64_t first = 0, end = 0;
   // From the first token's sequence on (of up to 64 from the first one), a lane holds one sequence of 64: lane i looks among them for the first one that ends behind its token, ahead of offsets that are none.

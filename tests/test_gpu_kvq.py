@@ -787,3 +787,41 @@ def test_few_rows_do_not_feel_what_they_do_not_see(B, form, dtype, dim, shared):
                 assert bool(dirty[row:11, 2:, mine].isnan().all())
                 others = [i for i in range(dim) if not mine.start <= i < mine.stop]
                 assert torch.equal(dirty[:, :, others], clean[:, :, others])
+
+
+@pytest.mark.parametrize("form", FORMS)
+@pytest.mark.parametrize("hq,hkv,dim", [(8, 2, 64), (4, 1, 32), (32, 8, 128)])
+def test_batches_padded_with_sequences(B, form, hq, hkv, dim):  # noqa: F811
+    """A batch held ready for 400 sequences of which 150 are there, with empty ones among them and rows behind the last: append, read, decode and shared attention do what they do for those alone."""
+    import torch
+    gen = generator(dim + 1)
+    new = [(1, 0, 2, 1, 0)[i % 5] for i in range(150)] + [0] * 250
+    lens = [m + i % 23 for i, m in enumerate(new[:150])] + [0] * 250
+    c = Cache(B, gen, form, "bf16", hq, hkv, dim, lens, 16)
+    n, off = sum(new), offsets(new)
+    rows = rand(gen, "bf16", n + 70, hq + 2 * hkv, dim)
+    q_out = torch.full((n + 70, hq, dim), 7.0, device=DEV, dtype=torch.bfloat16)
+    faults = torch.zeros(1, dtype=torch.int32, device=DEV)
+    rotation = B.make_kv_rotation(B.flame_kv_rotation_frequencies(dim))
+    B.flame_kvq_append(c.cfg, c.packed, rows[:, hq:hq + hkv], rows[:, hq + hkv:], ints(off), ints(lens), q=rows[:, :hq], q_out=q_out, rotation=rotation, faults=faults)
+    rk, rv = (torch.full((n + 70, hkv, dim), 7.0, device=DEV, dtype=torch.bfloat16) for _ in range(2))
+    B.flame_kvq_read(c.cfg, c.packed, ints(off), ints(lens), rk, rv, faults=faults)
+    assert int(faults[0]) == 0 and bool((q_out[n:] == 7.0).all()) and bool((rk[n:] == 7.0).all())
+    pools = c.pools()
+    seq = np.repeat(np.arange(400), new)
+    position = np.concatenate([np.arange(a - m, a) for a, m in zip(lens, new)])
+    where = c.table_host[seq, position // 16], position % 16
+    assert np.array_equal(host(rv)[:n], kv_oracle.quantise(host(rows[:n, hq + hkv:]), form, "bf16")[2]) and np.array_equal(pools[1][where], host(rv)[:n])
+    assert np.array_equal(pools[0][where], host(rk)[:n])
+    turned = kv_oracle.rotate(host(rows[:n, :hq]), position, B.flame_kv_rotation_frequencies(dim), False)
+    assert np.abs(host(q_out)[:n] - turned).max() <= 2.0 ** -8 * np.abs(turned).max() + 2.0 ** -19 * np.abs(host(rows)).max()
+    # single tokens of all 400, and the same in groups
+    q = rand(gen, "bf16", 400, hq, dim)
+    out, shared = torch.full_like(q, 7.0), torch.full_like(q, 7.0)
+    B.flame_kvq_decode(c.cfg, c.packed, q, ints(lens), out, workspace_for(B, c.cfg, 400), faults=faults)
+    first = list(range(0, 401, 8)) + [400] * 30
+    B.flame_kvq_shared(c.cfg, c.packed, q, None, ints(lens), ints(first), ints([0] * 400), shared, shared_workspace(B, c.cfg, len(first) - 1, 400), faults=faults)
+    assert int(faults[0]) == 0 and not out[150:].any() and not shared[150:].any()
+    for b in range(0, 150, 11):
+        check_attention(host(out[b:b + 1]), host(q[b:b + 1]), *c.rows(b, lens[b], pools=pools), "bf16", what=b)
+        check_attention(host(shared[b:b + 1]), host(q[b:b + 1]), *c.rows(b, lens[b], pools=pools), "bf16", what=b)
