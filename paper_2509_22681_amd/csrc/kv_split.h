@@ -293,6 +293,14 @@ __device__ __forceinline__ void split_units(const KvAttention &a, float *__restr
       const int key = min(t * KT + (lane & (KT - 1)), s.n - 1);
       return key < 0 ? -1 : kv_token_offset(a.pages, table, (uint32_t)key + (SHARED ? s.skip : 0));
     };
+    // The same in two steps: which page, and, once that is there, where.
+    struct Page { int32_t page; uint32_t slot; };
+    auto page_of = [&](int t) -> Page {
+      const int key = min(t * KT + (lane & (KT - 1)), s.n - 1);
+      const uint32_t token = (uint32_t)max(key, 0) + (SHARED ? s.skip : 0), i = kv_page_index(a.pages, token);
+      return Page{table[i], token - i * (uint32_t)a.pages.page_size};
+    };
+    auto place_of = [&](const Page &p) -> int64_t { return (uint32_t)p.page < (uint32_t)a.pages.n_pages ? p.page * a.pages.page + (int64_t)p.slot * a.pages.slot : -1; };
     struct Values {
       word4 k[KB][KS];
       uint32_t v[VK][VW];
@@ -531,6 +539,29 @@ __device__ __forceinline__ void split_units(const KvAttention &a, float *__restr
     };
     if (s.n > 0) {
       Tile x, y;
+      if constexpr (FORM != kPlain) {
+        // Loads return in order: a page that is asked for ahead of a tile's loads is known while those are still on their way, and the next tile's can follow them.
+        Page next = page_of(t0);
+        Page after = page_of(min(t0 + 1, t1 - 1));
+        request(x, t0, place_of(next));
+        next = after;
+#pragma unroll 1
+        for (int t = t0; t < t1; t += 2) {
+          after = page_of(min(t + 2, t1 - 1));
+          __builtin_amdgcn_sched_barrier(0);
+          request(y, min(t + 1, t1 - 1), place_of(next));
+          __builtin_amdgcn_sched_barrier(0);
+          add(x, t);
+          __builtin_amdgcn_sched_barrier(0);
+          if (t + 1 >= t1) break;
+          next = page_of(min(t + 3, t1 - 1));
+          __builtin_amdgcn_sched_barrier(0);
+          request(x, min(t + 2, t1 - 1), place_of(after));
+          __builtin_amdgcn_sched_barrier(0);
+          add(y, t + 1);
+          __builtin_amdgcn_sched_barrier(0);
+        }
+      } else {
       request(x, t0, look_up(t0));
       int64_t next = look_up(min(t0 + 1, t1 - 1));
 #pragma unroll 1
@@ -546,6 +577,7 @@ __device__ __forceinline__ void split_units(const KvAttention &a, float *__restr
         __builtin_amdgcn_sched_barrier(0);
         add(y, t + 1);
         __builtin_amdgcn_sched_barrier(0);
+      }
       }
     }
     l = split_sum(l);
