@@ -105,11 +105,13 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, cons
     const float2 ml = kv_own_state(a)[from];
     add(ml.x, ml.y, *(const f32x4 *)(a.own + from * DH + f));
   }
-  const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
+  // A row whose logits are all -infinity has zeros, though its weights of zero may have met infinite values or NaN among its own keys.  (NaN logits leave l NaN.)
+  const bool nothing = m == -INFINITY && l == 0.f;
+  const float inv = 1.f / l;
   typedef T out4 __attribute__((ext_vector_type(4)));
   out4 y;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) y[i] = kv_round<T>(o[i] * inv);
+  for (int i = 0; i < 4; ++i) y[i] = kv_round<T>(nothing ? 0.f : o[i] * inv);
   *(out4 *)(a.out.p + q_row * a.out.row + head * a.out.head + f * sizeof(T)) = y;
 }
 

@@ -825,3 +825,28 @@ def test_batches_padded_with_sequences(B, form, hq, hkv, dim):  # noqa: F811
     for b in range(0, 150, 11):
         check_attention(host(out[b:b + 1]), host(q[b:b + 1]), *c.rows(b, lens[b], pools=pools), "bf16", what=b)
         check_attention(host(shared[b:b + 1]), host(q[b:b + 1]), *c.rows(b, lens[b], pools=pools), "bf16", what=b)
+
+
+@pytest.mark.parametrize("form", [None, "f8", "f4"])
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+def test_shared_rows_without_a_logit_above_minus_infinity(B, form, dtype, dim):  # noqa: F811
+    """Every logit is -infinity: zeros whatever the values hold, over the history and over own tokens, few (one part) and many (several); codes, of which none is infinite, take the
+    infinity from the queries."""
+    import torch
+    gen = generator(dim)
+    groups = [(600, [(601, 1, None), (604, 3, None), (2100, 2, None), (600, 40, None)]), (0, [(9, 1, None), (900, 5, None)])]
+    for tokens in (0, 4096):
+        c, lens, new, prefix, lists, first = shared_case(B, gen, form, dtype, 4, 2, dim, groups, tokens=tokens)
+        if form is None:
+            c.k[..., 0] = -math.inf
+            c.v[..., 3], c.v[..., 4], c.v[..., dim - 1] = math.inf, math.nan, -math.inf
+        else:
+            c.k[..., 0] = 0xb8 if form == "f8" else c.k[..., 0] & 0xf0 | 0x0a       # -1
+            c.vs[..., 0] = 255
+        for single in (True, False):
+            q = torch.zeros(len(lens) if single else sum(new), 4, dim, device=DEV, dtype=torch_type(dtype))
+            q[..., 0] = 1.0 if form is None else math.inf
+            out = torch.full_like(q, 7.0)
+            call(B, c, "shared", q, None if single else ints(offsets(new)), ints(lens), ints(first), ints(prefix), out, shared_workspace(B, c.cfg, len(first) - 1, len(lens), len(q)))
+            assert not bool(out.any()), (tokens, single, [b for b, x in enumerate(out.flatten(1).any(1).tolist()) if x])
