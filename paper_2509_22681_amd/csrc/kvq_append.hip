@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_append_kernel(KvBatch batch, 
   __builtin_amdgcn_wave_barrier();
   const int per_row = head_dim / 8, shift = per_row == 4 ? 2 : per_row == 8 ? 3 : 4;      // lanes of a row
   const int at = lane & (per_row - 1), rows = 64 / per_row;
-  const int there = t.there, below = t.position < 0;
+  const int written = t.there && t.position >= 0;                 // the token's query
   // rows (token, head) of keys and values, then of queries; the grid's second dimension shares them
   for (int r = rows * blockIdx.y; r < count * n_kv; r += rows * gridDim.y) {
     const int mine = r + (lane >> shift), i = mine / n_kv, h = mine - i * n_kv;
@@ -183,8 +183,8 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_append_kernel(KvBatch batch, 
   // (a row's lanes are of one wavefront, which loads all of them before it stores any: q_out may be q)
   for (int r = rows * blockIdx.y; r < count * n_q; r += rows * gridDim.y) {
     const int mine = r + (lane >> shift), i = mine / n_q, h = mine - i * n_q;
-    const bool go = __shfl(there, i & 63) && !__shfl(below, i & 63) && i < count;
-    if (!go) continue;
+    const int go = __shfl(written, i & 63);                       // (by all lanes: one that is switched off has nothing to be read from it)
+    if (!go || i >= count) continue;
     const int64_t row = row0 + i;
     float x[8];
     load_turned<T>(q.p + row * q.row + h * q.head, at, rot, turn_s[wave][i], x);

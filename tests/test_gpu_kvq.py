@@ -850,3 +850,73 @@ def test_shared_rows_without_a_logit_above_minus_infinity(B, form, dtype, dim): 
             out = torch.full_like(q, 7.0)
             call(B, c, "shared", q, None if single else ints(offsets(new)), ints(lens), ints(first), ints(prefix), out, shared_workspace(B, c.cfg, len(first) - 1, len(lens), len(q)))
             assert not bool(out.any()), (tokens, single, [b for b, x in enumerate(out.flatten(1).any(1).tolist()) if x])
+
+
+MANY_ROWS = [("f8", "bf16", 2, 1, 32, 32, 130, 2101, 1), ("f4", "f16", 6, 3, 32, 0, 70, 4203, 3), ("f8", "f32", 3, 3, 64, 0, 200, 8301, 2), ("f4", "bf16", 5, 5, 32, 16, 300, 70001, 1),
+             ("f8", "f16", 4, 1, 32, 0, 1000, 140001, 3), ("f4", "f32", 1, 1, 32, 0, 129, 66001, 0), ("f8", "bf16", 1, 1, 32, 0, 64, 270001, 2), ("f8", "f32", 8, 2, 128, 64, 17, 20003, 5)]
+
+
+@pytest.mark.parametrize("form,dtype,hq,hkv,dim,rot,n_seqs,n,ahead", MANY_ROWS)
+def test_append_and_read_of_many_rows(B, form, dtype, hq, hkv, dim, rot, n_seqs, n, ahead):  # noqa: F811
+    """Batches large enough that a wavefront takes several tokens (append up to four, read up to 64) and that rows go past the caches (from 16 MB): ragged sequences, runs of more empty ones than
+    lanes, rows ahead of the first and behind the last, and tokens below position 0, whose queries are not written."""
+    import torch
+    gen, rng = generator(n), np.random.default_rng(n)
+    share = rng.exponential(1.0, n_seqs)
+    share[rng.random(n_seqs) < 0.2] = 0
+    if n_seqs > 128:
+        share[10:90] = 0
+    share[[0, -1]] = 0, 1.0
+    new = np.floor(share / share.sum() * (n - 10)).astype(np.int64)
+    new[1] += n - int(new.sum())
+    before = rng.integers(0, 20, n_seqs)
+    before[1] = -7                                                      # seven of its new tokens are at positions below 0
+    lens = new + before
+    off, page = offsets(new) + ahead, 16
+    used = -(-lens // page)
+    order = rng.permutation(int(used.sum()) + 2)
+    table = np.full((n_seqs, int(used.max())), -7, np.int32)
+    for b, first in enumerate(np.cumsum(used) - used):
+        table[b, :used[b]] = order[first:first + used[b]]
+    cfg = B.make_kv_config(dtype, hq, hkv, dim)
+    pool = B.make_kvq_pool(cfg, form, len(order), page)
+    cache = B.pack_kvq_cache(cfg, form, *pool, ints(table))
+    rows = rand(gen, dtype, ahead + n + 3, hq + 2 * hkv, dim)
+    q, k, v = rows[:, :hq], rows[:, hq:hq + hkv], rows[:, hq + hkv:]
+    q_out, faults = torch.full((len(rows), hq, dim), 7.0, device=DEV, dtype=torch_type(dtype)), torch.zeros(2, dtype=torch.int32, device=DEV)
+    f = B.flame_kv_rotation_frequencies(rot) if rot else np.zeros(0)
+    B.flame_kvq_append(cfg, cache, k, v, ints(off), ints(lens), q=q, q_out=q_out, rotation=B.make_kv_rotation(f) if rot else None, faults=faults[:1])
+    seq = np.repeat(np.arange(n_seqs), new)
+    position = np.arange(n) + ahead - off[seq + 1] + lens[seq]
+    there = position >= 0
+    assert int(faults[0]) == 2 and int((~there).sum()) == 7
+    row = np.flatnonzero(there) + ahead
+    page_of, slot = table[seq[there], position[there] // page], position[there] % page
+    empty = np.ones((len(order), page), bool)
+    empty[page_of, slot] = False
+    held = []
+    for data, codes_t, scales_t in ((k, pool[0], pool[2]), (v, pool[1], pool[3])):
+        got, got_scales = kv_oracle.unpack(codes_t.cpu().numpy(), form)[page_of, slot], scales_t.cpu().numpy()[page_of, slot]
+        x = host(data)[row]
+        held.append(kv_oracle.stored_values(got, got_scales, form))
+        if data is v or not rot:
+            codes, scales, _ = kv_oracle.quantise(x, form, dtype)
+            assert np.array_equal(got, codes) and np.array_equal(got_scales, scales)
+        else:
+            relative, least, limit = HALF[form]
+            turned, pair = kv_oracle.rotate(x, position[there], f, False), np.abs(x).max(-1, keepdims=True) * 2 * 2.0 ** -21
+            scale = np.repeat((np.abs(turned).reshape(*turned.shape[:-1], -1, 32).max(-1) + pair) * 2 / limit, 32, -1)
+            assert (np.abs(held[-1] - turned) <= pair * (1 + relative) + np.maximum(relative * np.abs(turned), least * scale)).all()
+        assert not codes_t.cpu().numpy()[empty].any() and not scales_t.cpu().numpy()[empty].any()
+    want = kv_oracle.rotate(host(q)[row], position[there], f, False)
+    wide = np.abs(host(q)[row]).max(-1, keepdims=True) * 2
+    assert (np.abs(host(q_out)[row] - want) <= HALF_STEP[dtype] * np.abs(want) + (wide * 2.0 ** -21 + (2.0 ** -25 if dtype == "f16" else 0) if rot else 0)).all() if rot else np.array_equal(host(q_out)[row], host(q)[row])
+    others = np.ones(len(rows), bool)
+    others[row] = False
+    others = torch.tensor(others, device=DEV)
+    assert bool((q_out[others] == 7.0).all()), torch.argwhere(others & (q_out != 7.0).flatten(1).any(1)).flatten()[:10].tolist()
+    back = [torch.full((len(rows), hkv, dim), 7.0, device=DEV, dtype=torch_type(dtype)) for _ in range(2)]
+    B.flame_kvq_read(cfg, cache, ints(off), ints(lens), *back, faults=faults[1:])
+    assert int(faults[1]) == 2
+    for x, values in zip(back, held):
+        assert np.array_equal(host(x)[row], values) and bool((x[others] == 7.0).all())
