@@ -920,3 +920,27 @@ def test_append_and_read_of_many_rows(B, form, dtype, hq, hkv, dim, rot, n_seqs,
     assert int(faults[1]) == 2
     for x, values in zip(back, held):
         assert np.array_equal(host(x)[row], values) and bool((x[others] == 7.0).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("form", FORMS)
+def test_values_below_the_normal_range(B, form, dtype):  # noqa: F811
+    """Blocks of subnormal values, alone and beside larger ones: rounded as all others, codes and scales bit for bit."""
+    import torch
+    tiny = np.concatenate([np.arange(0, 160) * 2.0 ** -133, [2.0 ** -127, 2.0 ** -126, 1.5 * 2.0 ** -127, 2.0 ** -125]])
+    tiny = np.concatenate([tiny, -tiny])
+    rng = np.random.default_rng(3)
+    x = rng.choice(tiny, (64, 1, 128))
+    x[32:, :, ::32] = 2.0 ** rng.integers(-126, -115, (32, 1, 4))
+    x = torch.tensor(x).to(torch_type(dtype)).to(DEV)
+    n = len(x)
+    cfg = B.make_kv_config(dtype, 1, 1, 128)
+    pool = B.make_kvq_pool(cfg, form, 1, n)
+    cache = B.pack_kvq_cache(cfg, form, *pool, ints([[0]]))
+    B.flame_kvq_append(cfg, cache, x, x, ints([0, n]), ints([n]))
+    back, back_v = torch.empty_like(x), torch.empty_like(x)
+    B.flame_kvq_read(cfg, cache, ints([0, n]), ints([n]), back, back_v)
+    codes, scales, values = kv_oracle.quantise(host(x), form, dtype)
+    got = kv_oracle.unpack(pool[0][0].cpu().numpy(), form)
+    assert np.array_equal(pool[2][0].cpu().numpy(), scales)
+    assert np.array_equal(got, codes) and np.array_equal(host(back), values) and np.array_equal(host(back_v), values)
