@@ -141,7 +141,10 @@ typedef struct {
  *                FLAME_KV_FAULT_OFFSET also for group_offsets that decrease, are below 0, or do not go from 0 to n_seqs: a sequence that is in no group, or of up to 64 groups in one
  *                behind offsets that are none, sees its own tokens alone.  (Of more groups, which rows see what is not defined.)
  *   workspace    of flame_kv_shared_workspace_bytes bytes for these numbers or larger ones; as in flame_kv_extend
- * n_tokens is below 2^24. */
+ * n_tokens is below 2^24.
+ * Made for few new rows of many sequences.  A sequence's own keys are read again for every 16 of its rows (new tokens times the query heads of a key head): long pieces behind a history are faster by flame_kv_extend on
+ * tables that name its pages for each (16 x 400 new behind 4 histories of 2000..8000, 32/8 heads of 128, f8: 1085 us here, 892 there).  And in a call of more than some 400 row tiles ((n_tokens G / 128 + n_groups) key heads,
+ * G query heads to a key head) a history is not cut along its keys, so that one much longer than the others takes its time alone. */
 int flame_kv_shared(const flame_kv_config *cfg, const flame_kv_cache *cache, const flame_kv_rows *q, const int32_t *q_offsets, const int32_t *kv_lens, const flame_kv_groups *groups,
                     int32_t n_seqs, int64_t n_tokens, const flame_kv_rows *out, void *workspace, int64_t workspace_bytes, int32_t *faults, void *stream);
 

@@ -253,6 +253,8 @@ static KvRoute route_of(const flame_kv_config &c, int32_t n_seqs, int64_t n_rows
   //     12800 (400 x 4, 8/2 of 64, over 1100) 68 | 73 (59 | 60)
   //   up to 32: 1024 (4 x 8, 32/8, over 4096) 26 | 26 (24 | 26), (over 16384) 54 | 70 (44 | 59), 8192 (32 x 8, over 2048) 69 | 76 (55 | 66), 2048 (32 x 8, 8/2 of 64, over 8192) 38 | 39 (34 | 32);
   //   more: 384 (12 new, 32/8, over 16384) 37 | 34 (31 | 33), 4096 (128 new) 48 | 32
+  // At the limit, 16384 (64 x 8, 32/8, over 2000), 126 | 98 (94 | 89): it stands there for batches of unequal sequences, whose average says little and which row tiles, one long piece on few workgroups, serve worse still:
+  //   63 single tokens over 2000 beside 400 new over 16384, 32/8 of 128, 439 | 511 (330 | 501), 8/2 of 64 68 | 74 (70 | 70); 400 new over 16384 beside 63 empty sequences 367 | 447 (298 | 443).
   const int64_t few = f32 ? (rows <= 32 ? kSplitRowHeads : 1024) : rows > 32 ? 0 : codes ? kSplitRowHeads : rows > 16 ? 512 : n_seqs > 64 ? 8192 : 2048;
   if (decode || (paged && capacity > kSmallCache && heads <= few)) return KvRoute{true, 1, 1, kv_split_workspace_bytes(c.head_dim, heads)};
   // Four or two wavefronts share 32 rows where that many workgroups of one wavefront per 32 rows leave places of the chip empty, or all are placed at
@@ -300,6 +302,8 @@ KvSharedRoute kv_shared_route(const flame_kv_config &c, int32_t n_groups, int64_
   const int64_t tile = kFlashRows / r.wavefronts;
   r.slots = n_rows * group / tile + n_groups;
   r.part_rows = n_groups > 0 ? heads : 0;
+  // (Beyond kPartWorkgroups histories are not cut, whatever their lengths: one much longer than the others is then walked by one workgroup a row tile and key head.  One of 100000 tokens among others of 1000, a single
+  // token each, 32/8 heads of 128, bf16: 48 groups 208 us, 56 or 64 groups 2760.)
   if (n_groups > 0 && (n_rows * group / 128 + n_groups) * c.n_kv_heads <= kPartWorkgroups && capacity >= kSmallCache) {
     if (n_groups <= 64) {
       // parts of equal length, for the chip's places

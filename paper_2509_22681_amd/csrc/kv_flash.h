@@ -42,7 +42,11 @@ template <typename T, int DH, int KP> constexpr int flash_lds_bytes() {
   return stages > parts ? stages : parts;
 }
 // Workgroups of 4 wavefronts on a compute unit, as LDS and registers allow (three in place of two of heads of 64: 64 prompts of 512..1024, 8 heads, 142 -> 114 us, one of 16384 395 -> 352;
-// four in place of three of 32 features 185 -> 165, fp32 three in place of two 622 -> 561).  Heads of 32 spill 1 to 4 registers at these bounds, none of it between the products.
+// four in place of three of 32 features 185 -> 165, fp32 three in place of two 622 -> 561).  Over values heads of 32 spill up to 4 registers at these bounds, none of it between the products.
+// Over codes, which wait for their conversion in registers, 16-bit heads of 32 spill 9 to 44 with one or two wavefronts to 32 rows, and heads of 64 7 to 11 with one (kv_shared.h: 13 to 29, and 6 to 10).  It pays all the
+// same where workgroups are many, and costs something where rounds are few.  us at these bounds | with one workgroup less, f8 (f4), bf16: 32 prompts of 512..1024, 16/16 heads of 32, 81 | 93 (85 | 92), fp32 287 | 313 (286 |
+// 312); 64 prompts, 8/2 heads of 64, 107 | 137 (106 | 136); 64 x 64 new over 300..4000, 16/16 of 32, 122 | 116 (123 | 109); 6 x 400 over 4000..16384 186 | 186 (186 | 172, fp16 172 | 172); histories that are shared: 400
+// sequences behind 4 of 4000..10000, 16/16 of 32, 57 | 60 (55 | 59), fp32 127 | 139 (127 | 138), 200 of them 40 | 40; 256 behind 2 of 8000..16000, 8/8 of 64, 37 | 41 (37 | 41).
 template <typename T, int DH, int KP> constexpr int flash_workgroups() {
   constexpr int lds = flash_lds_bytes<T, DH, KP>();
   return lds > 72 * 1024 ? 1 : DH == 32 && sizeof(T) == 2 && lds <= 32 * 1024 ? 4 : DH * sizeof(T) <= 128 && lds <= 40 * 1024 ? 3 : 2;

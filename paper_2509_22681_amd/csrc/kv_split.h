@@ -28,9 +28,9 @@ namespace flame {
 
 namespace {
 
-// Wavefronts per SIMD, as their registers allow, and in all.  Two tiles in flight fill the registers: 128 features spill 11 to 13 of 256 (48 to 56 bytes a lane), and scalars go to lanes of
+// Wavefronts per SIMD, as their registers allow, and in all.  Two tiles of values in flight fill the registers: 128 features spill 10 of 256 (44 bytes a lane; fp32 13, 56), and scalars go to lanes of
 // others (some 350 of 128 features in 16 bits, fewer in the rest).  Decoding of many keys runs at
-// memory speed all the same.
+// memory speed all the same.  Codes take less: none of their kernels spills vectors (128 features, 16 bits: f8 199 registers, f4 169).
 constexpr int split_occupancy(int dh) { return dh == 128 ? 2 : dh == 64 ? 3 : 4; }
 constexpr int split_workers(int dh) { return 1024 * split_occupancy(dh); }
 constexpr int kRows = 16;           // query rows of a unit

@@ -255,8 +255,10 @@ __global__ __launch_bounds__(64 * kWaves) void kvq_read_kernel(KvBatch batch, Kv
   }
 }
 
-// Rows of more than kStream bytes go past the caches: they are not there any more when the next kernel wants them, and what would be is lost.  us in the caches | past them: read f4 of 2 x 79 MB (bf16, 8 heads of
-// 128) 160 | 147, of 2 x 34 MB (8/2 heads of 64) 46 | 30, fp32 of 2 x 130 MB 160 | 95
+// Rows of more than kStream bytes go past the caches: they are not there any more when the next kernel wants them, and what would be is lost.  us in the caches | past them (of the two halves of a read, or of the
+// queries): read of 2 x 79 MB (bf16, 8 heads of 128) f8 56 | 37, f4 48 | 32, 2 x 40 MB 31 | 21, 26 | 18, 2 x 200 MB 127 | 112, 112 | 104, 2 x 34 MB (2 heads of 64) 28 | 19, 18 | 17, fp32 of 2 x 130 MB 73 | 49, 69 | 45;
+// append of 4800 tokens with 39 MB of queries (32/8 heads of 128) 29 | 21, of 12000 66 | 62, 63 | 59.  Up to 2 x 24 MB both take the same within a microsecond or two (2 x 16 MB 10.4 | 10.3, f4 10.1 | 8.6), and a next kernel
+// finds small rows in the caches.
 constexpr int64_t kStream = 16 << 20;
 template <typename F> void with_stored(int32_t dtype, int32_t form, int64_t bytes, F f) {
   kv_with_type(dtype, [&](auto t) {
