@@ -701,12 +701,6 @@ __device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_blo
     if (__syncthreads_or(odd)) {
       run(std::true_type{});
       __syncthreads();
-      // A row whose logits are all -infinity has zeros, though its weights of zero have met infinite values or NaN.  (NaN logits leave l NaN.)
-      const bool nothing = m == -INFINITY && pair_sum(l) == 0.f;
-#pragma unroll
-      for (int b = 0; b < DB; ++b)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[b][e] = nothing ? 0.f : o[b][e];
     }
   } else {
 #pragma unroll
@@ -759,11 +753,12 @@ __device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_blo
         if (f == 0) (SHARED ? kv_shared_state(a) : kv_part_state(a, a.splits))[to] = float2{top, sum};
         continue;
       }
-      const float inv = top == -INFINITY && sum == 0.f ? 0.f : 1.f / sum;
+      const bool nothing = top == -INFINITY && sum == 0.f;        // (as below)
+      const float inv = 1.f / sum;
       typedef T out4 __attribute__((ext_vector_type(4)));
       out4 y;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) y[e] = kv_round<T>(x[e] * inv);
+      for (int e = 0; e < 4; ++e) y[e] = kv_round<T>(nothing ? 0.f : x[e] * inv);
       *(out4 *)(a.out.p + (first + tk) * a.out.row + h * a.out.head + f * sizeof(T)) = y;
     }
     return;
@@ -790,7 +785,10 @@ __device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_blo
     if (lh == 0) (SHARED ? kv_shared_state(a) : kv_part_state(a, a.splits))[to] = float2{m, l};
     return;
   }
-  const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
+  // A row whose logits are all -infinity has zeros, though its weights of zero may have met infinite values or NaN.  (NaN logits leave l NaN.)  That is for the whole row to say: parts keep what they have
+  // met, as a row with a logit above -infinity in another part is NaN where it sees one.
+  const bool nothing = m == -INFINITY && l == 0.f;
+  const float inv = 1.f / l;
   // Rows to memory: each wavefront turns its 32 x DH patch in LDS, 16-byte chunks XORed with the row.
   char *patch = lds + wave * (32 * RB);
   static_assert(KP > 1 || 4 * 32 * RB <= 2 * STAGE, "the patches fit in the stages");
@@ -801,7 +799,7 @@ __device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_blo
       const int at = (8 * (e >> 2) + 4 * lh + (e & 3)) * DB * 4;
       struct alignas(4 * DB) Values { float f[DB]; } x;
 #pragma unroll
-      for (int b = 0; b < DB; ++b) x.f[b] = o[b][e] * inv;
+      for (int b = 0; b < DB; ++b) x.f[b] = nothing ? 0.f : o[b][e] * inv;
       *(Values *)(patch + l32 * RB + (((at >> 4) ^ (l32 & (CH - 1))) << 4) + (at & 15)) = x;
     }
   } else {
@@ -812,7 +810,7 @@ __device__ __forceinline__ void flash_rows(const KvAttention &a, unsigned my_blo
         // features 32 b + 8 i + 4 lh + 0..3 of row l32
         s16x4 x;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = __builtin_bit_cast(short, kv_round<T>(o[b][4 * i + e] * inv));
+        for (int e = 0; e < 4; ++e) x[e] = __builtin_bit_cast(short, kv_round<T>(nothing ? 0.f : o[b][4 * i + e] * inv));
         *(s16x4 *)(patch + l32 * RB + (((4 * b + i) ^ (l32 & (CH - 1))) << 4) + lh * 8) = x;
       }
   }
@@ -869,11 +867,12 @@ __global__ __launch_bounds__(256) void kv_flash_join_kernel(KvAttention a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) o[e] += x[e] * take;
   }
-  const float inv = m == -INFINITY && l == 0.f ? 0.f : 1.f / l;
+  const bool nothing = m == -INFINITY && l == 0.f;                // (see flash_rows)
+  const float inv = 1.f / l;
   typedef T out4 __attribute__((ext_vector_type(4)));
   out4 y;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) y[e] = kv_round<T>(o[e] * inv);
+  for (int e = 0; e < 4; ++e) y[e] = kv_round<T>(nothing ? 0.f : o[e] * inv);
   *(out4 *)(a.out.p + q_row * a.out.row + head * a.out.head + f * sizeof(T)) = y;
 }
 

@@ -13,7 +13,8 @@ namespace {
 
 // Row tiles over the histories in the first workgroups, split attention over the sequences' own keys in those behind them.  Own keys fill the places that the tiles leave, and where those take nearly all of the
 // chip's, as parts of equal length do, begin when tiles end (96 sequences with 20-800 tokens of their own behind 8 histories of 2000-12000, 32/8 heads of 128, bf16: tiles alone 54 us, own keys alone 45, both 100).
-// The registers are those of the two together at the row tiles' bounds: over values 128 features spill 19 (fp32 22) of 256, over codes heads of 32 spill 13 to 29 and heads of 64 up to 10 (see flash_workgroups).
+// The registers are those of the two together at the row tiles' bounds: over values 128 features spill 19 (fp32 22) of 256 and 16-bit heads of 64 with one
+// wavefront to 32 rows 7 of 168, over codes heads of 32 spill 13 to 29 and heads of 64 up to 10 (see flash_workgroups).
 template <typename T, int DH, int KP, int FORM>
 __global__ __launch_bounds__(256, (flash_workgroups<T, DH, KP>())) void kv_shared_kernel(KvAttention a, float *__restrict__ split_parts) {
   const unsigned tiles = gridDim.x - a.split_blocks;
@@ -108,7 +109,7 @@ __global__ __launch_bounds__(256) void kv_shared_join_kernel(KvAttention a, cons
     const float2 ml = kv_own_state(a)[from];
     add(ml.x, ml.y, *(const f32x4 *)(a.own + from * DH + f));
   }
-  // A row whose logits are all -infinity has zeros, though its weights of zero may have met infinite values or NaN among its own keys.  (NaN logits leave l NaN.)
+  // A row whose logits are all -infinity has zeros, though its weights of zero may have met infinite values or NaN.  (NaN logits leave l NaN.)
   const bool nothing = m == -INFINITY && l == 0.f;
   const float inv = 1.f / l;
   typedef T out4 __attribute__((ext_vector_type(4)));

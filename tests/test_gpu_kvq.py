@@ -944,3 +944,47 @@ def test_values_below_the_normal_range(B, form, dtype):  # noqa: F811
     got = kv_oracle.unpack(pool[0][0].cpu().numpy(), form)
     assert np.array_equal(pool[2][0].cpu().numpy(), scales)
     assert np.array_equal(got, codes) and np.array_equal(host(back), values) and np.array_equal(host(back_v), values)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("dim", [32, 64, 128])
+def test_nan_values_of_keys_whose_logits_are_minus_infinity(B, dtype, dim):  # noqa: F811
+    """Keys 0..699 have logits of -infinity, and one of them a value that is NaN: rows with a logit above that are NaN in its feature, by every call however the keys are cut, and those without one are zeros."""
+    import torch
+
+    from test_gpu_kv import spread
+    gen, n, at = generator(dim), 1500, 10
+    cfg = B.make_kv_config(dtype, 8, 2, dim)
+    k, v = rand(gen, dtype, 4096, 2, dim), rand(gen, dtype, 4096, 2, dim)
+    k[:700, :, 0] = -math.inf
+    v[at, :, 3] = math.nan
+
+    def check(out, positions, what):
+        seen, nothing = torch.tensor(positions >= 700, device=DEV), torch.tensor(positions < 700, device=DEV)
+        assert bool(out[seen][..., 3].isnan().all()) and bool(out[seen][..., 4:].isfinite().all()) and not bool(out[nothing].any()), what
+
+    def queries(tokens):
+        q = rand(gen, dtype, tokens, 8, dim)
+        q[..., 0] = 1.0
+        return q
+
+    for size in (0, 1, 2):
+        q = queries(n)
+        out = torch.full_like(q, 7.0)
+        B.flame_kv_prompt(cfg, q, k[:n], v[:n], ints(offsets([n] + spread(size, dtype, 2))), out)
+        check(out, np.arange(n), ("prompt", size))
+    for seqs, new, pages in ((1, 100, 256), (8, 300, 256), (8, 3, 256), (8, 1, 256), (2, 900, 100), (1, 900, 256), (1, 20, 256), (2, 40, 94)):
+        cache = B.pack_kv_cache(cfg, k.reshape(256, 16, 2, dim), v.reshape(256, 16, 2, dim), ints(np.tile(np.arange(pages), (seqs, 1))))
+        q, lens = queries(seqs * new), ints([n] * seqs)
+        positions = np.tile(np.arange(n - new, n), seqs)
+        out = torch.full_like(q, 7.0)
+        B.flame_kv_extend(cfg, cache, q, ints(offsets([new] * seqs)), lens, out, workspace_for(B, cfg, seqs, seqs * new))
+        check(out, positions, ("extend", seqs, new))
+        if new == 1:
+            out.fill_(7.0)
+            B.flame_kv_decode(cfg, cache, q, lens, out, workspace_for(B, cfg, seqs))
+            check(out, positions, "decode")
+        for prefix in (0, 690, 1000, 1300):
+            out.fill_(7.0)
+            B.flame_kv_shared(cfg, cache, q, ints(offsets([new] * seqs)), lens, ints([0, seqs]), ints([prefix] * seqs), out, shared_workspace(B, cfg, 1, seqs, len(q)))
+            check(out, positions, ("shared", seqs, new, pages, prefix))
